@@ -20,7 +20,7 @@
  * Conventions for every entry point:
  *  - Pointers are device pointers (HBM) owned by the caller; the library
  *    allocates no device memory. Inputs and outputs of one call must not
- *    overlap. Pointers must be 4-byte aligned.
+ *    overlap. Pointers must be 4-byte aligned, unless a call says otherwise.
  *  - `stream` is a hipStream_t (NULL = the default stream). Calls enqueue work
  *    on it and return without synchronising.
  *  - Arguments are checked before anything is launched; a rejected call
@@ -49,7 +49,9 @@
  *    accumulating adder and the element-wise MAC separately;
  *  - hobflops_pack_batch, hobflops_avgpool, hobflops_conv2d_algo,
  *    hobflops_conv2d_value_ops, hobflops_conv2d_value_tile,
- *    hobflops_conv2d_on_values and the *_supported queries are additions.
+ *    hobflops_conv2d_on_values and the *_supported queries are additions, and so
+ *    are the blocks of narrow floats and the gated block (hobflops_block_*,
+ *    hobflops_gated_*, hobflops_w4_*).
  */
 #ifndef HOBFLOPS_H
 #define HOBFLOPS_H
@@ -70,7 +72,7 @@ enum {
   HOBFLOPS_OK = 0,
   HOBFLOPS_EINVAL = -1,       /* bad size, shape, format or null pointer */
   HOBFLOPS_EUNSUPPORTED = -2, /* valid request, no generated kernel for it */
-  HOBFLOPS_EALIGN = -3,       /* a pointer is not 4-byte aligned */
+  HOBFLOPS_EALIGN = -3,       /* a pointer is not aligned (4 bytes, or as a call says) */
   HOBFLOPS_EHIP = -4          /* the HIP runtime reported an error */
 };
 
@@ -295,6 +297,99 @@ int hobflops_avgpool_netlist_ops(hobflops_fmt in_fmt, hobflops_fmt acc_fmt, hobf
 int hobflops_wait_failures(uint32_t* count, int reset);
 int hobflops_set_wait_limit(uint32_t sleeps);
 uint32_t hobflops_get_wait_limit(void);
+
+/* ---- Blocks of narrow floats, and a gated feed-forward block on them ----------
+ *
+ * Narrow codes: 1 + wE + wF bits, LSB first fraction, exponent, sign, without
+ * the exception field of the FloPoCo words above. Exponent 0 holds zero and the
+ * subnormal values F * 2^(1 - bias - wF), so that a code needs no exception field;
+ * (4, 3) gives S.1111.111 to NaN and has no infinity, (5, 2) keeps infinity and
+ * NaN in its highest exponent, (2, 1) has neither. A block is `group` consecutive
+ * values of a row under one scale: 32 values and a power of two for the 8-bit
+ * formats (4, 3) and (5, 2); 32, 64 or 128 values for the 4-bit format (2, 1).
+ * The value of a code is the format's value times the scale.
+ *   codes:  uint8 [rows][ceil(cols * bits / 8)]; of two 4-bit codes in a byte the
+ *           even column is the low half
+ *   scales: [rows][ceil(cols / group)], HOBFLOPS_SCALE_POW2: uint8 s for
+ *           2^(s - 127), 255 for NaN; _BF16, _F32: the factor itself
+ * Types of tensors: float32, bfloat16 and float16 (pointers aligned to the
+ * element; HOBFLOPS_EALIGN otherwise). Rows are `ld` elements apart (ld >= the
+ * row's length). Where a call takes a workspace, its size comes from the query;
+ * it is device memory of the caller's, 16-byte aligned, whose contents mean
+ * nothing between calls. */
+enum { HOBFLOPS_TYPE_F32 = 0, HOBFLOPS_TYPE_BF16 = 1, HOBFLOPS_TYPE_F16 = 2 };
+enum { HOBFLOPS_SCALE_POW2 = 0, HOBFLOPS_SCALE_BF16 = 1, HOBFLOPS_SCALE_F32 = 2 };
+enum { HOBFLOPS_GATE_SILU = 0, HOBFLOPS_GATE_GELU = 1, HOBFLOPS_GATE_RELU = 2 };
+
+/* Values to blocks. With a power-of-two scale 2^k, k is the smallest number
+ * >= -110 for which no finite value of the group rounds beyond the format's
+ * largest; the other scales are the group's largest magnitude / 6, rounded to the
+ * scale's type (largest codes of 6 are kept where that rounding makes a value
+ * larger). Codes round to nearest, ties to the even code. NaN and infinities do
+ * not count for a group's scale: in (5, 2) they keep their codes, in (4, 3) both
+ * become NaN, in (2, 1), which can hold neither, the group's scale becomes NaN. */
+int hobflops_block_pack(const void* src, int type, int64_t rows, int64_t cols, int64_t ld,
+                        hobflops_fmt f, int group, int scale, uint8_t* codes, void* scales,
+                        void* stream);
+
+/* Blocks to values, rounded to nearest even in dst's type (exact in float32 and
+ * bfloat16 but for values of 2^128 and above, which go to infinity). */
+int hobflops_block_unpack(const uint8_t* codes, const void* scales, int64_t rows, int64_t cols,
+                          hobflops_fmt f, int group, int scale, void* dst, int type, int64_t ld,
+                          void* stream);
+
+/* The gated block of T tokens (T >= 0):
+ *   g = x w_gate^T, u = x w_up^T, h = act(g) * u
+ * x [T][D] (rows ldx apart), w_gate and w_up [F][D] (ldw), h and its gradient dh
+ * [T][F] (ldh), of type bfloat16 or float16; sums, g, u and the activation in
+ * float32, one rounding at the end. act: HOBFLOPS_GATE_*, g sigmoid(g), g Phi(g)
+ * (Phi the normal distribution) or max(g, 0).
+ * ckpt: (4, 3) or (5, 2), the format of the checkpoints; {0, 0}: none, forward
+ * only. */
+typedef struct {
+  int64_t T, D, F;
+  int64_t ldx, ldw, ldh;
+  int type, act;
+  hobflops_fmt ckpt;
+} hobflops_gated_desc;
+
+/* Workspace bytes of a forward (backward 0) or backward (1) call. */
+int hobflops_gated_workspace(const hobflops_gated_desc* d, int backward, int64_t* bytes);
+
+/* Forward. With d->ckpt the blocks of g and u, [T] rows of F values, are written
+ * too (from their float32 values); without, the four pointers are not used. */
+int hobflops_gated_forward(const hobflops_gated_desc* d, const void* x, const void* w_gate,
+                           const void* w_up, void* h, uint8_t* g_codes, uint8_t* g_scales,
+                           uint8_t* u_codes, uint8_t* u_scales, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* Gradients of the loss by x, w_gate and w_up from dh and the blocks of x ([T]
+ * rows of D values: hobflops_block_pack), g and u:
+ *   dg = dh * u * act'(g), du = dh * act(g)   (act' of max(g, 0) is 0 at 0)
+ *   dx = dg w_gate + du w_up [T][D], dw_gate = dg^T x, dw_up = du^T x [F][D]
+ * all dense and of d->type. dg and du are rounded to d->type before the products,
+ * whose sums are float32. With T = 0 the gradients of the weights are zero.
+ * Sums run in a fixed order: the same inputs give the same bits. */
+int hobflops_gated_backward(const hobflops_gated_desc* d, const void* dh, const uint8_t* x_codes,
+                            const uint8_t* x_scales, const uint8_t* g_codes,
+                            const uint8_t* g_scales, const uint8_t* u_codes,
+                            const uint8_t* u_scales, const void* w_gate, const void* w_up,
+                            void* dx, void* dw_gate, void* dw_up, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/* Products of T tokens (T >= 0, meant for few) with 4-bit weights, blocks of the
+ * format (2, 1), [N] rows of K values: y[t][n] = sum_k x[t][k] w[n][k]. x [T][K]
+ * (rows ldx apart) and y [T][N] (ldy) of type bfloat16 or float16, sums in
+ * float32. group: 32, 64 or 128; scale: HOBFLOPS_SCALE_*. */
+int hobflops_w4_linear(const void* x, int type, int64_t T, int64_t K, int64_t N, int64_t ldx,
+                       const uint8_t* codes, const void* scales, int group, int scale, void* y,
+                       int64_t ldy, void* stream);
+
+/* The gated block on 4-bit weights, in one launch: h = act(x Wg^T) * (x Wu^T). */
+int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, int64_t ldx,
+                      const uint8_t* g_codes, const void* g_scales, const uint8_t* u_codes,
+                      const void* u_scales, int group, int scale, int act, void* h, int64_t ldh,
+                      void* stream);
 
 /* Text for a status code; for HOBFLOPS_EHIP, the last HIP error of this
  * thread. The pointer stays valid until the next call on the same thread. */

@@ -754,7 +754,8 @@ def _compile(src, obj, stats=None):
 def build(jobs=None, verbose=True):
     """Generate and compile everything; returns the library path."""
     gen_files = generate(verbose=verbose)
-    srcs = [os.path.join(HERE, "csrc", "abi.hip"), os.path.join(HERE, "csrc", "pack.hip")] + gen_files
+    srcs = [os.path.join(HERE, "csrc", n) for n in
+            ("abi.hip", "pack.hip", "block.hip", "gated.hip", "weights4.hip")] + gen_files
     os.makedirs(OBJ, exist_ok=True)
     jobs = jobs or min(16, os.cpu_count() or 4)
     stats = {}

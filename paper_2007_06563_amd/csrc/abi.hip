@@ -12,6 +12,7 @@
 #include <mutex>
 #include <vector>
 
+#include "block.hpp"
 #include "hobflops.h"
 #include "pack.hpp"
 #include "registry.hpp"
@@ -153,6 +154,81 @@ int conv_check(const hobflops_conv_desc* d) {
       (int64_t)d->KH * d->KW * d->C > (int64_t)1 << 24 || MT > 65535)
     return HOBFLOPS_EINVAL;
   return HOBFLOPS_OK;
+}
+
+// ---- blocks of narrow floats and the gated block --------------------------------
+
+int type_ok(int type) { return type >= HOBFLOPS_TYPE_F32 && type <= HOBFLOPS_TYPE_F16; }
+int type_bytes(int type) { return type == HOBFLOPS_TYPE_F32 ? 4 : 2; }
+int scale_bytes(int scale) {
+  return scale == HOBFLOPS_SCALE_POW2 ? 1 : scale == HOBFLOPS_SCALE_BF16 ? 2 : 4;
+}
+int aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+
+// The kernels' index of a narrow format, or -1.
+int narrow_format(hobflops_fmt f) {
+  if (f.wE == 4 && f.wF == 3) return kE4M3;
+  if (f.wE == 5 && f.wF == 2) return kE5M2;
+  if (f.wE == 2 && f.wF == 1) return kE2M1;
+  return -1;
+}
+
+// Extents of a matrix: the bytes of rows * ld elements are far below 2^63, and a
+// row has fewer than 2^31 values.
+int extent_ok(int64_t rows, int64_t cols, int64_t ld) {
+  return rows >= 0 && cols >= 0 && cols < ((int64_t)1 << 31) && ld >= cols &&
+         ld < ((int64_t)1 << 40) && rows < ((int64_t)1 << 31) &&
+         (rows == 0 || ld < ((int64_t)1 << 58) / rows);
+}
+
+int block_check(int type, int64_t rows, int64_t cols, int64_t ld, hobflops_fmt f, int group,
+                int scale, int* fmt) {
+  if (!extent_ok(rows, cols, ld) || !type_ok(type)) return HOBFLOPS_EINVAL;
+  if (f.wE < 1 || f.wF < 1) return HOBFLOPS_EINVAL;
+  if (group != 32 && group != 64 && group != 128) return HOBFLOPS_EINVAL;
+  if (scale < HOBFLOPS_SCALE_POW2 || scale > HOBFLOPS_SCALE_F32) return HOBFLOPS_EINVAL;
+  *fmt = narrow_format(f);
+  if (*fmt < 0) return HOBFLOPS_EUNSUPPORTED;
+  if (*fmt != kE2M1 && (group != 32 || scale != HOBFLOPS_SCALE_POW2)) return HOBFLOPS_EUNSUPPORTED;
+  return HOBFLOPS_OK;
+}
+
+// Checks of a gated block's descriptor; *fmt: the checkpoints' format, -1 for none.
+int gated_check(const hobflops_gated_desc* d, int backward, int* fmt) {
+  if (!d) return HOBFLOPS_EINVAL;
+  if (d->D < 1 || d->F < 1 || !extent_ok(d->T, d->D, d->ldx) || !extent_ok(d->F, d->D, d->ldw) ||
+      !extent_ok(d->T, d->F, d->ldh) || d->T > (int64_t)1 << 24 || d->D > (int64_t)1 << 20 ||
+      d->F > (int64_t)1 << 20)
+    return HOBFLOPS_EINVAL;
+  if (!type_ok(d->type) || d->act < HOBFLOPS_GATE_SILU || d->act > HOBFLOPS_GATE_RELU)
+    return HOBFLOPS_EINVAL;
+  *fmt = -1;
+  if (d->ckpt.wE != 0 || d->ckpt.wF != 0) {
+    if (d->ckpt.wE < 1 || d->ckpt.wF < 1) return HOBFLOPS_EINVAL;
+    *fmt = narrow_format(d->ckpt);
+    if (*fmt != kE4M3 && *fmt != kE5M2) return HOBFLOPS_EUNSUPPORTED;
+  } else if (backward) {
+    return HOBFLOPS_EINVAL;
+  }
+  return d->type == HOBFLOPS_TYPE_F32 ? HOBFLOPS_EUNSUPPORTED : HOBFLOPS_OK;
+}
+
+int w4_run(W4Product p, bool gated, void* stream) {
+  if (!extent_ok(p.T, p.K, p.ldx) || !extent_ok(p.T, p.N, p.ldy) || p.K < 1 || p.N < 1 ||
+      p.K > (int64_t)1 << 24 || p.N > (int64_t)1 << 24 || !type_ok(p.type))
+    return HOBFLOPS_EINVAL;
+  if (p.group != 32 && p.group != 64 && p.group != 128) return HOBFLOPS_EINVAL;
+  if (p.scale < HOBFLOPS_SCALE_POW2 || p.scale > HOBFLOPS_SCALE_F32) return HOBFLOPS_EINVAL;
+  if (gated && (p.act < HOBFLOPS_GATE_SILU || p.act > HOBFLOPS_GATE_RELU)) return HOBFLOPS_EINVAL;
+  if (p.type == HOBFLOPS_TYPE_F32) return HOBFLOPS_EUNSUPPORTED;
+  if (p.T == 0) return HOBFLOPS_OK;
+  if (!p.x || !p.y || !p.w.codes || !p.w.scales || (gated && (!p.w_up.codes || !p.w_up.scales)))
+    return HOBFLOPS_EINVAL;
+  const int sb = scale_bytes(p.scale);
+  if (!aligned_to(p.x, 2) || !aligned_to(p.y, 2) || !aligned_to(p.w.scales, sb) ||
+      (gated && !aligned_to(p.w_up.scales, sb)))
+    return HOBFLOPS_EALIGN;
+  return hip_status(launch_w4(p, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -535,12 +611,117 @@ int hobflops_set_wait_limit(uint32_t sleeps) {
 
 uint32_t hobflops_get_wait_limit(void) { return g_spin_cap.load(std::memory_order_relaxed); }
 
+int hobflops_block_pack(const void* src, int type, int64_t rows, int64_t cols, int64_t ld,
+                        hobflops_fmt f, int group, int scale, uint8_t* codes, void* scales,
+                        void* stream) {
+  int fmt = -1;
+  const int st = block_check(type, rows, cols, ld, f, group, scale, &fmt);
+  if (st != HOBFLOPS_OK) return st;
+  if (rows == 0 || cols == 0) return HOBFLOPS_OK;
+  if (!src || !codes || !scales) return HOBFLOPS_EINVAL;
+  if (!aligned_to(src, type_bytes(type)) || !aligned_to(scales, scale_bytes(scale)))
+    return HOBFLOPS_EALIGN;
+  const BlockTensor t{src, type, rows, cols, ld, codes, scales, group, scale};
+  return hip_status(launch_block_pack(t, fmt, (hipStream_t)stream));
+}
+
+int hobflops_block_unpack(const uint8_t* codes, const void* scales, int64_t rows, int64_t cols,
+                          hobflops_fmt f, int group, int scale, void* dst, int type, int64_t ld,
+                          void* stream) {
+  int fmt = -1;
+  const int st = block_check(type, rows, cols, ld, f, group, scale, &fmt);
+  if (st != HOBFLOPS_OK) return st;
+  if (rows == 0 || cols == 0) return HOBFLOPS_OK;
+  if (!dst || !codes || !scales) return HOBFLOPS_EINVAL;
+  if (!aligned_to(dst, type_bytes(type)) || !aligned_to(scales, scale_bytes(scale)))
+    return HOBFLOPS_EALIGN;
+  const BlockTensor t{dst,   type, rows, cols, ld, const_cast<uint8_t*>(codes),
+                      const_cast<void*>(scales), group, scale};
+  return hip_status(launch_block_unpack(t, fmt, (hipStream_t)stream));
+}
+
+int hobflops_gated_workspace(const hobflops_gated_desc* d, int backward, int64_t* bytes) {
+  int fmt = -1;
+  if (!bytes) return HOBFLOPS_EINVAL;
+  const int st = gated_check(d, backward, &fmt);
+  if (st != HOBFLOPS_OK) return st;
+  *bytes = backward ? gated_backward_workspace(*d) : gated_forward_workspace(*d);
+  return HOBFLOPS_OK;
+}
+
+int hobflops_gated_forward(const hobflops_gated_desc* d, const void* x, const void* w_gate,
+                           const void* w_up, void* h, uint8_t* g_codes, uint8_t* g_scales,
+                           uint8_t* u_codes, uint8_t* u_scales, void* workspace,
+                           int64_t workspace_bytes, void* stream) {
+  int fmt = -1;
+  const int st = gated_check(d, 0, &fmt);
+  if (st != HOBFLOPS_OK) return st;
+  if (d->T == 0) return HOBFLOPS_OK;
+  if (!x || !w_gate || !w_up || !h) return HOBFLOPS_EINVAL;
+  if (fmt >= 0 && (!g_codes || !g_scales || !u_codes || !u_scales)) return HOBFLOPS_EINVAL;
+  const int64_t need = gated_forward_workspace(*d);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return HOBFLOPS_EINVAL;
+  if (!aligned_to(x, 2) || !aligned_to(w_gate, 2) || !aligned_to(w_up, 2) || !aligned_to(h, 2) ||
+      (need > 0 && !aligned_to(workspace, 16)))
+    return HOBFLOPS_EALIGN;
+  const GatedForward p{x, w_gate, w_up, h, {g_codes, g_scales}, {u_codes, u_scales}, workspace};
+  return hip_status(launch_gated_forward(*d, p, fmt, (hipStream_t)stream));
+}
+
+int hobflops_gated_backward(const hobflops_gated_desc* d, const void* dh, const uint8_t* x_codes,
+                            const uint8_t* x_scales, const uint8_t* g_codes,
+                            const uint8_t* g_scales, const uint8_t* u_codes,
+                            const uint8_t* u_scales, const void* w_gate, const void* w_up,
+                            void* dx, void* dw_gate, void* dw_up, void* workspace,
+                            int64_t workspace_bytes, void* stream) {
+  int fmt = -1;
+  const int st = gated_check(d, 1, &fmt);
+  if (st != HOBFLOPS_OK) return st;
+  if (!dw_gate || !dw_up) return HOBFLOPS_EINVAL;
+  const int64_t need = gated_backward_workspace(*d);
+  if (d->T > 0 && (!dh || !x_codes || !x_scales || !g_codes || !g_scales || !u_codes ||
+                   !u_scales || !w_gate || !w_up || !dx || !workspace || workspace_bytes < need))
+    return HOBFLOPS_EINVAL;
+  if (!aligned_to(dh, 2) || !aligned_to(w_gate, 2) || !aligned_to(w_up, 2) || !aligned_to(dx, 2) ||
+      !aligned_to(dw_gate, 2) || !aligned_to(dw_up, 2) || (d->T > 0 && !aligned_to(workspace, 16)))
+    return HOBFLOPS_EALIGN;
+  GatedBackward p{};
+  p.dh = dh;
+  p.w_gate = w_gate;
+  p.w_up = w_up;
+  p.x = {const_cast<uint8_t*>(x_codes), const_cast<uint8_t*>(x_scales)};
+  p.gate = {const_cast<uint8_t*>(g_codes), const_cast<uint8_t*>(g_scales)};
+  p.up = {const_cast<uint8_t*>(u_codes), const_cast<uint8_t*>(u_scales)};
+  p.dx = dx;
+  p.dw_gate = dw_gate;
+  p.dw_up = dw_up;
+  p.workspace = workspace;
+  return hip_status(launch_gated_backward(*d, p, fmt, (hipStream_t)stream));
+}
+
+int hobflops_w4_linear(const void* x, int type, int64_t T, int64_t K, int64_t N, int64_t ldx,
+                       const uint8_t* codes, const void* scales, int group, int scale, void* y,
+                       int64_t ldy, void* stream) {
+  const W4Product p{x, type, T, K, N, ldx, ldy, {codes, scales}, {nullptr, nullptr},
+                    group, scale, HOBFLOPS_GATE_SILU, y};
+  return w4_run(p, false, stream);
+}
+
+int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, int64_t ldx,
+                      const uint8_t* g_codes, const void* g_scales, const uint8_t* u_codes,
+                      const void* u_scales, int group, int scale, int act, void* h, int64_t ldh,
+                      void* stream) {
+  const W4Product p{x, type, T, K, N, ldx, ldh, {g_codes, g_scales}, {u_codes, u_scales},
+                    group, scale, act, h};
+  return w4_run(p, true, stream);
+}
+
 const char* hobflops_status_string(int status) {
   switch (status) {
     case HOBFLOPS_OK: return "ok";
     case HOBFLOPS_EINVAL: return "invalid argument";
     case HOBFLOPS_EUNSUPPORTED: return "no generated kernel for this format combination";
-    case HOBFLOPS_EALIGN: return "pointer not 4-byte aligned";
+    case HOBFLOPS_EALIGN: return "pointer not aligned";
     case HOBFLOPS_EHIP: return g_errbuf[0] ? g_errbuf : "HIP error";
     default: return "unknown status";
   }

@@ -5,6 +5,7 @@ torch's current stream; torch supplies device memory and streams. There is no
 CPU fallback: a missing library or a host tensor raises.
 Plane tensors are int32 (the bit patterns of PL32 words).
 """
+import collections
 import ctypes
 import os
 
@@ -20,6 +21,11 @@ ROUND_NEAREST_EVEN, ROUND_TOWARD_ZERO, ORDER_KY_KX_C = 0, 1, 0
 ALGO_AUTO, ALGO_FUSED, ALGO_SPLIT, ALGO_SPLIT_COMPACT = 0, 1, 2, 3
 OFM_PLANES, OFM_F32, OFM_CODE = 0, 1, 2
 TILE_112X64, TILE_56X64, TILE_32X64, TILE_32X32, TILE_16X32 = 1, 2, 3, 4, 5
+SCALE_POW2, SCALE_BF16, SCALE_F32 = 0, 1, 2
+GATE_SILU, GATE_GELU, GATE_RELU = 0, 1, 2
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_SCALES = {torch.uint8: SCALE_POW2, torch.bfloat16: SCALE_BF16, torch.float32: SCALE_F32}
+_SCALE_TYPES = {v: k for k, v in _SCALES.items()}
 
 
 class HobflopsError(RuntimeError):
@@ -49,13 +55,25 @@ class PackJob(ctypes.Structure):
                 ("len", ctypes.c_int64), ("planes", ctypes.c_void_p)]
 
 
+class GatedDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int64), ("F", ctypes.c_int64),
+                ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldh", ctypes.c_int64),
+                ("type", ctypes.c_int), ("act", ctypes.c_int), ("ckpt", Fmt)]
+
+
+# What gated_forward keeps for gated_backward: (codes, scales) of x, g and u.
+GatedSaved = collections.namedtuple("GatedSaved", "x gate up fmt")
+
+
 EXPORTS = ("hobflops_plane_words", "hobflops_pack", "hobflops_pack_batch", "hobflops_unpack",
            "hobflops_conv2d",
            "hobflops_conv2d_supported", "hobflops_conv2d_algo", "hobflops_conv2d_value_ops",
            "hobflops_conv2d_value_tile", "hobflops_conv2d_on_values",
            "hobflops_muladd", "hobflops_muladd_supported",
            "hobflops_netlist_ops", "hobflops_avgpool", "hobflops_avgpool_supported",
-           "hobflops_avgpool_netlist_ops", "hobflops_wait_failures", "hobflops_set_wait_limit",
+           "hobflops_avgpool_netlist_ops", "hobflops_block_pack", "hobflops_block_unpack",
+           "hobflops_gated_workspace", "hobflops_gated_forward", "hobflops_gated_backward",
+           "hobflops_w4_linear", "hobflops_w4_gated", "hobflops_wait_failures", "hobflops_set_wait_limit",
            "hobflops_get_wait_limit", "hobflops_status_string")
 
 
@@ -84,6 +102,14 @@ def lib():
         L.hobflops_avgpool.argtypes = [vp, vp, ci, ci, ci, ci, Fmt, Fmt, Fmt, ci, vp]
         L.hobflops_avgpool_supported.argtypes = [Fmt, Fmt, Fmt, ci]
         L.hobflops_avgpool_netlist_ops.argtypes = [Fmt, Fmt, Fmt, ci] + [ctypes.POINTER(ci)] * 2
+        L.hobflops_block_pack.argtypes = [vp, ci, i64, i64, i64, Fmt, ci, ci, vp, vp, vp]
+        L.hobflops_block_unpack.argtypes = [vp, vp, i64, i64, Fmt, ci, ci, vp, ci, i64, vp]
+        L.hobflops_gated_workspace.argtypes = [ctypes.POINTER(GatedDesc), ci, ctypes.POINTER(i64)]
+        L.hobflops_gated_forward.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 9 + [i64, vp]
+        L.hobflops_gated_backward.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 13 + [i64, vp]
+        L.hobflops_w4_linear.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, ci, vp, i64, vp]
+        L.hobflops_w4_gated.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, vp, vp, ci, ci, ci, vp,
+                                        i64, vp]
         L.hobflops_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ci]
         L.hobflops_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.hobflops_get_wait_limit.argtypes = []
@@ -356,3 +382,201 @@ def set_wait_limit(sleeps):
 
 def get_wait_limit():
     return int(lib().hobflops_get_wait_limit())
+
+
+# ---- blocks of narrow floats and the gated feed-forward block ------------------
+# The launches go to the current stream of the first tensor's device.
+
+
+def _rows(t, name):
+    """(pointer, rows, columns, elements between rows) of a GPU matrix whose rows are dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("hobflops operates on GPU tensors only")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: a matrix is needed, not {tuple(t.shape)}")
+    r, c = t.shape
+    sr, sc = t.stride()
+    if (c > 1 and sc != 1) or (r > 1 and sr < c):
+        raise ValueError(f"{name}: rows must be dense and not overlap")
+    return t.data_ptr(), r, c, (sr if r > 1 else c)
+
+
+def _type(t, name):
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{name}: float32, bfloat16 or float16 values are needed, not {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _dense(t, shape, dtype, device, name):
+    """The pointer of a dense tensor of this shape, type and device."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name}: a tensor on {device} is needed")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} is needed")
+    return t.data_ptr()
+
+
+def _out_rows(t, shape, dtype, device, name):
+    """A caller's output matrix (dense rows), or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: a {dtype} tensor {tuple(shape)} on {device} is needed")
+    return t
+
+
+def _raw_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def block_shapes(rows, cols, f, group=32):
+    """The shapes of the codes and of the scales of a [rows, cols] matrix in blocks."""
+    f = fmt(f)
+    bits = 1 + f.wE + f.wF
+    return (rows, (cols * bits + 7) // 8), (rows, -(-cols // group))
+
+
+def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
+    """float32, bfloat16 or float16 values [rows, cols] (dense rows, any distance apart) -> codes
+    of the narrow format f ((4, 3), (5, 2): 8 bits, (2, 1): 4 bits), uint8, and the scales of
+    their groups: (codes, scales). 8-bit codes take groups of 32 and SCALE_POW2."""
+    f = fmt(f)
+    ptr, rows, cols, ld = _rows(src, "block_pack src")
+    kind = _type(src, "block_pack src")
+    cshape, sshape = block_shapes(rows, cols, f, group) if group in (32, 64, 128) else ((0,), (0,))
+    stype = _SCALE_TYPES.get(scale, torch.uint8)
+    if codes is None:
+        codes = torch.empty(cshape, dtype=torch.uint8, device=src.device)
+    if scales is None:
+        scales = torch.empty(sshape, dtype=stype, device=src.device)
+    pc = _dense(codes, cshape, torch.uint8, src.device, "block_pack codes")
+    ps = _dense(scales, sshape, stype, src.device, "block_pack scales")
+    _check(lib().hobflops_block_pack(ptr, kind, rows, cols, ld, f, group, scale, pc, ps,
+                                     _raw_stream(src.device)))
+    return codes, scales
+
+
+def block_unpack(codes, scales, cols, f, group=32, dtype=torch.float32, out=None):
+    """Codes and scales of block_pack -> the values they stand for, [rows, cols]."""
+    f = fmt(f)
+    if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dim() != 2:
+        raise TypeError("block_unpack: codes [rows, bytes] on a GPU are needed")
+    rows = codes.shape[0]
+    cshape, sshape = block_shapes(rows, cols, f, group) if group in (32, 64, 128) else ((0,), (0,))
+    if scales.dtype not in _SCALES:
+        raise TypeError(f"block_unpack: scales of {scales.dtype}")
+    pc = _dense(codes, cshape, torch.uint8, codes.device, "block_unpack codes")
+    ps = _dense(scales, sshape, scales.dtype, codes.device, "block_unpack scales")
+    if out is not None:
+        dtype = out.dtype
+    out = _out_rows(out, (rows, cols), dtype, codes.device, "block_unpack out")
+    ptr, _, _, ld = _rows(out, "block_unpack out")
+    _check(lib().hobflops_block_unpack(pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
+                                       _type(out, "block_unpack out"), ld,
+                                       _raw_stream(codes.device)))
+    return out
+
+
+def _gated_weights(x, w_gate, w_up):
+    """(pointers, F, D, row distance) of the two weights."""
+    pg, F, D, ldw = _rows(w_gate, "gated w_gate")
+    pu, Fu, Du, ldu = _rows(w_up, "gated w_up")
+    if (Fu, Du) != (F, D) or ldu != ldw:
+        raise ValueError("gated: w_gate and w_up must have one shape and row distance")
+    if w_gate.dtype != x.dtype or w_up.dtype != x.dtype:
+        raise TypeError("gated: the weights must have the type of the activations")
+    if w_gate.device != x.device or w_up.device != x.device:
+        raise TypeError("gated: tensors of different devices")
+    return pg, pu, F, D, ldw
+
+
+def _workspace(d, backward, device):
+    n = ctypes.c_int64()
+    _check(lib().hobflops_gated_workspace(ctypes.byref(d), backward, ctypes.byref(n)))
+    if n.value == 0:
+        return None, 0, 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n.value
+
+
+def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
+    """h = act(x w_gate^T) * (x w_up^T): x [T, D], w_gate and w_up [F, D], bfloat16 or float16 ->
+    h [T, F]. With ckpt, an 8-bit format: (h, saved), the blocks of x, g and u in that format, for
+    gated_backward."""
+    px, T, D, ldx = _rows(x, "gated_forward x")
+    pg, pu, F, Dw, ldw = _gated_weights(x, w_gate, w_up)
+    if Dw != D:
+        raise ValueError("gated_forward: x and the weights differ in D")
+    h = _out_rows(out, (T, F), x.dtype, x.device, "gated_forward out")
+    ph, _, _, ldh = _rows(h, "gated_forward out")
+    f = Fmt(0, 0) if ckpt is None else fmt(ckpt)
+    d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f)
+    ws, pw, nw = _workspace(d, 0, x.device)
+    stream = _raw_stream(x.device)
+    if ckpt is None:
+        _check(lib().hobflops_gated_forward(ctypes.byref(d), px, pg, pu, ph, None, None, None,
+                                            None, pw, nw, stream))
+        return h
+    cshape, sshape = block_shapes(T, F, f)
+    blocks = [torch.empty(s, dtype=torch.uint8, device=x.device)
+              for s in (cshape, sshape, cshape, sshape)]
+    _check(lib().hobflops_gated_forward(ctypes.byref(d), px, pg, pu, ph,
+                                        *[b.data_ptr() for b in blocks], pw, nw, stream))
+    return h, GatedSaved(block_pack(x, f), tuple(blocks[:2]), tuple(blocks[2:]), f)
+
+
+def gated_backward(dh, saved, w_gate, w_up, act=GATE_SILU):
+    """The gradients (dx, dw_gate, dw_up) of gated_forward from dh [T, F] and what it saved."""
+    ph, T, F, ldh = _rows(dh, "gated_backward dh")
+    pg, pu, Fw, D, ldw = _gated_weights(dh, w_gate, w_up)
+    if Fw != F:
+        raise ValueError("gated_backward: dh and the weights differ in F")
+    f = saved.fmt
+    dev, dtype = dh.device, dh.dtype
+    ptrs = []
+    for (codes, scales), cols, name in ((saved.x, D, "x"), (saved.gate, F, "gate"),
+                                        (saved.up, F, "up")):
+        cshape, sshape = block_shapes(T, cols, f)
+        ptrs += [_dense(codes, cshape, torch.uint8, dev, f"gated_backward saved.{name} codes"),
+                 _dense(scales, sshape, torch.uint8, dev, f"gated_backward saved.{name} scales")]
+    d = GatedDesc(T, D, F, D, ldw, ldh, _type(dh, "gated_backward dh"), act, f)
+    ws, pw, nw = _workspace(d, 1, dev)
+    dx = torch.empty((T, D), dtype=dtype, device=dev)
+    dw_gate = torch.empty((F, D), dtype=dtype, device=dev)
+    dw_up = torch.empty((F, D), dtype=dtype, device=dev)
+    _check(lib().hobflops_gated_backward(ctypes.byref(d), ph, *ptrs, pg, pu, dx.data_ptr(),
+                                         dw_gate.data_ptr(), dw_up.data_ptr(), pw, nw,
+                                         _raw_stream(dev)))
+    return dx, dw_gate, dw_up
+
+
+def _w4(x, weights, group, out, name):
+    """Checked arguments of a product with 4-bit weights, up to and from the weights' pointers."""
+    px, T, K, ldx = _rows(x, f"{name} x")
+    N, scale, ptrs = weights[0].shape[0], weights[1].dtype, []
+    if scale not in _SCALES:
+        raise TypeError(f"{name}: scales of {scale}")
+    if group not in (32, 64, 128):
+        raise ValueError(f"{name}: groups of 32, 64 or 128 are supported, not {group}")
+    for i in range(0, len(weights), 2):
+        ptrs += [_dense(weights[i], (N, (K + 1) // 2), torch.uint8, x.device, f"{name} codes"),
+                 _dense(weights[i + 1], (N, -(-K // group)), scale, x.device, f"{name} scales")]
+    y = _out_rows(out, (T, N), x.dtype, x.device, f"{name} out")
+    py, _, _, ldy = _rows(y, f"{name} out")
+    head = (px, _type(x, f"{name} x"), T, K, N, ldx, *ptrs, group, _SCALES[scale])
+    return y, head, (py, ldy, _raw_stream(x.device))
+
+
+def w4_linear(x, codes, scales, group=32, out=None):
+    """y = x W^T for few tokens: x [T, K] bfloat16 or float16, W [N, K] as 4-bit codes and scales
+    (block_pack with the format (2, 1)) -> y [T, N]."""
+    y, head, tail = _w4(x, (codes, scales), group, out, "w4_linear")
+    _check(lib().hobflops_w4_linear(*head, *tail))
+    return y
+
+
+def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, out=None):
+    """h = act(x Wg^T) * (x Wu^T) for few tokens, both weights as 4-bit codes and scales."""
+    y, head, tail = _w4(x, (g_codes, g_scales, u_codes, u_scales), group, out, "w4_gated")
+    _check(lib().hobflops_w4_gated(*head, act, *tail))
+    return y

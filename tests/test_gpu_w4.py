@@ -1,0 +1,141 @@
+"""Products with 4-bit weights on the GPU against a plain 64-bit reference.
+
+Tolerance, derived: K products summed in float32 in some order, the scale applied to parts of the
+sum: (K + 4) 2^-23 sum |x w|, and the output's rounding; of the gated form the errors of both
+products through the activation (slope at most 1.13, its own error 2^-19 of its argument).
+"""
+import numpy as np
+import pytest
+import torch
+
+import narrow_ref as ref
+from gpu_util import need_gpu, say
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"bf16": 0.0, "f16": 2.0 ** -24}
+EPS, ACT = 2.0 ** -23, 2.0 ** -19
+SCALES = {"pow2": 0, "bf16": 1, "f32": 2}
+
+
+def _weights(hf, N, K, group, scale, seed):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn((N, K), generator=g) * K ** -0.5
+    codes, scales = hf.block_pack(w.cuda(), (2, 1), group=group, scale=SCALES[scale])
+    f = scales.cpu().double().numpy()
+    f = np.exp2(f - 127) if scale == "pow2" else f
+    return codes, scales, ref.unpack(ref.nibbles(codes.cpu().numpy(), K), f, (2, 1), group)
+
+
+def _x(T, K, dtype, seed, ld=None, offset=0):
+    g = torch.Generator().manual_seed(seed)
+    ld = ld or K
+    flat = torch.randn(T * ld + offset, generator=g).to(TYPES[dtype]).cuda()
+    return flat[offset:].view(T, ld)[:, :K]
+
+
+SHAPES = [(1, 1, 1), (1, 32, 16), (1, 33, 5), (2, 64, 7), (3, 130, 33), (1, 4096, 40), (1, 2056, 17),
+          (4, 256, 64), (5, 1000, 50), (8, 512, 129), (9, 520, 31), (16, 1024, 48), (17, 264, 100),
+          (33, 136, 65), (64, 2080, 20), (100, 72, 30), (1, 31, 3), (7, 8200, 9)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype,group,scale", [("bf16", 32, "pow2"), ("f16", 64, "bf16"),
+                                               ("bf16", 128, "f32"), ("f16", 32, "f32"),
+                                               ("bf16", 128, "bf16")])
+def test_linear_and_gated(shape, dtype, group, scale):
+    hf = need_gpu()
+    T, K, N = shape
+    say("w4", shape, dtype, group, scale)
+    cg, sg, wg = _weights(hf, N, K, group, scale, 1)
+    cu, su, wu = _weights(hf, N, K, group, scale, 2)
+    for ld, off in ((None, 0), (K + 3, 1)):
+        xt = _x(T, K, dtype, 3, ld, off)
+        x = xt.double().cpu().numpy()
+        g, u = x @ wg.T, x @ wu.T
+        eg, eu = ((K + 4) * EPS * (np.abs(x) @ np.abs(w).T) for w in (wg, wu))
+        out = torch.full((T, N + 2), 7.0, dtype=TYPES[dtype], device="cuda")
+        y = hf.w4_linear(xt, cg, sg, group=group, out=out[:, :N]).double().cpu().numpy()
+        assert (np.abs(y - g) <= eg + UNIT[dtype] * np.abs(g) + TINY[dtype]).all()
+        assert (out[:, N:] == 7.0).all()
+        for act in (0, 1, 2):
+            h = hf.w4_gated(xt, cg, sg, cu, su, act, group=group).double().cpu().numpy()
+            a = ref.act(g, act)[0]
+            e = (1.13 * eg + ACT * np.abs(g)) * (np.abs(u) + eu) + np.abs(a) * eu
+            want = a * u
+            assert (np.abs(h - want) <= e + UNIT[dtype] * np.abs(want) + TINY[dtype]).all()
+
+
+@pytest.mark.parametrize("T", [1, 3, 6, 20])
+@pytest.mark.parametrize("group,scale", [(32, "pow2"), (64, "f32")])
+def test_all_codes_exactly(T, group, scale):
+    """x with one 1 a token picks single weights: every code of every place, exactly."""
+    hf = need_gpu()
+    K, N = 160, 24
+    rng = np.random.default_rng(4)
+    packed = torch.from_numpy(rng.integers(0, 256, (N, K // 2), dtype=np.uint8)).cuda()
+    groups = -(-K // group)
+    if scale == "pow2":
+        scales = torch.from_numpy(rng.integers(117, 131, (N, groups), dtype=np.uint8)).cuda()
+        f = np.exp2(scales.cpu().double().numpy() - 127)
+    else:
+        scales = torch.exp2(torch.randint(-9, 4, (N, groups)).float()).cuda()
+        f = scales.cpu().double().numpy()
+    w = ref.unpack(ref.nibbles(packed.cpu().numpy(), K), f, (2, 1), group)
+    for k0 in range(0, K, T):
+        n = min(T, K - k0)
+        x = torch.zeros(T, K, dtype=torch.bfloat16)
+        x[torch.arange(n), k0 + torch.arange(n)] = 1.0
+        y = hf.w4_linear(x.cuda(), packed, scales, group=group).double().cpu().numpy()
+        assert np.array_equal(y[:n], w[:, k0:k0 + n].T) and not y[n:].any()
+
+
+@pytest.mark.parametrize("T", [1, 2, 5, 18])
+def test_what_is_not_finite(T):
+    """An infinity or NaN of a token reaches that token's outputs alone; a NaN scale its row's."""
+    hf = need_gpu()
+    K, N = 200, 37
+    codes, scales, w = _weights(hf, N, K, 32, "pow2", 5)
+    x = _x(T, K, "bf16", 6).clone()
+    base = hf.w4_linear(x, codes, scales).clone()
+    x[T - 1, 0] = float("inf")
+    scales = scales.clone()
+    scales[11, 2] = 255
+    y = hf.w4_linear(x, codes, scales)
+    rows = torch.arange(N) != 11
+    assert torch.equal(y[:T - 1].cpu()[:, rows], base[:T - 1].cpu()[:, rows])
+    assert y[:, 11].isnan().all()
+    last = y[T - 1].cpu()[rows].double().numpy()
+    w0 = w[rows.numpy(), 0]
+    assert np.isnan(last[w0 == 0]).all()
+    assert np.array_equal(last[w0 != 0], np.sign(w0[w0 != 0]) * np.inf)
+
+
+def test_no_tokens_and_streams():
+    hf = need_gpu()
+    codes, scales, w = _weights(hf, 40, 64, 32, "pow2", 7)
+    assert hf.w4_linear(torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), codes,
+                        scales).shape == (0, 40)
+    x = _x(3, 64, "bf16", 8)
+    y = hf.w4_linear(x, codes, scales)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        z = [hf.w4_linear(x, codes, scales) for _ in range(3)]
+    s.synchronize()
+    assert all(torch.equal(y, t) for t in z)
+
+
+def test_arguments():
+    hf = need_gpu()
+    codes, scales, _ = _weights(hf, 40, 64, 32, "pow2", 7)
+    x = _x(3, 64, "bf16", 8)
+    with pytest.raises(ValueError):
+        hf.w4_linear(x, codes, scales, group=48)
+    with pytest.raises(ValueError):
+        hf.w4_linear(x, codes, scales[:, :1].contiguous())
+    with pytest.raises(ValueError):
+        hf.w4_linear(x[:, ::2], codes, scales)
+    with pytest.raises(hf.HobflopsError):
+        hf.w4_linear(x.float(), codes, scales)
