@@ -345,12 +345,15 @@ int hobflops_block_unpack(const uint8_t* codes, const void* scales, int64_t rows
  * float32, one rounding at the end. act: HOBFLOPS_GATE_*, g sigmoid(g), g Phi(g)
  * (Phi the normal distribution) or max(g, 0).
  * ckpt: (4, 3) or (5, 2), the format of the checkpoints; {0, 0}: none, forward
- * only. */
+ * only. With align 16 and D, ldx and ldw multiples of 8 the
+ * kernels read x and the weights in place; else the call copies what it must into the
+ * workspace first. HOBFLOPS_EALIGN if a pointer is not aligned as align says. */
 typedef struct {
   int64_t T, D, F;
   int64_t ldx, ldw, ldh;
   int type, act;
   hobflops_fmt ckpt;
+  int align; /* bytes that the pointers of x and the weights are aligned to: 2, 4, 8 or 16 */
 } hobflops_gated_desc;
 
 /* Workspace bytes of a forward (backward 0) or backward (1) call. */

@@ -202,6 +202,7 @@ int gated_check(const hobflops_gated_desc* d, int backward, int* fmt) {
     return HOBFLOPS_EINVAL;
   if (!type_ok(d->type) || d->act < HOBFLOPS_GATE_SILU || d->act > HOBFLOPS_GATE_RELU)
     return HOBFLOPS_EINVAL;
+  if (d->align != 2 && d->align != 4 && d->align != 8 && d->align != 16) return HOBFLOPS_EINVAL;
   *fmt = -1;
   if (d->ckpt.wE != 0 || d->ckpt.wF != 0) {
     if (d->ckpt.wE < 1 || d->ckpt.wF < 1) return HOBFLOPS_EINVAL;
@@ -661,7 +662,8 @@ int hobflops_gated_forward(const hobflops_gated_desc* d, const void* x, const vo
   if (fmt >= 0 && (!g_codes || !g_scales || !u_codes || !u_scales)) return HOBFLOPS_EINVAL;
   const int64_t need = gated_forward_workspace(*d);
   if (need > 0 && (!workspace || workspace_bytes < need)) return HOBFLOPS_EINVAL;
-  if (!aligned_to(x, 2) || !aligned_to(w_gate, 2) || !aligned_to(w_up, 2) || !aligned_to(h, 2) ||
+  if (!aligned_to(x, d->align) || !aligned_to(w_gate, d->align) || !aligned_to(w_up, d->align) ||
+      !aligned_to(h, 2) ||
       (need > 0 && !aligned_to(workspace, 16)))
     return HOBFLOPS_EALIGN;
   const GatedForward p{x, w_gate, w_up, h, {g_codes, g_scales}, {u_codes, u_scales}, workspace};
@@ -682,8 +684,8 @@ int hobflops_gated_backward(const hobflops_gated_desc* d, const void* dh, const 
   if (d->T > 0 && (!dh || !x_codes || !x_scales || !g_codes || !g_scales || !u_codes ||
                    !u_scales || !w_gate || !w_up || !dx || !workspace || workspace_bytes < need))
     return HOBFLOPS_EINVAL;
-  if (!aligned_to(dh, 2) || !aligned_to(w_gate, 2) || !aligned_to(w_up, 2) || !aligned_to(dx, 2) ||
-      !aligned_to(dw_gate, 2) || !aligned_to(dw_up, 2) || (d->T > 0 && !aligned_to(workspace, 16)))
+  if (!aligned_to(dh, 2) || !aligned_to(w_gate, d->align) || !aligned_to(w_up, d->align) ||
+      !aligned_to(dx, 2) || !aligned_to(dw_gate, 2) || !aligned_to(dw_up, 2) || (d->T > 0 && !aligned_to(workspace, 16)))
     return HOBFLOPS_EALIGN;
   GatedBackward p{};
   p.dh = dh;

@@ -7,116 +7,368 @@
 #include <stdint.h>
 
 #include "block.hpp"
+#include "gemm.hpp"
 #include "narrow.hpp"
 
 namespace hobflops {
 namespace {
 
-// ---- a product of any strides ----------------------------------------------
+// ---- the products ------------------------------------------------------------
 
-// C[m][n] = sum_k A(m, k) B(n, k), operands by their strides; a 64x64 tile of
-// four waves (32x32 each), 32 of K at a time through LDS.
-struct Operand {
-  const void* p;
-  int64_t row, k;  // strides in elements
-};
-constexpr int kTile = 64, kTileK = 32, kPad = 8;
-
-template <class T, class Out>
-__global__ __launch_bounds__(256) void product_kernel(Operand a, Operand b, Out* c, int64_t ldc,
-                                                      int64_t M, int64_t N, int64_t K, int add) {
+// Rows of an operand as the products need them: 16-byte aligned, zeros from cols up to ldd.
+template <class T>
+__global__ __launch_bounds__(256) void align_kernel(const void* src, int64_t ld, int64_t rows,
+                                                    int64_t cols, void* dst, int64_t ldd) {
   typedef typename T::elem E;
-  __shared__ E sa[kTile][kTileK + kPad], sb[kTile][kTileK + kPad];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
-  f32x4 acc[2][2] = {};
-  for (int64_t k0 = 0; k0 < K; k0 += kTileK) {
-    for (int i = tid; i < kTile * kTileK; i += 256) {
-      const int r = i / kTileK, k = i % kTileK;
-      const bool ka = k0 + k < K;
-      sa[r][k] = ka && m0 + r < M ? ((const E*)a.p)[(m0 + r) * a.row + (k0 + k) * a.k] : (E)0.0f;
-      sb[r][k] = ka && n0 + r < N ? ((const E*)b.p)[(n0 + r) * b.row + (k0 + k) * b.k] : (E)0.0f;
-    }
-    __syncthreads();
-    typename T::vec8 fa[2], fb[2];
+  const int64_t per = ldd / 8, n = rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per, col = (i - row * per) * 8;
+    const E* s = (const E*)src + row * ld;
+    typename T::vec8 v;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      fa[i] = *(const typename T::vec8*)&sa[wm + 16 * i + (lane & 15)][8 * (lane >> 4)];
-      fb[i] = *(const typename T::vec8*)&sb[wn + 16 * i + (lane & 15)][8 * (lane >> 4)];
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
-    __syncthreads();
+    for (int j = 0; j < 8; ++j) v[j] = col + j < cols ? s[col + j] : (E)0.0f;
+    *(typename T::vec8*)((E*)dst + row * ldd + col) = v;
   }
+}
+
+// Four values of a row, those before `end` of it.
+template <class T>
+__device__ __forceinline__ void store4(typename T::elem* p, int64_t col, int64_t end, bool vec,
+                                       const float (&v)[4]) {
+  typedef typename T::elem E;
+  if (vec && col + 4 <= end) {
+    E e[4] = {(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
+    __builtin_memcpy(__builtin_assume_aligned(p + col, 8), e, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < end) p[col + i] = (E)v[i];
+  }
+}
+
+struct ForwardArgs {
+  const void *w[2], *x;
+  int64_t ldw, ldx, T_, F, K, ldh;
+  void* h;
+  GatedBlocks gate, up;
+  int act, vec;
+  uint32_t ni, nj;
+};
+
+// The scale and codes of 32 values of a token: 8 in each of the lanes l, l ^ 16, l ^ 32, l ^ 48,
+// v[i] the values 16 i + 4 (lane / 16) + 0..3 of the group.
+template <int kFmt>
+__device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int64_t F, int64_t f0,
+                                            int lane, bool row_ok, bool vec, const f32x4 (&v)[2]) {
+  const int q = lane >> 4;
+  uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = m0 + wm + 16 * i + 4 * (lane >> 4) + r;
-        const int64_t n = n0 + wn + 16 * j + (lane & 15);
-        if (m < M && n < N) {
-          const float v = acc[i][j][r] + (add ? (float)c[m * ldc + n] : 0.0f);
-          c[m * ldc + n] = (Out)v;
-        }
-      }
-}
-
-template <class T, class Out>
-void product(Operand a, Operand b, Out* c, int64_t ldc, int64_t M, int64_t N, int64_t K, int add,
-             hipStream_t stream) {
-  const dim3 grid((unsigned)((M + kTile - 1) / kTile), (unsigned)((N + kTile - 1) / kTile));
-  product_kernel<T, Out><<<grid, 256, 0, stream>>>(a, b, c, ldc, M, N, K, add);
-}
-
-// h, and the blocks of both projections: one thread a value, 32 lanes a group.
-template <class T, int kFmt>
-__global__ __launch_bounds__(256) void gate_kernel(const float* g, const float* u, void* h,
-                                                   int64_t T_, int64_t F, int64_t ldh, int act,
-                                                   GatedBlocks gb, GatedBlocks ub) {
-  const int64_t groups = (F + 31) / 32;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / (groups * 32), col = i - row * groups * 32;
-  if (row >= T_) return;
-  const float vg = col < F ? g[row * F + col] : 0.0f, vu = col < F ? u[row * F + col] : 0.0f;
-  if (col < F) ((typename T::elem*)h)[row * ldh + col] = (typename T::elem)(gate_act(vg, act) * vu);
-  if (kFmt < 0) return;
-  constexpr int kF = kFmt < 0 ? 0 : kFmt;
-  for (int w = 0; w < 2; ++w) {
-    const float v = w ? vu : vg;
-    const GatedBlocks& b = w ? ub : gb;
-    uint32_t a = finite_abs(v);
-    for (int m = 1; m < 32; m <<= 1) {
-      const uint32_t o = (uint32_t)__shfl_xor((int)a, m);
-      a = a > o ? a : o;
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t m = f0 + 16 * i + 4 * q + r < F ? finite_abs(v[i][r]) : 0u;
+      a = a > m ? a : m;
     }
-    const int k = block_scale<kF>(a);
-    if ((col & 31) == 0) b.scales[row * groups + col / 32] = (uint8_t)(k + 127);
-    if (col < F) b.codes[row * F + col] = (uint8_t)encode4<kF>(v * pow2f(-k), 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int m = 16; m < 64; m <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)a, m);
+    a = a > o ? a : o;
+  }
+  const int k = block_scale<kFmt>(a);
+  const float s = pow2f(-k);
+  if (!row_ok || f0 >= F) return;
+  if (q == 0) b.scales[t * ((F + 31) / 32) + f0 / 32] = (uint8_t)(k + 127);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w = encode4<kFmt>(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
+    const int64_t f = f0 + 16 * i + 4 * q;
+    uint8_t* p = b.codes + t * F + f;
+    if (vec && f + 4 <= F) {
+      __builtin_memcpy(__builtin_assume_aligned(p, 4), &w, 4);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (f + r < F) p[r] = (uint8_t)(w >> (8 * r));
+    }
   }
 }
 
-// dg, du [T][F] and x [T][D] from the blocks.
+// h = act(x Wg^T) * (x Wu^T): the tile's rows are BI / 2 of w_gate and the same of w_up, a wave
+// has both sums of its outputs.
+template <class T, int kFmt, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(64 * WI * WJ) void forward_kernel(ForwardArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr int NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
+  __shared__ __align__(1024) uint8_t s0[(BI + BJ) * 128], s1[(BI + BJ) * 128];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t ti, tj;
+  tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
+  const int64_t i0 = (int64_t)ti * (BI / 2), j0 = (int64_t)tj * BJ;
+  LoadRows<BI, NW, 2> la;
+  LoadRows<BJ, NW, 1> lb;
+  const void* const xs[1] = {p.x};
+  la.start(p.w, p.ldw, p.F, i0, p.K, 0, wave, lane);
+  lb.start(xs, p.ldx, p.T_, j0, p.K, 0, wave, lane);
+  const int wi = wave % WI, wj = wave / WI;
+  ReadRows<T, NI> ra;
+  ReadRows<T, NJ> rb;
+  ra.start(wi * NI * 16, lane);
+  rb.start(BI + wj * NJ * 16, lane);
+  f32x4 g[NI][NJ] = {}, u[NI][NJ] = {};
+  const auto compute = [&](const uint8_t* s) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      typename T::vec8 fb[NJ], fg[NI], fu[NI];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fb[j] = rb.get(s, j, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fg[i] = ra.get(s, i, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fu[i] = ra.get(s, i + BI / 32, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) g[i][j] = T::mfma(fg[i], fb[j], g[i][j]);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) u[i][j] = T::mfma(fu[i], fb[j], u[i][j]);
+    }
+  };
+  const int64_t steps = (p.K + kStepK - 1) / kStepK;
+  la.load(s0, wave);
+  lb.load(s0 + BI * 128, wave);
+  for (int64_t k = 0; k < steps; k += 2) {
+    stage_ready();
+    if (k + 1 < steps) {
+      la.load(s1, wave);
+      lb.load(s1 + BI * 128, wave);
+    }
+    compute(s0);
+    if (k + 1 < steps) {
+      stage_ready();
+      if (k + 2 < steps) {
+        la.load(s0, wave);
+        lb.load(s0 + BI * 128, wave);
+      }
+      compute(s1);
+    }
+  }
+  const int q = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t t = j0 + wj * NJ * 16 + 16 * j + (lane & 15);
+    const bool row_ok = t < p.T_;
+    typename T::elem* row = (typename T::elem*)p.h + (row_ok ? t : 0) * p.ldh;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int64_t f = i0 + wi * NI * 16 + 16 * i + 4 * q;
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = gate_act(g[i][j][r], p.act) * u[i][j][r];
+      if (row_ok) store4<T>(row, f, p.F, p.vec & 1, v);
+    }
+    if constexpr (kFmt >= 0) {
+#pragma unroll
+      for (int i = 0; i < NI; i += 2) {
+        const int64_t f0 = i0 + wi * NI * 16 + 16 * i;
+        const f32x4 vg[2] = {g[i][j], g[i + 1][j]}, vu[2] = {u[i][j], u[i + 1][j]};
+        store_block<kFmt>(p.gate, t, p.F, f0, lane, row_ok, p.vec & 2, vg);
+        store_block<kFmt>(p.up, t, p.F, f0, lane, row_ok, p.vec & 2, vu);
+      }
+    }
+  }
+#endif
+}
+
+// The gradients' products, D[i][j] with i along a row of the output:
+//  kWeights 0: dx[t][d], i = d, j = t: A the weights (K-major, w_gate then w_up), B the rows
+//    [t][2 Fp] of dg and du, k = 2 Fp.
+//  kWeights 1: dw[f][d], i = d, j = f of 2 Fp: A the rows of x, B those of dg and du, both K-major, k = T.
+// Fp is F rounded up to 64; dg and du are zero between F and Fp.
+struct GradArgs {
+  const void *a[2], *b;
+  int64_t lda, ldb, cols, ni_, nj_, K, F, Fp;  // cols: D rounded up to 8, ni_ = D, nj_: T or 2 Fp
+  void* out[2];
+  float* part;  // with splits: [splits][nj_][ni_ rounded up to 4]
+  int64_t per;  // k of a split, a multiple of 64
+  int vec;
+  uint32_t ni, nj;
+};
+template <class T, bool kWeights, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(64 * WI * WJ) void grad_kernel(GradArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr int NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
+  __shared__ __align__(1024) uint8_t s0[(BI + BJ) * 128], s1[(BI + BJ) * 128];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t ti, tj;
+  tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
+  const int64_t i0 = (int64_t)ti * BI, j0 = (int64_t)tj * BJ;
+  const int64_t k0 = (int64_t)blockIdx.y * p.per;
+  const int64_t k1 = k0 + p.per < p.K ? k0 + p.per : p.K;
+  const int64_t steps = (k1 - k0 + kStepK - 1) / kStepK;
+  LoadColumns<BI, NW> la;
+  if (kWeights)
+    la.start(p.a[0], p.lda, p.cols, i0, p.K, k0, wave, lane);
+  else if (k0 < p.Fp)
+    la.start(p.a[0], p.lda, p.cols, i0, p.F, k0, wave, lane);
+  else
+    la.start(p.a[1], p.lda, p.cols, i0, p.F, k0 - p.Fp, wave, lane);
+  LoadColumns<BJ, NW> lbc;
+  LoadRows<BJ, NW, 1> lbr;
+  const void* const bs[1] = {p.b};
+  if (kWeights)
+    lbc.start(p.b, p.ldb, p.nj_, j0, p.K, k0, wave, lane);
+  else
+    lbr.start(bs, p.ldb, p.nj_, j0, p.K, k0, wave, lane);
+  int64_t k = k0;
+  const auto load = [&](uint8_t* s) {
+    if (!kWeights && k == p.Fp && k0 < p.Fp)
+      la.start(p.a[1], p.lda, p.cols, i0, p.F, 0, wave, lane);
+    la.load(s, wave);
+    if (kWeights)
+      lbc.load(s + BI * 128, wave);
+    else
+      lbr.load(s + BI * 128, wave);
+    k += kStepK;
+  };
+  const int wi = wave % WI, wj = wave / WI;
+  ReadColumns<T, NI, BI> ra;
+  ReadColumns<T, NJ, BJ> rbc;
+  ReadRows<T, NJ> rbr;
+  ra.start(wi * NI * 16, lane);
+  if (kWeights)
+    rbc.start(wj * NJ * 16, lane);
+  else
+    rbr.start(wj * NJ * 16, lane);
+  f32x4 acc[NI][NJ] = {};
+  const auto compute = [&](const uint8_t* s) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      typename T::vec8 fb[NJ], fa[NI];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        fb[j] = kWeights ? rbc.get(s + BI * 128, j, ks) : rbr.get(s + BI * 128, j, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fa[i] = ra.get(s, i, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
+    }
+  };
+  if (steps > 0) load(s0);
+  for (int64_t n = 0; n < steps; n += 2) {
+    stage_ready();
+    if (n + 1 < steps) load(s1);
+    compute(s0);
+    if (n + 1 < steps) {
+      stage_ready();
+      if (n + 2 < steps) load(s0);
+      compute(s1);
+    }
+  }
+  const int q = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t c = j0 + wj * NJ * 16 + 16 * j + (lane & 15);
+    if (c >= p.nj_) continue;
+    const int64_t half = kWeights && c >= p.Fp ? 1 : 0, row = c - half * p.Fp;
+    if (kWeights && row >= p.F) continue;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int64_t d = i0 + wi * NI * 16 + 16 * i + 4 * q;
+      if (d >= p.ni_) continue;
+      if (p.part) {
+        const int64_t ldp = (p.ni_ + 3) & ~(int64_t)3;
+        *(f32x4*)(p.part + ((int64_t)blockIdx.y * p.nj_ + c) * ldp + d) = acc[i][j];
+      } else {
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        store4<T>((typename T::elem*)p.out[half] + row * p.ni_, d, p.ni_, p.vec, v);
+      }
+    }
+  }
+#endif
+}
+
+// Sums the splits of a product in their order.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(const float* part, int splits, int64_t rows,
+                                                   int64_t cols, typename T::elem* out, bool vec) {
+  const int64_t ldp = (cols + 3) & ~(int64_t)3, n = rows * ldp;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n;
+       i += (int64_t)gridDim.x * 1024) {
+    f32x4 v = *(const f32x4*)(part + i);
+    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + s * n + i);
+    const int64_t row = i / ldp, col = i - row * ldp;
+    const float e[4] = {v[0], v[1], v[2], v[3]};
+    store4<T>(out + row * cols, col, cols, vec, e);
+  }
+}
+
+// dg and du, rows [t][2 Fp] (du from Fp on, zeros from F to Fp), from dh and the blocks of g and u:
+// 8 values a thread.
+struct GateGradArgs {
+  const void* dh;
+  GatedBlocks gate, up;
+  void* out;
+  int64_t T_, F, Fp, ldh;
+  int act, vec;  // vec 1: dh in 16-byte accesses, 2: codes in 8-byte ones
+};
 template <class T, int kFmt>
-__global__ __launch_bounds__(256) void gate_grad_kernel(const void* dh, int64_t ldh, int64_t T_,
-                                                        int64_t F, int act, GatedBlocks gb,
-                                                        GatedBlocks ub, void* dg, void* du) {
+__global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs p) {
   typedef typename T::elem E;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / F, col = i - row * F, groups = (F + 31) / 32;
-  if (row >= T_) return;
-  const int64_t s = row * groups + col / 32;
-  const float g = decode4<kFmt>(gb.codes[i])[0] * load_scale(gb.scales, s, HOBFLOPS_SCALE_POW2);
-  const float u = decode4<kFmt>(ub.codes[i])[0] * load_scale(ub.scales, s, HOBFLOPS_SCALE_POW2);
-  const float d = (float)((const E*)dh)[row * ldh + col];
-  float a, da;
-  gate_act_grad(g, act, a, da);
-  ((E*)dg)[i] = (E)(d * u * da);
-  ((E*)du)[i] = (E)(d * a);
+  const int64_t per = p.Fp / 8, n = p.T_ * per, groups = (p.F + 31) / 32;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per, col = (i - row * per) * 8;
+    typename T::vec8 dg, du;
+    if (col < p.F) {
+      const E* dh = (const E*)p.dh + row * p.ldh + col;
+      const uint8_t *gc = p.gate.codes + row * p.F + col, *uc = p.up.codes + row * p.F + col;
+      uint32_t wg[2] = {0, 0}, wu[2] = {0, 0};
+      typename T::vec8 d;
+      const bool whole = col + 8 <= p.F;
+      if ((p.vec & 1) && whole) {
+        d = *(const typename T::vec8*)dh;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = col + j < p.F ? dh[j] : (E)0.0f;
+      }
+      if ((p.vec & 2) && whole) {
+        __builtin_memcpy(wg, __builtin_assume_aligned(gc, 8), 8);
+        __builtin_memcpy(wu, __builtin_assume_aligned(uc, 8), 8);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j < p.F) {
+            wg[j >> 2] |= (uint32_t)gc[j] << (8 * (j & 3));
+            wu[j >> 2] |= (uint32_t)uc[j] << (8 * (j & 3));
+          }
+      }
+      const int64_t s = row * groups + col / 32;
+      const float sg = load_scale(p.gate.scales, s, HOBFLOPS_SCALE_POW2);
+      const float su = load_scale(p.up.scales, s, HOBFLOPS_SCALE_POW2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 g = decode4<kFmt>(wg[h]), u = decode4<kFmt>(wu[h]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float a, da;
+          gate_act_grad(g[j] * sg, p.act, a, da);
+          const bool in = col + 4 * h + j < p.F;
+          const float v = (float)d[4 * h + j];
+          dg[4 * h + j] = in ? (E)(v * (u[j] * su) * da) : (E)0.0f;
+          du[4 * h + j] = in ? (E)(v * a) : (E)0.0f;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dg[j] = du[j] = (E)0.0f;
+    }
+    E* out = (E*)p.out + row * 2 * p.Fp + col;
+    *(typename T::vec8*)out = dg;
+    *(typename T::vec8*)(out + p.Fp) = du;
+  }
 }
 
 __global__ void zero_kernel(uint16_t* p, int64_t n) {
@@ -125,67 +377,206 @@ __global__ void zero_kernel(uint16_t* p, int64_t n) {
     p[i] = 0;
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void round_kernel(const float* src, typename T::elem* dst,
-                                                    int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) dst[i] = (typename T::elem)src[i];
+int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+unsigned grid_of(int64_t threads, int64_t most) {
+  const int64_t n = (threads + 255) / 256;
+  return (unsigned)(n < most ? n : most);
+}
+
+// What a call keeps in its workspace, by byte offsets; -1: not needed.
+struct ForwardPlan {
+  int64_t x = -1, wg = -1, wu = -1, bytes = 0;
+};
+int64_t take(int64_t* total, int64_t bytes) {
+  const int64_t at = *total;
+  *total += round_up(bytes, 256);
+  return at;
+}
+ForwardPlan plan_forward(const hobflops_gated_desc& d) {
+  ForwardPlan p;
+  const int64_t Dp = round_up(d.D, 8);
+  const bool rows = d.align >= 16 && d.D % 8 == 0;
+  if (!rows || d.ldx % 8 != 0 || d.ldx >= (int64_t)1 << 21) p.x = take(&p.bytes, d.T * Dp * 2);
+  if (!rows || d.ldw % 8 != 0 || d.ldw >= (int64_t)1 << 21) {
+    p.wg = take(&p.bytes, d.F * Dp * 2);
+    p.wu = take(&p.bytes, d.F * Dp * 2);
+  }
+  return p;
+}
+
+constexpr int kMaxSplits = 32;
+struct BackwardPlan {
+  int64_t x = -1, wg = -1, wu = -1, dgu = -1, part = -1, bytes = 0;
+  int64_t Dp, Fp;
+  int splits, small;  // of dx; 128 x 128 tiles
+};
+BackwardPlan plan_backward(const hobflops_gated_desc& d) {
+  BackwardPlan p;
+  p.Dp = round_up(d.D, 8);
+  p.Fp = round_up(d.F, kStepK);
+  if (d.T == 0) return p;
+  p.x = take(&p.bytes, d.T * p.Dp * 2);
+  p.dgu = take(&p.bytes, d.T * 2 * p.Fp * 2);
+  if (d.align < 16 || d.D % 8 != 0 || d.ldw % 8 != 0 || d.ldw >= (int64_t)1 << 21) {
+    p.wg = take(&p.bytes, d.F * p.Dp * 2);
+    p.wu = take(&p.bytes, d.F * p.Dp * 2);
+  }
+  const int64_t tiles = ((d.D + 255) / 256) * ((d.T + 255) / 256);
+  p.small = tiles < 128;
+  const int64_t n = p.small ? ((d.D + 127) / 128) * ((d.T + 127) / 128) : tiles;
+  const int64_t steps = 2 * p.Fp / kStepK;
+  int64_t s = n < 256 ? 256 / n : 1;
+  s = s < kMaxSplits ? s : kMaxSplits;
+  p.splits = (int)(s < steps / 4 ? s : steps / 4 > 1 ? steps / 4 : 1);
+  if (p.splits > 1) p.part = take(&p.bytes, p.splits * d.T * round_up(d.D, 4) * 4);
+  return p;
 }
 
 template <class T>
-hipError_t forward(const hobflops_gated_desc& d, const GatedForward& p, int fmt, hipStream_t s) {
-  if (d.T == 0) return hipSuccess;
-  float* g = (float*)p.workspace;
-  float* u = g + d.T * d.F;
-  const Operand x{p.x, d.ldx, 1};
-  product<T>(x, Operand{p.w_gate, d.ldw, 1}, g, d.F, d.T, d.F, d.D, 0, s);
-  product<T>(x, Operand{p.w_up, d.ldw, 1}, u, d.F, d.T, d.F, d.D, 0, s);
-  const int64_t n = d.T * ((d.F + 31) / 32) * 32;
-  const unsigned grid = (unsigned)((n + 255) / 256);
+void align_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd,
+                hipStream_t s) {
+  align_kernel<T><<<grid_of(rows * ldd / 8, 65536), 256, 0, s>>>(src, ld, rows, cols, dst, ldd);
+}
+
+template <class T, int kFmt>
+void forward_tiles(ForwardArgs& p, hipStream_t s) {
+  const int64_t big = ((p.F + 127) / 128) * ((p.T_ + 255) / 256);
+  if (big >= 192) {
+    p.ni = (uint32_t)((p.F + 127) / 128);
+    p.nj = (uint32_t)((p.T_ + 255) / 256);
+    forward_kernel<T, kFmt, 256, 256, 2, 4><<<p.ni * p.nj, 512, 0, s>>>(p);
+  } else {
+    p.ni = (uint32_t)((p.F + 63) / 64);
+    p.nj = (uint32_t)((p.T_ + 63) / 64);
+    forward_kernel<T, kFmt, 128, 64, 2, 2><<<p.ni * p.nj, 256, 0, s>>>(p);
+  }
+}
+
+template <class T>
+hipError_t forward(const hobflops_gated_desc& d, const GatedForward& c, int fmt, hipStream_t s) {
+  const ForwardPlan plan = plan_forward(d);
+  uint8_t* ws = (uint8_t*)c.workspace;
+  const int64_t Dp = round_up(d.D, 8);
+  ForwardArgs p{};
+  p.x = c.x;
+  p.w[0] = c.w_gate;
+  p.w[1] = c.w_up;
+  p.ldx = d.ldx;
+  p.ldw = d.ldw;
+  p.K = d.D;
+  if (plan.x >= 0) {
+    align_rows<T>(c.x, d.ldx, d.T, d.D, ws + plan.x, Dp, s);
+    p.x = ws + plan.x;
+    p.ldx = Dp;
+    p.K = Dp;
+  }
+  if (plan.wg >= 0) {
+    align_rows<T>(c.w_gate, d.ldw, d.F, d.D, ws + plan.wg, Dp, s);
+    align_rows<T>(c.w_up, d.ldw, d.F, d.D, ws + plan.wu, Dp, s);
+    p.w[0] = ws + plan.wg;
+    p.w[1] = ws + plan.wu;
+    p.ldw = Dp;
+  }
+  p.T_ = d.T;
+  p.F = d.F;
+  p.ldh = d.ldh;
+  p.h = c.h;
+  p.gate = c.gate;
+  p.up = c.up;
+  p.act = d.act;
+  p.vec = (((uintptr_t)c.h & 7u) == 0 && d.ldh % 4 == 0 ? 1 : 0) |
+          (((uintptr_t)c.gate.codes & 3u) == 0 && ((uintptr_t)c.up.codes & 3u) == 0 && d.F % 4 == 0 ? 2 : 0);
   if (fmt == kE4M3)
-    gate_kernel<T, kE4M3><<<grid, 256, 0, s>>>(g, u, p.h, d.T, d.F, d.ldh, d.act, p.gate, p.up);
+    forward_tiles<T, kE4M3>(p, s);
   else if (fmt == kE5M2)
-    gate_kernel<T, kE5M2><<<grid, 256, 0, s>>>(g, u, p.h, d.T, d.F, d.ldh, d.act, p.gate, p.up);
+    forward_tiles<T, kE5M2>(p, s);
   else
-    gate_kernel<T, -1><<<grid, 256, 0, s>>>(g, u, p.h, d.T, d.F, d.ldh, d.act, p.gate, p.up);
+    forward_tiles<T, -1>(p, s);
   return hipGetLastError();
 }
 
+template <class T, bool kWeights>
+void grad_tiles(GradArgs& p, bool small, int splits, hipStream_t s) {
+  const int64_t b = small ? 128 : 256;
+  p.ni = (uint32_t)((p.ni_ + b - 1) / b);
+  p.nj = (uint32_t)((p.nj_ + b - 1) / b);
+  const dim3 grid(p.ni * p.nj, (unsigned)splits);
+  if (small)
+    grad_kernel<T, kWeights, 128, 128, 2, 2><<<grid, 256, 0, s>>>(p);
+  else
+    grad_kernel<T, kWeights, 256, 256, 2, 4><<<grid, 512, 0, s>>>(p);
+}
+
 template <class T>
-hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& p, int fmt, hipStream_t s) {
+hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fmt, hipStream_t s) {
   typedef typename T::elem E;
   if (d.T == 0) {
-    zero_kernel<<<1024, 256, 0, s>>>((uint16_t*)p.dw_gate, d.F * d.D);
-    zero_kernel<<<1024, 256, 0, s>>>((uint16_t*)p.dw_up, d.F * d.D);
+    zero_kernel<<<1024, 256, 0, s>>>((uint16_t*)c.dw_gate, d.F * d.D);
+    zero_kernel<<<1024, 256, 0, s>>>((uint16_t*)c.dw_up, d.F * d.D);
     return hipGetLastError();
   }
-  float* sum = (float*)p.workspace;  // dx before its rounding
-  E* dg = (E*)(sum + d.T * d.D);
-  E* du = dg + d.T * d.F;
-  E* x = du + d.T * d.F;
-  BlockTensor t{x, d.type, d.T, d.D, d.D, p.x.codes, p.x.scales, 32, HOBFLOPS_SCALE_POW2};
-  hipError_t e = launch_block_unpack(t, fmt, s);
+  const BackwardPlan plan = plan_backward(d);
+  uint8_t* ws = (uint8_t*)c.workspace;
+  const BlockTensor t{ws + plan.x, d.type, d.T, d.D, plan.Dp, c.x.codes, c.x.scales, 32,
+                      HOBFLOPS_SCALE_POW2};
+  const hipError_t e = launch_block_unpack(t, fmt, s);
   if (e != hipSuccess) return e;
-  const unsigned grid = (unsigned)((d.T * d.F + 255) / 256);
+  GateGradArgs gg{c.dh, c.gate, c.up, ws + plan.dgu, d.T, d.F, plan.Fp, d.ldh, d.act, 0};
+  gg.vec = (aligned16(c.dh) && d.ldh % 8 == 0 ? 1 : 0) |
+           (((uintptr_t)c.gate.codes & 7u) == 0 && ((uintptr_t)c.up.codes & 7u) == 0 && d.F % 8 == 0 ? 2 : 0);
+  const unsigned grid = grid_of(d.T * plan.Fp / 8, 1 << 20);
   if (fmt == kE4M3)
-    gate_grad_kernel<T, kE4M3><<<grid, 256, 0, s>>>(p.dh, d.ldh, d.T, d.F, d.act, p.gate, p.up, dg, du);
+    gate_grad_kernel<T, kE4M3><<<grid, 256, 0, s>>>(gg);
   else
-    gate_grad_kernel<T, kE5M2><<<grid, 256, 0, s>>>(p.dh, d.ldh, d.T, d.F, d.act, p.gate, p.up, dg, du);
-  product<T>(Operand{dg, 1, d.F}, Operand{x, 1, d.D}, (E*)p.dw_gate, d.D, d.F, d.D, d.T, 0, s);
-  product<T>(Operand{du, 1, d.F}, Operand{x, 1, d.D}, (E*)p.dw_up, d.D, d.F, d.D, d.T, 0, s);
-  product<T>(Operand{dg, d.F, 1}, Operand{p.w_gate, 1, d.ldw}, sum, d.D, d.T, d.D, d.F, 0, s);
-  product<T>(Operand{du, d.F, 1}, Operand{p.w_up, 1, d.ldw}, sum, d.D, d.T, d.D, d.F, 1, s);
-  const int64_t n = d.T * d.D;
-  round_kernel<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum, (E*)p.dx, n);
+    gate_grad_kernel<T, kE5M2><<<grid, 256, 0, s>>>(gg);
+  GradArgs p{};
+  p.F = d.F;
+  p.Fp = plan.Fp;
+  p.b = ws + plan.dgu;
+  p.ldb = 2 * plan.Fp;
+  p.ni_ = d.D;
+  p.cols = plan.Dp;
+  p.vec = d.D % 4 == 0;  // the outputs are dense
+  GradArgs w = p;
+  w.a[0] = ws + plan.x;
+  w.lda = plan.Dp;
+  w.nj_ = 2 * plan.Fp;
+  w.K = d.T;
+  w.per = round_up(d.T, kStepK);
+  w.out[0] = c.dw_gate;
+  w.out[1] = c.dw_up;
+  w.vec = p.vec && ((uintptr_t)c.dw_gate & 7u) == 0 && ((uintptr_t)c.dw_up & 7u) == 0;
+  const int64_t wt = ((d.D + 255) / 256) * ((2 * plan.Fp + 255) / 256);
+  grad_tiles<T, true>(w, wt < 192, 1, s);
+  p.a[0] = c.w_gate;
+  p.a[1] = c.w_up;
+  p.lda = d.ldw;
+  if (plan.wg >= 0) {
+    align_rows<T>(c.w_gate, d.ldw, d.F, d.D, ws + plan.wg, plan.Dp, s);
+    align_rows<T>(c.w_up, d.ldw, d.F, d.D, ws + plan.wu, plan.Dp, s);
+    p.a[0] = ws + plan.wg;
+    p.a[1] = ws + plan.wu;
+    p.lda = plan.Dp;
+  }
+  p.nj_ = d.T;
+  p.K = 2 * plan.Fp;
+  p.out[0] = c.dx;
+  p.vec = p.vec && ((uintptr_t)c.dx & 7u) == 0;
+  p.per = round_up((p.K + plan.splits - 1) / plan.splits, kStepK);
+  const int splits = (int)((p.K + p.per - 1) / p.per);
+  if (plan.part >= 0) p.part = (float*)(ws + plan.part);
+  grad_tiles<T, false>(p, plan.small, splits, s);
+  if (p.part)
+    join_kernel<T><<<grid_of(d.T * round_up(d.D, 4) / 4, 4096), 256, 0, s>>>(p.part, splits, d.T,
+                                                                             d.D, (E*)c.dx, p.vec);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t gated_forward_workspace(const hobflops_gated_desc& d) { return 8 * d.T * d.F; }
-int64_t gated_backward_workspace(const hobflops_gated_desc& d) {
-  return 4 * d.T * d.D + 4 * d.T * d.F + 2 * d.T * d.D;
-}
+int64_t gated_forward_workspace(const hobflops_gated_desc& d) { return plan_forward(d).bytes; }
+int64_t gated_backward_workspace(const hobflops_gated_desc& d) { return plan_backward(d).bytes; }
 
 hipError_t launch_gated_forward(const hobflops_gated_desc& d, const GatedForward& p, int fmt,
                                 hipStream_t stream) {

@@ -58,7 +58,8 @@ class PackJob(ctypes.Structure):
 class GatedDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int64), ("F", ctypes.c_int64),
                 ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldh", ctypes.c_int64),
-                ("type", ctypes.c_int), ("act", ctypes.c_int), ("ckpt", Fmt)]
+                ("type", ctypes.c_int), ("act", ctypes.c_int), ("ckpt", Fmt),
+                ("align", ctypes.c_int)]
 
 
 # What gated_forward keeps for gated_backward: (codes, scales) of x, g and u.
@@ -490,6 +491,14 @@ def _gated_weights(x, w_gate, w_up):
     return pg, pu, F, D, ldw
 
 
+def _align(*ptrs):
+    """The alignment in bytes that all the pointers have: 2, 4, 8 or 16."""
+    bits = 16
+    for p in ptrs:
+        bits |= p
+    return bits & -bits
+
+
 def _workspace(d, backward, device):
     n = ctypes.c_int64()
     _check(lib().hobflops_gated_workspace(ctypes.byref(d), backward, ctypes.byref(n)))
@@ -510,7 +519,8 @@ def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
     h = _out_rows(out, (T, F), x.dtype, x.device, "gated_forward out")
     ph, _, _, ldh = _rows(h, "gated_forward out")
     f = Fmt(0, 0) if ckpt is None else fmt(ckpt)
-    d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f)
+    d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f,
+                  _align(px, pg, pu))
     ws, pw, nw = _workspace(d, 0, x.device)
     stream = _raw_stream(x.device)
     if ckpt is None:
@@ -539,7 +549,7 @@ def gated_backward(dh, saved, w_gate, w_up, act=GATE_SILU):
         cshape, sshape = block_shapes(T, cols, f)
         ptrs += [_dense(codes, cshape, torch.uint8, dev, f"gated_backward saved.{name} codes"),
                  _dense(scales, sshape, torch.uint8, dev, f"gated_backward saved.{name} scales")]
-    d = GatedDesc(T, D, F, D, ldw, ldh, _type(dh, "gated_backward dh"), act, f)
+    d = GatedDesc(T, D, F, D, ldw, ldh, _type(dh, "gated_backward dh"), act, f, _align(pg, pu))
     ws, pw, nw = _workspace(d, 1, dev)
     dx = torch.empty((T, D), dtype=dtype, device=dev)
     dw_gate = torch.empty((F, D), dtype=dtype, device=dev)

@@ -40,7 +40,7 @@ def test_block_nothing_to_do(hf):
 
 
 def _gated(hf, **kw):
-    d = dict(T=4, D=64, F=96, ldx=64, ldw=64, ldh=96, type=1, act=0, ckpt=hf.fmt((4, 3)))
+    d = dict(T=4, D=64, F=96, ldx=64, ldw=64, ldh=96, type=1, act=0, ckpt=hf.fmt((4, 3)), align=16)
     d.update({k: v for k, v in kw.items() if k in d})
     return hf.GatedDesc(*d.values())
 
@@ -48,7 +48,7 @@ def _gated(hf, **kw):
 @pytest.mark.parametrize("bad,status", [
     (dict(T=-1), -1), (dict(D=0), -1), (dict(F=0), -1), (dict(ldx=63), -1), (dict(ldw=63), -1),
     (dict(ldh=95), -1), (dict(type=0), -2), (dict(type=5), -1), (dict(act=3), -1),
-    (dict(act=-1), -1), (dict(T=1 << 25), -1), (dict(D=1 << 21, ldx=1 << 21, ldw=1 << 21), -1)])
+    (dict(act=-1), -1), (dict(align=0), -1), (dict(align=32), -1), (dict(T=1 << 25), -1), (dict(D=1 << 21, ldx=1 << 21, ldw=1 << 21), -1)])
 def test_gated_refusals(hf, bad, status):
     L, n = hf.lib(), ctypes.c_int64()
     d = _gated(hf, **bad)

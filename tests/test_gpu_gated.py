@@ -266,3 +266,64 @@ def test_graph():
         got = [o.clone() for o in outs]
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, step()))
+
+
+def _act64(g, act):
+    if act == 0:
+        s = torch.sigmoid(g)
+        return g * s, s + g * s * (1 - s)
+    if act == 1:
+        p = torch.special.ndtr(g)
+        return g * p, p + g * torch.exp(-g * g / 2) / (2 * np.pi) ** 0.5
+    return g.clamp(min=0), (g > 0).double()
+
+
+def _within(got, want, bound, what):
+    off = (got.double() - want).abs() - bound
+    assert not off.isnan().any() and off.max() <= 0, (what, float(off.max()))
+
+
+@pytest.mark.parametrize("T,D,F,dtype,f,act", [
+    (520, 136, 12500, "bf16", (4, 3), 0),      # ragged large tiles of the forward product
+    (4000, 2056, 2800, "f16", (5, 2), 1),      # and of both gradients
+    (4096, 2048, 3008, "bf16", (4, 3), 0),
+    (700, 264, 3000, "bf16", (5, 2), 2),       # small tiles, many of them
+    (30, 1000, 9000, "f16", (4, 3), 0),        # a long sum in parts
+    (2500, 4096, 40, "bf16", (4, 3), 1)])
+def test_large(T, D, F, dtype, f, act):
+    """The kernels of large sizes, with the bounds above, against torch in 64 bits on the GPU."""
+    hf = need_gpu()
+    say("large", T, D, F, dtype, f, act)
+    (xt, _), (gt, _), (ut, _), (dt, _) = (
+        _make(r, c, dtype, 20 + i, s) for i, (r, c, s) in enumerate(
+            ((T, D, 1.0), (F, D, 2.0 / D ** 0.5), (F, D, 1.0 / D ** 0.5), (T, F, 0.25))))
+    x, wg, wu, dh = (t.double() for t in (xt, gt, ut, dt))
+    h, saved = hf.gated_forward(xt, gt, ut, act, ckpt=f)
+    g, u = x @ wg.T, x @ wu.T
+    eg, eu = (D * EPS * (x.abs() @ w.abs().T) for w in (wg, wu))
+    a = _act64(g, act)[0]
+    _within(h, a * u, (1.13 * eg + ACT * g.abs()) * (u.abs() + eu) + a.abs() * eu +
+            UNIT[dtype] * (a * u).abs() + TINY[dtype], "h")
+    assert torch.equal(hf.gated_forward(xt, gt, ut, act), h)
+    q = [hf.block_unpack(*b, c, f).double() for b, c in ((saved.x, D), (saved.gate, F), (saved.up, F))]
+    for v, ev, b, name in ((g, eg, q[1], "gate"), (u, eu, q[2], "up")):
+        # a scale at most twice what the group's largest value needs: half a step of that binade
+        pad = torch.nn.functional.pad(v.abs() + ev, (0, -F % 32)).reshape(T, -1, 32)
+        low = 2.0 ** (1 - f[1] - (2 ** (f[0] - 1) - 1) - (8 if f == (4, 3) else 15))
+        small = (pad.amax(2) * 2 * low).repeat_interleave(32, 1)[:, :F]
+        _within(b, v, ev + (v.abs() + ev) * 2.0 ** -f[1] / 2 + small, name)
+    xq, gq, uq = q
+    a, da = _act64(gq, act)
+    dg, du = dh * uq * da, dh * a
+    eg = (dh * uq).abs() * ACT * (1 + gq.abs()) + UNIT[dtype] * dg.abs() + TINY[dtype]
+    eu = dh.abs() * ACT * gq.abs() + UNIT[dtype] * du.abs() + TINY[dtype]
+    ag, au = dg.abs() + eg, du.abs() + eu
+    grads = hf.gated_backward(dt, saved, gt, ut, act)
+    for got, want, e, name in (
+            (grads[0], dg @ wg + du @ wu, eg @ wg.abs() + eu @ wu.abs() +
+             2 * F * EPS * (ag @ wg.abs() + au @ wu.abs()), "dx"),
+            (grads[1], dg.T @ xq, eg.T @ xq.abs() + T * EPS * (ag.T @ xq.abs()), "dw_gate"),
+            (grads[2], du.T @ xq, eu.T @ xq.abs() + T * EPS * (au.T @ xq.abs()), "dw_up")):
+        _within(got, want, e * (1 + UNIT[dtype]) + UNIT[dtype] * want.abs() + TINY[dtype], name)
+    again = hf.gated_backward(dt, saved, gt, ut, act)
+    assert all(torch.equal(p, q) for p, q in zip(grads, again))
