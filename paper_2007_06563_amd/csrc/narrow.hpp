@@ -100,13 +100,13 @@ __device__ __forceinline__ f32x4 decode4(uint32_t w) {
   return f32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
+__device__ __forceinline__ float pow2_scale_of(uint32_t b) {
+  return __uint_as_float(b == 255u ? 0x7FC00000u : b == 0u ? 0x00400000u : b << 23);
+}
 // The scale of a group of 4-bit codes as a float32: a byte's power of two (255:
 // NaN), a bfloat16 or a float32.
 __device__ __forceinline__ float load_scale(const void* s, int64_t i, int kind) {
-  if (kind == HOBFLOPS_SCALE_POW2) {
-    const uint32_t b = ((const uint8_t*)s)[i];
-    return __uint_as_float(b == 255u ? 0x7FC00000u : b == 0u ? 0x00400000u : b << 23);
-  }
+  if (kind == HOBFLOPS_SCALE_POW2) return pow2_scale_of(((const uint8_t*)s)[i]);
   if (kind == HOBFLOPS_SCALE_BF16) return (float)((const __bf16*)s)[i];
   return ((const float*)s)[i];
 }
