@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "block.hpp"
 #include "gemm.hpp"
 #include "narrow.hpp"
@@ -93,13 +95,22 @@ __device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int
   }
 }
 
+// The stages of a kernel: separate arrays, so that the compiler knows that loads into one do not
+// touch the others and puts no wait before the reads of those.
+#define HOBFLOPS_STAGES2(bytes)                         \
+  __shared__ __align__(1024) uint8_t s0[bytes], s1[bytes]; \
+  uint8_t(*const stages[2])[bytes] = {&s0, &s1}
+#define HOBFLOPS_STAGES3(bytes)                                   \
+  __shared__ __align__(1024) uint8_t s0[bytes], s1[bytes], s2[bytes]; \
+  uint8_t(*const stages[3])[bytes] = {&s0, &s1, &s2}
+
 // h = act(x Wg^T) * (x Wu^T): the tile's rows are BI / 2 of w_gate and the same of w_up, a wave
 // has both sums of its outputs.
-template <class T, int kFmt, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(64 * WI * WJ) void forward_kernel(ForwardArgs p) {
+template <class T, int kFmt, int BI, int BJ, int WJ, int S>
+__device__ __forceinline__ void forward_tile(const ForwardArgs& p,
+                                             uint8_t (*const (&stages)[S])[(BI + BJ) * 128]) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
-  __shared__ __align__(1024) uint8_t s0[(BI + BJ) * 128], s1[(BI + BJ) * 128];
+  constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t ti, tj;
   tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
@@ -110,50 +121,17 @@ __global__ __launch_bounds__(64 * WI * WJ) void forward_kernel(ForwardArgs p) {
   la.start(p.w, p.ldw, p.F, i0, p.K, 0, wave, lane);
   lb.start(xs, p.ldx, p.T_, j0, p.K, 0, wave, lane);
   const int wi = wave % WI, wj = wave / WI;
-  ReadRows<T, NI> ra;
-  ReadRows<T, NJ> rb;
+  ReadRows<T, 2 * NI, BI / 2> ra;
+  ReadRows<T, NJ, 0> rb;
   ra.start(wi * NI * 16, lane);
-  rb.start(BI + wj * NJ * 16, lane);
-  f32x4 g[NI][NJ] = {}, u[NI][NJ] = {};
-  const auto compute = [&](const uint8_t* s) {
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      typename T::vec8 fb[NJ], fg[NI], fu[NI];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) fb[j] = rb.get(s, j, ks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) fg[i] = ra.get(s, i, ks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) fu[i] = ra.get(s, i + BI / 32, ks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) g[i][j] = T::mfma(fg[i], fb[j], g[i][j]);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) u[i][j] = T::mfma(fu[i], fb[j], u[i][j]);
-    }
+  rb.start(wj * NJ * 16, lane);
+  f32x4 acc[2 * NI][NJ] = {};
+  const auto load = [&](uint8_t* s) {
+    la.load(s, wave);
+    lb.load(s + BI * 128, wave);
   };
-  const int64_t steps = (p.K + kStepK - 1) / kStepK;
-  la.load(s0, wave);
-  lb.load(s0 + BI * 128, wave);
-  for (int64_t k = 0; k < steps; k += 2) {
-    stage_ready();
-    if (k + 1 < steps) {
-      la.load(s1, wave);
-      lb.load(s1 + BI * 128, wave);
-    }
-    compute(s0);
-    if (k + 1 < steps) {
-      stage_ready();
-      if (k + 2 < steps) {
-        la.load(s0, wave);
-        lb.load(s0 + BI * 128, wave);
-      }
-      compute(s1);
-    }
-  }
+  sum_tiles<T, 2 * NI, NJ, (BI + BJ) / 8 / NW, S>(acc, stages, ra, BI * 128, rb, load,
+                                                  (int)((p.K + kStepK - 1) / kStepK));
   const int q = lane >> 4;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
@@ -165,20 +143,32 @@ __global__ __launch_bounds__(64 * WI * WJ) void forward_kernel(ForwardArgs p) {
       const int64_t f = i0 + wi * NI * 16 + 16 * i + 4 * q;
       float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = gate_act(g[i][j][r], p.act) * u[i][j][r];
+      for (int r = 0; r < 4; ++r) v[r] = gate_act(acc[i][j][r], p.act) * acc[NI + i][j][r];
       if (row_ok) store4<T>(row, f, p.F, p.vec & 1, v);
     }
     if constexpr (kFmt >= 0) {
 #pragma unroll
       for (int i = 0; i < NI; i += 2) {
         const int64_t f0 = i0 + wi * NI * 16 + 16 * i;
-        const f32x4 vg[2] = {g[i][j], g[i + 1][j]}, vu[2] = {u[i][j], u[i + 1][j]};
+        const f32x4 vg[2] = {acc[i][j], acc[i + 1][j]};
+        const f32x4 vu[2] = {acc[NI + i][j], acc[NI + i + 1][j]};
         store_block<kFmt>(p.gate, t, p.F, f0, lane, row_ok, p.vec & 2, vg);
         store_block<kFmt>(p.up, t, p.F, f0, lane, row_ok, p.vec & 2, vu);
       }
     }
   }
 #endif
+}
+
+template <class T, int kFmt>
+__global__ __launch_bounds__(512, 2) void forward_kernel(ForwardArgs p) {
+  HOBFLOPS_STAGES2(512 * 128);
+  forward_tile<T, kFmt, 256, 256, 4, 2>(p, stages);
+}
+template <class T, int kFmt>
+__global__ __launch_bounds__(256, 2) void forward_small_kernel(ForwardArgs p) {
+  HOBFLOPS_STAGES3(192 * 128);
+  forward_tile<T, kFmt, 128, 64, 2, 3>(p, stages);
 }
 
 // The gradients' products, D[i][j] with i along a row of the output:
@@ -195,79 +185,41 @@ struct GradArgs {
   int vec;
   uint32_t ni, nj;
 };
-template <class T, bool kWeights, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(64 * WI * WJ) void grad_kernel(GradArgs p) {
+template <class T, bool kWeights, int BI, int BJ, int WJ, int S>
+__device__ __forceinline__ void grad_tile(const GradArgs& p,
+                                          uint8_t (*const (&stages)[S])[(BI + BJ) * 128]) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
-  __shared__ __align__(1024) uint8_t s0[(BI + BJ) * 128], s1[(BI + BJ) * 128];
+  constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t ti, tj;
   tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
   const int64_t i0 = (int64_t)ti * BI, j0 = (int64_t)tj * BJ;
   const int64_t k0 = (int64_t)blockIdx.y * p.per;
   const int64_t k1 = k0 + p.per < p.K ? k0 + p.per : p.K;
-  const int64_t steps = (k1 - k0 + kStepK - 1) / kStepK;
-  LoadColumns<BI, NW> la;
-  if (kWeights)
-    la.start(p.a[0], p.lda, p.cols, i0, p.K, k0, wave, lane);
-  else if (k0 < p.Fp)
-    la.start(p.a[0], p.lda, p.cols, i0, p.F, k0, wave, lane);
-  else
-    la.start(p.a[1], p.lda, p.cols, i0, p.F, k0 - p.Fp, wave, lane);
-  LoadColumns<BJ, NW> lbc;
-  LoadRows<BJ, NW, 1> lbr;
+  const int steps = (int)((k1 - k0 + kStepK - 1) / kStepK);
+  LoadColumns<BI, NW, kWeights ? 1 : 2> la;
+  std::conditional_t<kWeights, LoadColumns<BJ, NW, 1>, LoadRows<BJ, NW, 1>> lb;
   const void* const bs[1] = {p.b};
-  if (kWeights)
-    lbc.start(p.b, p.ldb, p.nj_, j0, p.K, k0, wave, lane);
-  else
-    lbr.start(bs, p.ldb, p.nj_, j0, p.K, k0, wave, lane);
-  int64_t k = k0;
+  if constexpr (kWeights) {
+    const void* const as[1] = {p.a[0]};
+    la.start(as, p.lda, p.cols, i0, p.K, p.K, k0, k1, wave, lane);
+    lb.start(bs, p.ldb, p.nj_, j0, p.K, p.K, k0, k1, wave, lane);
+  } else {
+    la.start(p.a, p.lda, p.cols, i0, p.F, p.Fp, k0, k1, wave, lane);
+    lb.start(bs, p.ldb, p.nj_, j0, k1, k0, wave, lane);
+  }
   const auto load = [&](uint8_t* s) {
-    if (!kWeights && k == p.Fp && k0 < p.Fp)
-      la.start(p.a[1], p.lda, p.cols, i0, p.F, 0, wave, lane);
     la.load(s, wave);
-    if (kWeights)
-      lbc.load(s + BI * 128, wave);
-    else
-      lbr.load(s + BI * 128, wave);
-    k += kStepK;
+    lb.load(s + BI * 128, wave);
   };
   const int wi = wave % WI, wj = wave / WI;
   ReadColumns<T, NI, BI> ra;
-  ReadColumns<T, NJ, BJ> rbc;
-  ReadRows<T, NJ> rbr;
+  std::conditional_t<kWeights, ReadColumns<T, NJ, BJ>, ReadRows<T, NJ, 0>> rb;
   ra.start(wi * NI * 16, lane);
-  if (kWeights)
-    rbc.start(wj * NJ * 16, lane);
-  else
-    rbr.start(wj * NJ * 16, lane);
+  rb.start(wj * NJ * 16, lane);
   f32x4 acc[NI][NJ] = {};
-  const auto compute = [&](const uint8_t* s) {
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      typename T::vec8 fb[NJ], fa[NI];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        fb[j] = kWeights ? rbc.get(s + BI * 128, j, ks) : rbr.get(s + BI * 128, j, ks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) fa[i] = ra.get(s, i, ks);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
-    }
-  };
-  if (steps > 0) load(s0);
-  for (int64_t n = 0; n < steps; n += 2) {
-    stage_ready();
-    if (n + 1 < steps) load(s1);
-    compute(s0);
-    if (n + 1 < steps) {
-      stage_ready();
-      if (n + 2 < steps) load(s0);
-      compute(s1);
-    }
-  }
+  if (steps > 0)
+    sum_tiles<T, NI, NJ, (BI + BJ) / 8 / NW, S>(acc, stages, ra, BI * 128, rb, load, steps);
   const int q = lane >> 4;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
@@ -289,6 +241,17 @@ __global__ __launch_bounds__(64 * WI * WJ) void grad_kernel(GradArgs p) {
     }
   }
 #endif
+}
+
+template <class T, bool kWeights>
+__global__ __launch_bounds__(512, 2) void grad_kernel(GradArgs p) {
+  HOBFLOPS_STAGES2(512 * 128);
+  grad_tile<T, kWeights, 256, 256, 4, 2>(p, stages);
+}
+template <class T, bool kWeights>
+__global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs p) {
+  HOBFLOPS_STAGES3(256 * 128);
+  grad_tile<T, kWeights, 128, 128, 2, 3>(p, stages);
 }
 
 // Sums the splits of a product in their order.
@@ -445,11 +408,11 @@ void forward_tiles(ForwardArgs& p, hipStream_t s) {
   if (big >= 192) {
     p.ni = (uint32_t)((p.F + 127) / 128);
     p.nj = (uint32_t)((p.T_ + 255) / 256);
-    forward_kernel<T, kFmt, 256, 256, 2, 4><<<p.ni * p.nj, 512, 0, s>>>(p);
+    forward_kernel<T, kFmt><<<p.ni * p.nj, 512, 0, s>>>(p);
   } else {
     p.ni = (uint32_t)((p.F + 63) / 64);
     p.nj = (uint32_t)((p.T_ + 63) / 64);
-    forward_kernel<T, kFmt, 128, 64, 2, 2><<<p.ni * p.nj, 256, 0, s>>>(p);
+    forward_small_kernel<T, kFmt><<<p.ni * p.nj, 256, 0, s>>>(p);
   }
 }
 
@@ -503,9 +466,9 @@ void grad_tiles(GradArgs& p, bool small, int splits, hipStream_t s) {
   p.nj = (uint32_t)((p.nj_ + b - 1) / b);
   const dim3 grid(p.ni * p.nj, (unsigned)splits);
   if (small)
-    grad_kernel<T, kWeights, 128, 128, 2, 2><<<grid, 256, 0, s>>>(p);
+    grad_small_kernel<T, kWeights><<<grid, 256, 0, s>>>(p);
   else
-    grad_kernel<T, kWeights, 256, 256, 2, 4><<<grid, 512, 0, s>>>(p);
+    grad_kernel<T, kWeights><<<grid, 512, 0, s>>>(p);
 }
 
 template <class T>

@@ -36,100 +36,109 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 // uses it has an empty body there.
 #ifdef __HIP_DEVICE_COMPILE__
 
-// A descriptor of what is left of an operand from a point on: `left` bytes, at most 2^31.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rest_of(const void* p, int64_t left) {
-  const int64_t n = left < 0 ? 0 : left > (int64_t)kOutOfRange ? (int64_t)kOutOfRange : left;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)n, 0x00020000);
-}
-
-// Loads a tile of R rows and 64 k of a K-contiguous operand (one or, split by rows into halves,
-// two tensors) into a stage. NW waves.
+// Loads of a tile of R rows and 64 k of a K-contiguous operand (one tensor, or two, each half of
+// the tile's rows) into a stage, step after step. NW waves.
 template <int R, int NW, int kParts>
 struct LoadRows {
   static constexpr int kLoads = R / 8 / NW;  // of a wave: 8 rows each
-  const uint8_t* p[kParts];
-  int64_t left[kParts];  // bytes from the tile's first row on
-  int64_t k_left;
-  uint32_t step, off, chunk;  // bytes between a wave's loads; the lane's offset; its first k / 8
+  __amdgpu_buffer_rsrc_t part[kParts];       // from the tile's first row on
+  uint32_t k, K, step, off;  // the lane's next k; bytes between a wave's loads; the lane's offset
 
+  // row0 < rows: the tile's first row; 256 rows are less than 2^31 bytes apart
   __device__ __forceinline__ void start(const void* const (&src)[kParts], int64_t ld, int64_t rows,
-                                        int64_t row0, int64_t K, int64_t k0, int wave, int lane) {
+                                        int64_t row0, int64_t K_, int64_t k0, int wave, int lane) {
     const int r = 8 * wave + (lane >> 3);
-    chunk = (lane & 7) ^ ((r >> 1) & 7);
-    off = (uint32_t)(r * ld * 2) + chunk * 16;
+    K = (uint32_t)K_;
+    k = (uint32_t)k0 + ((lane & 7) ^ ((r >> 1) & 7)) * 8;
+    off = (uint32_t)(r * ld + k) * 2;
     step = (uint32_t)(8 * NW * ld * 2);
+    const int64_t left = ((rows - row0 - 1) * ld + K_) * 2;
+    const uint32_t range = left < (int64_t)kOutOfRange ? (uint32_t)left : kOutOfRange;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      p[i] = (const uint8_t*)src[i] + (row0 * ld + k0) * 2;
-      left[i] = ((rows - row0 - 1) * ld + K - k0) * 2;
-    }
-    k_left = K - k0;
+    for (int i = 0; i < kParts; ++i)
+      part[i] = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>((const uint8_t*)src[i] + row0 * ld * 2), 0, (int)range, 0x00020000);
   }
   __device__ __forceinline__ void load(uint8_t* stage, int wave) {
-    const uint32_t o = (int64_t)(chunk * 8) < k_left ? off : kOutOfRange;
+    const uint32_t o = k < K ? off : kOutOfRange;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int part = i * kParts / kLoads;
-      const uint32_t so = (uint32_t)(i - part * kLoads / kParts) * step;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rest_of(p[part], left[part]),
-                                               (lds_byte*)(stage + (wave + NW * i) * 1024), 16,
-                                               o + so, 0, 0, 0);
+      const int h = i * kParts / kLoads;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          part[h], (lds_byte*)(stage + (wave + NW * i) * 1024), 16,
+          o + (uint32_t)(i - h * kLoads / kParts) * step, 0, 0, 0);
     }
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      p[i] += kStepK * 2;
-      left[i] -= kStepK * 2;
-    }
-    k_left -= kStepK;
+    k += kStepK;
+    off += kStepK * 2;
   }
 };
 
-// Loads a tile of 64 k and R columns of a K-major operand (one or, one after the other along k,
-// two tensors) into a stage.
-template <int R, int NW>
+// Loads of a tile of 64 k and R columns of a K-major operand (one tensor, or two, one after the
+// other along k, the first padded to a multiple of 64 k) into a stage, step after step.
+template <int R, int NW, int kParts>
 struct LoadColumns {
-  static constexpr int kRowsPer = 512 / R;                 // k of a load
-  static constexpr int kLoads = kStepK / kRowsPer / NW;    // of a wave
-  const uint8_t* p;
-  int64_t left, advance;
+  static constexpr int kRowsPer = 512 / R;               // k of a load
+  static constexpr int kLoads = kStepK / kRowsPer / NW;  // of a wave
+  const uint8_t* p;  // the first tensor's row 0, at the tile's columns
+  int64_t second;
+  int ld2, k, K, Kp, end, width;
   uint32_t step, off;
 
-  // part: the tensor's K rows from k0 on
-  __device__ __forceinline__ void start(const void* src, int64_t ld, int64_t cols, int64_t col0,
-                                        int64_t K, int64_t k0, int wave, int lane) {
-    const int k = wave * kRowsPer + lane / (R / 8);
-    const int f = (k & 3) | ((k >> 3) & 1) << 2;
-    off = (uint32_t)(k * ld * 2) + (uint32_t)(((lane % (R / 8)) ^ (f << 1)) * 16);
-    step = (uint32_t)(NW * kRowsPer * ld * 2);
-    advance = kStepK * ld * 2;
-    p = (const uint8_t*)src + (k0 * ld + col0) * 2;
-    left = ((K - k0 - 1) * ld + cols - col0) * 2;
+  // K: the rows of a tensor, Kp: of the first and its padding, k1: where this sum ends (a step beyond
+  // it loads zeros); 64 rows are less than 2^31 bytes apart
+  __device__ __forceinline__ void start(const void* const (&src)[kParts], int64_t ld, int64_t cols,
+                                        int64_t col0, int64_t K_, int64_t Kp_, int64_t k0,
+                                        int64_t k1, int wave, int lane) {
+    const int r = wave * kRowsPer + lane / (R / 8);
+    const int f = (r & 3) | ((r >> 3) & 1) << 2;
+    ld2 = (int)(ld * 2);
+    k = (int)k0;
+    K = (int)K_;
+    Kp = (int)Kp_;
+    end = (int)k1;
+    width = (int)(cols - col0) * 2;
+    off = (uint32_t)(r * ld2) + (uint32_t)(((lane % (R / 8)) ^ (f << 1)) * 16);
+    step = (uint32_t)(NW * kRowsPer * ld2);
+    p = (const uint8_t*)src[0] + col0 * 2;
+    // the second tensor's distance, less the first one's padded rows: row k - Kp of it is row k of
+    // the first, this much further on
+    second = kParts == 2 ? (int64_t)(uintptr_t)src[kParts - 1] - (int64_t)(uintptr_t)src[0] - Kp_ * ld * 2 : 0;
   }
   __device__ __forceinline__ void load(uint8_t* stage, int wave) {
+    const bool more = kParts == 2 && k >= Kp;
+    int left = K - k + (more ? Kp : 0);
+    left = left < end - k ? left : end - k;
+    left = left < kStepK ? left : kStepK;
+    const int range = (left - 1) * ld2 + width;
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(p + (int64_t)k * ld2 + (more ? second : 0)), 0, left > 0 ? range : 0,
+        0x00020000);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rest_of(p, left),
-                                               (lds_byte*)(stage + (wave + NW * i) * 1024), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_byte*)(stage + (wave + NW * i) * 1024), 16,
                                                off + (uint32_t)i * step, 0, 0, 0);
-    p += advance;
-    left -= advance;
+    k += kStepK;
   }
 };
 
-// Fragments of a stage: N of 16 rows each, k step ks (32 k).
-template <class T, int N>
+// Fragments of a stage: N of 16 rows each, k step ks (32 k). kHalf: the second half of the
+// fragments is that many rows further on (the rows of the second tensor), 0: they follow on.
+template <class T, int N, int kHalf>
 struct ReadRows {
+  static constexpr int kReads = N;  // LDS reads of a k step
   uint32_t at;
   __device__ __forceinline__ void start(int row0, int lane) {
     const int r = lane & 15, q = lane >> 4;
     at = (uint32_t)((row0 + r) * 128 + ((q ^ (r >> 1)) << 4));
   }
   __device__ __forceinline__ typename T::vec8 get(const uint8_t* stage, int i, int ks) const {
-    return *(const typename T::vec8*)(stage + (at ^ (uint32_t)(ks * 64)) + i * 2048);
+    const int row = kHalf == 0 || i < N / 2 ? 16 * i : kHalf + 16 * (i - N / 2);
+    return *(const typename T::vec8*)(stage + (at ^ (uint32_t)(ks * 64)) + row * 128);
   }
 };
 template <class T, int N, int R>
 struct ReadColumns {
+  static constexpr int kReads = 2 * N;
   uint32_t at[N];
   __device__ __forceinline__ void start(int col0, int lane) {
     const int r = lane & 15, q = lane >> 4;
@@ -148,10 +157,75 @@ struct ReadColumns {
   }
 };
 
-// Waits for a wave's loads into LDS, then for the other waves: their loads have landed too, and
-// their reads of the stage that the next loads overwrite are done.
+// Waits until at most kPending of a wave's loads into LDS are under way and its LDS reads are
+// done, then for the other waves.
+template <int kPending>
 __device__ __forceinline__ void stage_ready() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  static_assert(kPending < 64);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kPending) : "memory");
+}
+
+// The order of a half step's instructions: after each matrix instruction its share of the LDS reads
+// and of the loads, so that neither waits for the other.
+template <int kMfma, int kReads, int kLoads>
+__device__ __forceinline__ void interleave() {
+  constexpr int kGroups = kReads > kLoads ? kReads : kLoads;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const int m = kMfma * (i + 1) / kGroups - kMfma * i / kGroups;
+    if (kReads * (i + 1) / kGroups > kReads * i / kGroups) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    if (kLoads * (i + 1) / kGroups > kLoads * i / kGroups) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+    if (m == 1) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (m == 2) __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    if (m == 3) __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
+    if (m == 4) __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    if (m > 4) __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+  }
+}
+
+// The sums of a wave's tile over `steps` steps of 64 k: acc[i][j] += A fragment i times B fragment j.
+// load(stage) issues a wave's kLoads loads of the next step's tiles (beyond the last step: of
+// zeros, so that the number under way is always the same). There are S stages. A step's fragments
+// are read half a step ahead of the matrix instructions that use them, and its tiles loaded S
+// steps ahead: the one wait and barrier of a step stands between its halves, after which the
+// stage that all waves have read takes the tiles S steps on.
+template <class T, int NI, int NJ, int kLoads, int S, int kBytes, class ReadA, class ReadB, class Load>
+__device__ __forceinline__ void sum_tiles(f32x4 (&acc)[NI][NJ], uint8_t (*const (&stage)[S])[kBytes],
+                                          const ReadA& ra, int a_bytes, const ReadB& rb, Load load,
+                                          int steps) {
+  typedef typename T::vec8 Vec;
+  Vec a0[NI], b0[NJ], a1[NI], b1[NJ];
+  const auto read = [&](const uint8_t* s, int ks, Vec(&a)[NI], Vec(&b)[NJ]) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) b[j] = rb.get(s + a_bytes, j, ks);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) a[i] = ra.get(s, i, ks);
+  };
+  const auto multiply = [&](const Vec(&a)[NI], const Vec(&b)[NJ]) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(a[i], b[j], acc[i][j]);
+  };
+#pragma unroll
+  for (int i = 0; i < S; ++i) load(*stage[i]);
+  stage_ready<(S - 1) * kLoads>();
+  read(*stage[0], 0, a0, b0);
+  // whole rounds of the stages (steps beyond the last are of zeros), so that the loop has one exit and
+  // the sums stay in their registers
+  for (int n = 0; n < steps; n += S) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      read(*stage[i], 1, a1, b1);
+      multiply(a0, b0);
+      interleave<NI * NJ, ReadA::kReads + ReadB::kReads, 0>();
+      stage_ready<(S - 2) * kLoads>();
+      load(*stage[i]);
+      read(*stage[(i + 1) % S], 0, a0, b0);
+      multiply(a1, b1);
+      interleave<NI * NJ, ReadA::kReads + ReadB::kReads, kLoads>();
+    }
+  }
 }
 
 #endif  // __HIP_DEVICE_COMPILE__

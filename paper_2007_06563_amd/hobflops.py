@@ -396,6 +396,8 @@ def _rows(t, name):
     if t.dim() != 2:
         raise ValueError(f"{name}: a matrix is needed, not {tuple(t.shape)}")
     r, c = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), r, c, c
     sr, sc = t.stride()
     if (c > 1 and sc != 1) or (r > 1 and sr < c):
         raise ValueError(f"{name}: rows must be dense and not overlap")
@@ -403,38 +405,47 @@ def _rows(t, name):
 
 
 def _type(t, name):
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise TypeError(f"{name}: float32, bfloat16 or float16 values are needed, not {t.dtype}")
-    return _TYPES[t.dtype]
+    return kind
 
 
 def _dense(t, shape, dtype, device, name):
     """The pointer of a dense tensor of this shape, type and device."""
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise TypeError(f"{name}: a tensor on {device} is needed")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} is needed")
     return t.data_ptr()
 
 
 def _out_rows(t, shape, dtype, device, name):
-    """A caller's output matrix (dense rows), or a new one."""
+    """(output matrix, pointer, elements between rows): a caller's, with dense rows, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        t = torch.empty(shape, dtype=dtype, device=device)
+        return t, t.data_ptr(), shape[1]
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: a {dtype} tensor {tuple(shape)} on {device} is needed")
-    return t
+    ptr, _, _, ld = _rows(t, name)
+    return t, ptr, ld
 
 
 def _raw_stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+    """The handle of torch's current stream (torch.cuda.current_stream would make an object of it,
+    at 2 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def block_shapes(rows, cols, f, group=32):
     """The shapes of the codes and of the scales of a [rows, cols] matrix in blocks."""
-    f = fmt(f)
-    bits = 1 + f.wE + f.wF
+    bits = 1 + sum(f) if isinstance(f, tuple) else 1 + f.wE + f.wF
     return (rows, (cols * bits + 7) // 8), (rows, -(-cols // group))
+
+
+def _block_shapes(rows, cols, f, group):
+    # a group that the library refuses: nothing to size, the call reports it
+    return block_shapes(rows, cols, f, group) if group in (32, 64, 128) else ((0, 0), (0, 0))
 
 
 def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
@@ -444,16 +455,22 @@ def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
     f = fmt(f)
     ptr, rows, cols, ld = _rows(src, "block_pack src")
     kind = _type(src, "block_pack src")
-    cshape, sshape = block_shapes(rows, cols, f, group) if group in (32, 64, 128) else ((0,), (0,))
-    stype = _SCALE_TYPES.get(scale, torch.uint8)
+    cshape, sshape = _block_shapes(rows, cols, f, group)
+    stype, dev = _SCALE_TYPES.get(scale, torch.uint8), src.device
     if codes is None:
-        codes = torch.empty(cshape, dtype=torch.uint8, device=src.device)
+        codes = torch.empty(cshape, dtype=torch.uint8, device=dev)
+        pc = codes.data_ptr()
+    else:
+        pc = _dense(codes, cshape, torch.uint8, dev, "block_pack codes")
     if scales is None:
-        scales = torch.empty(sshape, dtype=stype, device=src.device)
-    pc = _dense(codes, cshape, torch.uint8, src.device, "block_pack codes")
-    ps = _dense(scales, sshape, stype, src.device, "block_pack scales")
-    _check(lib().hobflops_block_pack(ptr, kind, rows, cols, ld, f, group, scale, pc, ps,
-                                     _raw_stream(src.device)))
+        scales = torch.empty(sshape, dtype=stype, device=dev)
+        ps = scales.data_ptr()
+    else:
+        ps = _dense(scales, sshape, stype, dev, "block_pack scales")
+    rc = lib().hobflops_block_pack(ptr, kind, rows, cols, ld, f, group, scale, pc, ps,
+                                   _raw_stream(dev))
+    if rc:
+        _check(rc)
     return codes, scales
 
 
@@ -462,19 +479,19 @@ def block_unpack(codes, scales, cols, f, group=32, dtype=torch.float32, out=None
     f = fmt(f)
     if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dim() != 2:
         raise TypeError("block_unpack: codes [rows, bytes] on a GPU are needed")
-    rows = codes.shape[0]
-    cshape, sshape = block_shapes(rows, cols, f, group) if group in (32, 64, 128) else ((0,), (0,))
+    rows, dev = codes.shape[0], codes.device
+    cshape, sshape = _block_shapes(rows, cols, f, group)
     if scales.dtype not in _SCALES:
         raise TypeError(f"block_unpack: scales of {scales.dtype}")
-    pc = _dense(codes, cshape, torch.uint8, codes.device, "block_unpack codes")
-    ps = _dense(scales, sshape, scales.dtype, codes.device, "block_unpack scales")
+    pc = _dense(codes, cshape, torch.uint8, dev, "block_unpack codes")
+    ps = _dense(scales, sshape, scales.dtype, dev, "block_unpack scales")
     if out is not None:
         dtype = out.dtype
-    out = _out_rows(out, (rows, cols), dtype, codes.device, "block_unpack out")
-    ptr, _, _, ld = _rows(out, "block_unpack out")
-    _check(lib().hobflops_block_unpack(pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
-                                       _type(out, "block_unpack out"), ld,
-                                       _raw_stream(codes.device)))
+    out, ptr, ld = _out_rows(out, (rows, cols), dtype, dev, "block_unpack out")
+    rc = lib().hobflops_block_unpack(pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
+                                     _type(out, "block_unpack out"), ld, _raw_stream(dev))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -516,8 +533,7 @@ def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
     pg, pu, F, Dw, ldw = _gated_weights(x, w_gate, w_up)
     if Dw != D:
         raise ValueError("gated_forward: x and the weights differ in D")
-    h = _out_rows(out, (T, F), x.dtype, x.device, "gated_forward out")
-    ph, _, _, ldh = _rows(h, "gated_forward out")
+    h, ph, ldh = _out_rows(out, (T, F), x.dtype, x.device, "gated_forward out")
     f = Fmt(0, 0) if ckpt is None else fmt(ckpt)
     d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f,
                   _align(px, pg, pu))
@@ -561,32 +577,37 @@ def gated_backward(dh, saved, w_gate, w_up, act=GATE_SILU):
 
 
 def _w4(x, weights, group, out, name):
-    """Checked arguments of a product with 4-bit weights, up to and from the weights' pointers."""
-    px, T, K, ldx = _rows(x, f"{name} x")
-    N, scale, ptrs = weights[0].shape[0], weights[1].dtype, []
+    """Checked arguments of a product with 4-bit weights: the output, and what comes before and
+    after the activation."""
+    px, T, K, ldx = _rows(x, name)
+    dev, scale = x.device, weights[1].dtype
     if scale not in _SCALES:
         raise TypeError(f"{name}: scales of {scale}")
     if group not in (32, 64, 128):
         raise ValueError(f"{name}: groups of 32, 64 or 128 are supported, not {group}")
-    for i in range(0, len(weights), 2):
-        ptrs += [_dense(weights[i], (N, (K + 1) // 2), torch.uint8, x.device, f"{name} codes"),
-                 _dense(weights[i + 1], (N, -(-K // group)), scale, x.device, f"{name} scales")]
-    y = _out_rows(out, (T, N), x.dtype, x.device, f"{name} out")
-    py, _, _, ldy = _rows(y, f"{name} out")
-    head = (px, _type(x, f"{name} x"), T, K, N, ldx, *ptrs, group, _SCALES[scale])
-    return y, head, (py, ldy, _raw_stream(x.device))
+    N = weights[0].shape[0]
+    cshape, sshape = (N, (K + 1) // 2), (N, -(-K // group))
+    ptrs = [_dense(w, sshape if i & 1 else cshape, scale if i & 1 else torch.uint8, dev, name)
+            for i, w in enumerate(weights)]
+    y, py, ldy = _out_rows(out, (T, N), x.dtype, dev, name)
+    return (y, (px, _type(x, name), T, K, N, ldx, *ptrs, group, _SCALES[scale]),
+            (py, ldy, _raw_stream(dev)))
 
 
 def w4_linear(x, codes, scales, group=32, out=None):
     """y = x W^T for few tokens: x [T, K] bfloat16 or float16, W [N, K] as 4-bit codes and scales
     (block_pack with the format (2, 1)) -> y [T, N]."""
     y, head, tail = _w4(x, (codes, scales), group, out, "w4_linear")
-    _check(lib().hobflops_w4_linear(*head, *tail))
+    rc = lib().hobflops_w4_linear(*head, *tail)
+    if rc:
+        _check(rc)
     return y
 
 
 def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, out=None):
     """h = act(x Wg^T) * (x Wu^T) for few tokens, both weights as 4-bit codes and scales."""
     y, head, tail = _w4(x, (g_codes, g_scales, u_codes, u_scales), group, out, "w4_gated")
-    _check(lib().hobflops_w4_gated(*head, act, *tail))
+    rc = lib().hobflops_w4_gated(*head, act, *tail)
+    if rc:
+        _check(rc)
     return y
