@@ -57,58 +57,102 @@ struct ForwardArgs {
   uint32_t ni, nj;
 };
 
-// The scale and codes of 32 values of a token: 8 in each of the lanes l, l ^ 16, l ^ 32, l ^ 48,
-// v[i] the values 16 i + 4 (lane / 16) + 0..3 of the group.
-template <int kFmt>
-__device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int64_t F, int64_t f0,
-                                            int lane, bool row_ok, bool vec, const f32x4 (&v)[2]) {
-  const int q = lane >> 4;
-  uint32_t a = 0;
+// A tile's sums stand with a lane's column lane % 16 and its rows 4 (lane / 16) + 0..3. For two tiles
+// one after the other in rows, a word (of one value, or of several) of each, a and b, is exchanged
+// between the four lanes of a column so that a lane has two neighbouring words: lane / 16 = q then
+// holds words 2 q and 2 q + 1 of the column's eight.
+__device__ __forceinline__ void gather_rows(uint32_t& a, uint32_t& b) {
+  const auto x = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+  a = y[0];
+  b = y[1];
+}
+
+// Two values rounded to 16 bits each, the first in the lower half.
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const typename T::vec2 v = {(typename T::elem)a, (typename T::elem)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// 32 rows of a column, from two tiles' sums, as 16-bit values at p[0..31], those before `end`:
+// 16 bytes a lane.
+template <class T>
+__device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, bool vec, bool ok, int lane,
+                                           f32x4 v0, f32x4 v1) {
+  uint32_t a0 = pack2<T>(v0[0], v0[1]), a1 = pack2<T>(v0[2], v0[3]);
+  uint32_t b0 = pack2<T>(v1[0], v1[1]), b1 = pack2<T>(v1[2], v1[3]);
+  gather_rows(a0, b0);
+  gather_rows(a1, b1);
+  if (!ok) return;
+  const u32x4v w = {a0, a1, b0, b1};
+  const int row = 8 * (lane >> 4);
+  if (vec && row + 8 <= end) {
+    __builtin_memcpy(__builtin_assume_aligned(p + row, 16), &w, 16);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const uint32_t m = f0 + 16 * i + 4 * q + r < F ? finite_abs(v[i][r]) : 0u;
-      a = a > m ? a : m;
-    }
-#pragma unroll
-  for (int m = 16; m < 64; m <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)a, m);
-    a = a > o ? a : o;
-  }
-  const int k = block_scale<kFmt>(a);
-  const float s = pow2f(-k);
-  if (!row_ok || f0 >= F) return;
-  if (q == 0) b.scales[t * ((F + 31) / 32) + f0 / 32] = (uint8_t)(k + 127);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t w = encode4<kFmt>(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
-    const int64_t f = f0 + 16 * i + 4 * q;
-    uint8_t* p = b.codes + t * F + f;
-    if (vec && f + 4 <= F) {
-      __builtin_memcpy(__builtin_assume_aligned(p, 4), &w, 4);
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (f + r < F) p[r] = (uint8_t)(w >> (8 * r));
-    }
+    for (int i = 0; i < 8; ++i)
+      if (row + i < end) {
+        const uint16_t e = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        __builtin_memcpy(p + row + i, &e, 2);
+      }
   }
 }
 
-// The stages of a kernel: separate arrays, so that the compiler knows that loads into one do not
-// touch the others and puts no wait before the reads of those.
-#define HOBFLOPS_STAGES2(bytes)                         \
-  __shared__ __align__(1024) uint8_t s0[bytes], s1[bytes]; \
-  uint8_t(*const stages[2])[bytes] = {&s0, &s1}
-#define HOBFLOPS_STAGES3(bytes)                                   \
-  __shared__ __align__(1024) uint8_t s0[bytes], s1[bytes], s2[bytes]; \
-  uint8_t(*const stages[3])[bytes] = {&s0, &s1, &s2}
+// The scale and codes of 32 rows of a column, from two tiles' sums: a group of token t from f0 on.
+template <int kFmt>
+__device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int64_t F, int64_t f0,
+                                            int lane, bool ok, bool vec, f32x4 v0, f32x4 v1) {
+  const int q = lane >> 4;
+  uint32_t a = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t m0 = f0 + 4 * q + r < F ? finite_abs(v0[r]) : 0u;
+    const uint32_t m1 = f0 + 16 + 4 * q + r < F ? finite_abs(v1[r]) : 0u;
+    a = a > m0 ? a : m0;
+    a = a > m1 ? a : m1;
+  }
+  const auto x = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  a = x[0] > x[1] ? x[0] : x[1];
+  const auto y = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  a = y[0] > y[1] ? y[0] : y[1];
+  const int k = block_scale<kFmt>(a);
+  const float s = pow2f(-k);
+  uint32_t w[2] = {encode4<kFmt>(v0[0] * s, v0[1] * s, v0[2] * s, v0[3] * s),
+                   encode4<kFmt>(v1[0] * s, v1[1] * s, v1[2] * s, v1[3] * s)};
+  gather_rows(w[0], w[1]);
+  if (!ok || f0 >= F) return;
+  if (q == 0) b.scales[t * ((F + 31) / 32) + f0 / 32] = (uint8_t)(k + 127);
+  const int64_t f = f0 + 8 * q;
+  uint8_t* p = b.codes + t * F + f;
+  if (vec && f + 8 <= F) {
+    __builtin_memcpy(__builtin_assume_aligned(p, 8), w, 8);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (f + r < F) p[r] = (uint8_t)(w[r >> 2] >> (8 * (r & 3)));
+  }
+}
+
+// The stages of a kernel: an array each, so that the compiler knows that loads into one do not touch the
+// others and puts no wait before the reads of those; the stages of one operand next to each
+// other, so that one address and the reads' constant offsets reach all of them.
+#define HOBFLOPS_STAGES2(rows_a, rows_b)                                              \
+  __shared__ __align__(1024) uint8_t a0[rows_a * 128], a1[rows_a * 128];              \
+  __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128];              \
+  uint8_t* const sa[2] = {a0, a1};                                                    \
+  uint8_t* const sb[2] = {b0, b1}
+#define HOBFLOPS_STAGES3(rows_a, rows_b)                                                    \
+  __shared__ __align__(1024) uint8_t a0[rows_a * 128], a1[rows_a * 128], a2[rows_a * 128];  \
+  __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128], b2[rows_b * 128];  \
+  uint8_t* const sa[3] = {a0, a1, a2};                                                      \
+  uint8_t* const sb[3] = {b0, b1, b2}
 
 // h = act(x Wg^T) * (x Wu^T): the tile's rows are BI / 2 of w_gate and the same of w_up, a wave
 // has both sums of its outputs.
 template <class T, int kFmt, int BI, int BJ, int WJ, int S>
-__device__ __forceinline__ void forward_tile(const ForwardArgs& p,
-                                             uint8_t (*const (&stages)[S])[(BI + BJ) * 128]) {
+__device__ __forceinline__ void forward_tile(const ForwardArgs& p, uint8_t* const (&sa)[S],
+                                             uint8_t* const (&sb)[S]) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -126,34 +170,28 @@ __device__ __forceinline__ void forward_tile(const ForwardArgs& p,
   ra.start(wi * NI * 16, lane);
   rb.start(wj * NJ * 16, lane);
   f32x4 acc[2 * NI][NJ] = {};
-  const auto load = [&](uint8_t* s) {
-    la.load(s, wave);
-    lb.load(s + BI * 128, wave);
+  const auto load = [&](int s) {
+    la.load(sa[s], wave);
+    lb.load(sb[s], wave);
   };
-  sum_tiles<T, 2 * NI, NJ, (BI + BJ) / 8 / NW, S>(acc, stages, ra, BI * 128, rb, load,
+  sum_tiles<T, 2 * NI, NJ, (BI + BJ) / 8 / NW, S>(acc, sa, sb, ra, rb, load,
                                                   (int)((p.K + kStepK - 1) / kStepK));
-  const int q = lane >> 4;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int64_t t = j0 + wj * NJ * 16 + 16 * j + (lane & 15);
-    const bool row_ok = t < p.T_;
-    typename T::elem* row = (typename T::elem*)p.h + (row_ok ? t : 0) * p.ldh;
+    const bool ok = t < p.T_;
+    typename T::elem* row = (typename T::elem*)p.h + (ok ? t : 0) * p.ldh;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int64_t f = i0 + wi * NI * 16 + 16 * i + 4 * q;
-      float v[4];
+    for (int i = 0; i < NI; i += 2) {
+      const int64_t f = i0 + wi * NI * 16 + 16 * i;
+      f32x4 v[2];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = gate_act(acc[i][j][r], p.act) * acc[NI + i][j][r];
-      if (row_ok) store4<T>(row, f, p.F, p.vec & 1, v);
-    }
-    if constexpr (kFmt >= 0) {
-#pragma unroll
-      for (int i = 0; i < NI; i += 2) {
-        const int64_t f0 = i0 + wi * NI * 16 + 16 * i;
-        const f32x4 vg[2] = {acc[i][j], acc[i + 1][j]};
-        const f32x4 vu[2] = {acc[NI + i][j], acc[NI + i + 1][j]};
-        store_block<kFmt>(p.gate, t, p.F, f0, lane, row_ok, p.vec & 2, vg);
-        store_block<kFmt>(p.up, t, p.F, f0, lane, row_ok, p.vec & 2, vu);
+      for (int r = 0; r < 8; ++r)
+        v[r >> 2][r & 3] = gate_act(acc[i + (r >> 2)][j][r & 3], p.act) * acc[NI + i + (r >> 2)][j][r & 3];
+      store_rows<T>(row + f, p.F - f, p.vec & 1, ok, lane, v[0], v[1]);
+      if constexpr (kFmt >= 0) {
+        store_block<kFmt>(p.gate, t, p.F, f, lane, ok, p.vec & 2, acc[i][j], acc[i + 1][j]);
+        store_block<kFmt>(p.up, t, p.F, f, lane, ok, p.vec & 2, acc[NI + i][j], acc[NI + i + 1][j]);
       }
     }
   }
@@ -162,13 +200,13 @@ __device__ __forceinline__ void forward_tile(const ForwardArgs& p,
 
 template <class T, int kFmt>
 __global__ __launch_bounds__(512, 2) void forward_kernel(ForwardArgs p) {
-  HOBFLOPS_STAGES2(512 * 128);
-  forward_tile<T, kFmt, 256, 256, 4, 2>(p, stages);
+  HOBFLOPS_STAGES2(256, 256);
+  forward_tile<T, kFmt, 256, 256, 4, 2>(p, sa, sb);
 }
 template <class T, int kFmt>
 __global__ __launch_bounds__(256, 2) void forward_small_kernel(ForwardArgs p) {
-  HOBFLOPS_STAGES3(192 * 128);
-  forward_tile<T, kFmt, 128, 64, 2, 3>(p, stages);
+  HOBFLOPS_STAGES3(128, 64);
+  forward_tile<T, kFmt, 128, 64, 2, 3>(p, sa, sb);
 }
 
 // The gradients' products, D[i][j] with i along a row of the output:
@@ -186,8 +224,8 @@ struct GradArgs {
   uint32_t ni, nj;
 };
 template <class T, bool kWeights, int BI, int BJ, int WJ, int S>
-__device__ __forceinline__ void grad_tile(const GradArgs& p,
-                                          uint8_t (*const (&stages)[S])[(BI + BJ) * 128]) {
+__device__ __forceinline__ void grad_tile(const GradArgs& p, uint8_t* const (&sa)[S],
+                                          uint8_t* const (&sb)[S]) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -208,9 +246,9 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p,
     la.start(p.a, p.lda, p.cols, i0, p.F, p.Fp, k0, k1, wave, lane);
     lb.start(bs, p.ldb, p.nj_, j0, k1, k0, wave, lane);
   }
-  const auto load = [&](uint8_t* s) {
-    la.load(s, wave);
-    lb.load(s + BI * 128, wave);
+  const auto load = [&](int s) {
+    la.load(sa[s], wave);
+    lb.load(sb[s], wave);
   };
   const int wi = wave % WI, wj = wave / WI;
   ReadColumns<T, NI, BI> ra;
@@ -219,24 +257,23 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p,
   rb.start(wj * NJ * 16, lane);
   f32x4 acc[NI][NJ] = {};
   if (steps > 0)
-    sum_tiles<T, NI, NJ, (BI + BJ) / 8 / NW, S>(acc, stages, ra, BI * 128, rb, load, steps);
-  const int q = lane >> 4;
+    sum_tiles<T, NI, NJ, (BI + BJ) / 8 / NW, S>(acc, sa, sb, ra, rb, load, steps);
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int64_t c = j0 + wj * NJ * 16 + 16 * j + (lane & 15);
-    if (c >= p.nj_) continue;
     const int64_t half = kWeights && c >= p.Fp ? 1 : 0, row = c - half * p.Fp;
-    if (kWeights && row >= p.F) continue;
+    const bool ok = c < p.nj_ && (!kWeights || row < p.F);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int64_t d = i0 + wi * NI * 16 + 16 * i + 4 * q;
-      if (d >= p.ni_) continue;
+    for (int i = 0; i < NI; i += 2) {
+      const int64_t d = i0 + wi * NI * 16 + 16 * i;
       if (p.part) {
-        const int64_t ldp = (p.ni_ + 3) & ~(int64_t)3;
-        *(f32x4*)(p.part + ((int64_t)blockIdx.y * p.nj_ + c) * ldp + d) = acc[i][j];
+        const int64_t ldp = (p.ni_ + 3) & ~(int64_t)3, at = d + 4 * (lane >> 4);
+        float* to = p.part + ((int64_t)blockIdx.y * p.nj_ + c) * ldp + at;
+        if (ok && at < p.ni_) *(f32x4*)to = acc[i][j];
+        if (ok && at + 16 < p.ni_) *(f32x4*)(to + 16) = acc[i + 1][j];
       } else {
-        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        store4<T>((typename T::elem*)p.out[half] + row * p.ni_, d, p.ni_, p.vec, v);
+        store_rows<T>((typename T::elem*)p.out[half] + (ok ? row : 0) * p.ni_ + d, p.ni_ - d, p.vec, ok,
+                      lane, acc[i][j], acc[i + 1][j]);
       }
     }
   }
@@ -245,13 +282,13 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p,
 
 template <class T, bool kWeights>
 __global__ __launch_bounds__(512, 2) void grad_kernel(GradArgs p) {
-  HOBFLOPS_STAGES2(512 * 128);
-  grad_tile<T, kWeights, 256, 256, 4, 2>(p, stages);
+  HOBFLOPS_STAGES2(256, 256);
+  grad_tile<T, kWeights, 256, 256, 4, 2>(p, sa, sb);
 }
 template <class T, bool kWeights>
 __global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs p) {
-  HOBFLOPS_STAGES3(256 * 128);
-  grad_tile<T, kWeights, 128, 128, 2, 3>(p, stages);
+  HOBFLOPS_STAGES3(128, 128);
+  grad_tile<T, kWeights, 128, 128, 2, 3>(p, sa, sb);
 }
 
 // Sums the splits of a product in their order.
@@ -448,8 +485,8 @@ hipError_t forward(const hobflops_gated_desc& d, const GatedForward& c, int fmt,
   p.gate = c.gate;
   p.up = c.up;
   p.act = d.act;
-  p.vec = (((uintptr_t)c.h & 7u) == 0 && d.ldh % 4 == 0 ? 1 : 0) |
-          (((uintptr_t)c.gate.codes & 3u) == 0 && ((uintptr_t)c.up.codes & 3u) == 0 && d.F % 4 == 0 ? 2 : 0);
+  p.vec = (aligned16(c.h) && d.ldh % 8 == 0 ? 1 : 0) |
+          (((uintptr_t)c.gate.codes & 7u) == 0 && ((uintptr_t)c.up.codes & 7u) == 0 && d.F % 8 == 0 ? 2 : 0);
   if (fmt == kE4M3)
     forward_tiles<T, kE4M3>(p, s);
   else if (fmt == kE5M2)
@@ -500,7 +537,7 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.ldb = 2 * plan.Fp;
   p.ni_ = d.D;
   p.cols = plan.Dp;
-  p.vec = d.D % 4 == 0;  // the outputs are dense
+  const bool rows8 = d.D % 8 == 0;  // the outputs are dense
   GradArgs w = p;
   w.a[0] = ws + plan.x;
   w.lda = plan.Dp;
@@ -509,7 +546,7 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   w.per = round_up(d.T, kStepK);
   w.out[0] = c.dw_gate;
   w.out[1] = c.dw_up;
-  w.vec = p.vec && ((uintptr_t)c.dw_gate & 7u) == 0 && ((uintptr_t)c.dw_up & 7u) == 0;
+  w.vec = rows8 && aligned16(c.dw_gate) && aligned16(c.dw_up);
   const int64_t wt = ((d.D + 255) / 256) * ((2 * plan.Fp + 255) / 256);
   grad_tiles<T, true>(w, wt < 192, 1, s);
   p.a[0] = c.w_gate;
@@ -525,7 +562,7 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.nj_ = d.T;
   p.K = 2 * plan.Fp;
   p.out[0] = c.dx;
-  p.vec = p.vec && ((uintptr_t)c.dx & 7u) == 0;
+  p.vec = rows8 && aligned16(c.dx);
   p.per = round_up((p.K + plan.splits - 1) / plan.splits, kStepK);
   const int splits = (int)((p.K + p.per - 1) / p.per);
   if (plan.part >= 0) p.part = (float*)(ws + plan.part);

@@ -165,65 +165,78 @@ __device__ __forceinline__ void stage_ready() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kPending) : "memory");
 }
 
-// The order of a half step's instructions: after each matrix instruction its share of the LDS reads
-// and of the loads, so that neither waits for the other.
+// The order of a quarter step's instructions: LDS reads behind the first of the matrix instructions, so
+// that they are done when the quarter is, loads spread over all of them.
 template <int kMfma, int kReads, int kLoads>
 __device__ __forceinline__ void interleave() {
-  constexpr int kGroups = kReads > kLoads ? kReads : kLoads;
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    const int m = kMfma * (i + 1) / kGroups - kMfma * i / kGroups;
-    if (kReads * (i + 1) / kGroups > kReads * i / kGroups) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    if (kLoads * (i + 1) / kGroups > kLoads * i / kGroups) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-    if (m == 1) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if (m == 2) __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-    if (m == 3) __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
-    if (m == 4) __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-    if (m > 4) __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+  for (int i = 0; i < kMfma; ++i) {
+#pragma unroll
+    for (int n = kReads * i / kMfma; n < kReads * (i + 1) / kMfma; ++n)
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+    for (int n = kLoads * i / kMfma; n < kLoads * (i + 1) / kMfma; ++n)
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
   }
 }
 
 // The sums of a wave's tile over `steps` steps of 64 k: acc[i][j] += A fragment i times B fragment j.
-// load(stage) issues a wave's kLoads loads of the next step's tiles (beyond the last step: of
-// zeros, so that the number under way is always the same). There are S stages. A step's fragments
-// are read half a step ahead of the matrix instructions that use them, and its tiles loaded S
-// steps ahead: the one wait and barrier of a step stands between its halves, after which the
-// stage that all waves have read takes the tiles S steps on.
-template <class T, int NI, int NJ, int kLoads, int S, int kBytes, class ReadA, class ReadB, class Load>
-__device__ __forceinline__ void sum_tiles(f32x4 (&acc)[NI][NJ], uint8_t (*const (&stage)[S])[kBytes],
-                                          const ReadA& ra, int a_bytes, const ReadB& rb, Load load,
-                                          int steps) {
+// load(s) issues a wave's kLoads loads of the next step's tiles into stage s (beyond the last step: of
+// zeros, so that the number under way is always the same). There are S stages.
+//
+// A half step (32 k) multiplies the lower half of A's fragments, then the upper half; each quarter
+// reads what the next one needs (the upper half; or the next half step's B and lower half), so that
+// half of A's fragments and two sets of B's are held, not two of both: the registers just last, and one
+// spilled to memory would cost more than any wait. A step's tiles are loaded S steps ahead: the one wait
+// and barrier of a step stands before its last quarter, after which the stage that all waves
+// have read takes the tiles S steps on.
+template <class T, int NI, int NJ, int kLoads, int S, class ReadA, class ReadB, class Load>
+__device__ __forceinline__ void sum_tiles(f32x4 (&acc)[NI][NJ], uint8_t* const (&sa)[S],
+                                          uint8_t* const (&sb)[S], const ReadA& ra, const ReadB& rb,
+                                          Load load, int steps) {
   typedef typename T::vec8 Vec;
-  Vec a0[NI], b0[NJ], a1[NI], b1[NJ];
-  const auto read = [&](const uint8_t* s, int ks, Vec(&a)[NI], Vec(&b)[NJ]) {
+  constexpr int H = NI / 2, kReadsA = ReadA::kReads / 2, kReadsB = ReadB::kReads;
+  Vec lo[H], hi[H], b[2][NJ];
+  const auto read_first = [&](int s, int ks) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) b[j] = rb.get(s + a_bytes, j, ks);
+    for (int j = 0; j < NJ; ++j) b[ks][j] = rb.get(sb[s], j, ks);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) a[i] = ra.get(s, i, ks);
+    for (int i = 0; i < H; ++i) lo[i] = ra.get(sa[s], i, ks);
   };
-  const auto multiply = [&](const Vec(&a)[NI], const Vec(&b)[NJ]) {
+  const auto read_upper = [&](int s, int ks) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < H; ++i) hi[i] = ra.get(sa[s], H + i, ks);
+  };
+  const auto multiply = [&](const Vec(&a)[H], int first, int ks) {
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(a[i], b[j], acc[i][j]);
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[first + i][j] = T::mfma(a[i], b[ks][j], acc[first + i][j]);
   };
 #pragma unroll
-  for (int i = 0; i < S; ++i) load(*stage[i]);
+  for (int i = 0; i < S; ++i) load(i);
   stage_ready<(S - 1) * kLoads>();
-  read(*stage[0], 0, a0, b0);
+  read_first(0, 0);
   // whole rounds of the stages (steps beyond the last are of zeros), so that the loop has one exit and
   // the sums stay in their registers
   for (int n = 0; n < steps; n += S) {
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-      read(*stage[i], 1, a1, b1);
-      multiply(a0, b0);
-      interleave<NI * NJ, ReadA::kReads + ReadB::kReads, 0>();
+    for (int s = 0; s < S; ++s) {
+      read_upper(s, 0);
+      multiply(lo, 0, 0);
+      interleave<H * NJ, kReadsA, 0>();
+      read_first(s, 1);
+      multiply(hi, H, 0);
+      interleave<H * NJ, kReadsA + kReadsB, 0>();
+      read_upper(s, 1);
+      multiply(lo, 0, 1);
+      interleave<H * NJ, kReadsA, 0>();
       stage_ready<(S - 2) * kLoads>();
-      load(*stage[i]);
-      read(*stage[(i + 1) % S], 0, a0, b0);
-      multiply(a1, b1);
-      interleave<NI * NJ, ReadA::kReads + ReadB::kReads, kLoads>();
+      load(s);
+      read_first((s + 1) % S, 0);
+      multiply(hi, H, 1);
+      interleave<H * NJ, kReadsA + kReadsB, kLoads>();
     }
   }
 }

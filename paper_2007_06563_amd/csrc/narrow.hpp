@@ -10,6 +10,7 @@ namespace hobflops {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
@@ -24,6 +25,9 @@ struct TypeBF16 {
   static __device__ __forceinline__ f32x4 mfma(vec8 a, vec8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ f32x16 mfma32(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
 };
 struct TypeF16 {
   typedef _Float16 elem;
@@ -31,6 +35,9 @@ struct TypeF16 {
   typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x4 mfma(vec8 a, vec8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mfma32(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
 };
 
@@ -112,7 +119,11 @@ __device__ __forceinline__ float load_scale(const void* s, int64_t i, int kind) 
 }
 
 // The gate's activation and its derivative.
-__device__ __forceinline__ float sigmoidf(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// (the reciprocal instruction is within one unit in the last place, the division around it would
+// cost ten instructions)
+__device__ __forceinline__ float sigmoidf(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+}
 __device__ __forceinline__ float normal_cdf(float g) {
   return 0.5f * (1.0f + erff(g * 0.70710678118654752f));
 }
