@@ -122,12 +122,6 @@ __global__ __launch_bounds__(kThreads) void block_pack_kernel(BlockParams p) {
   }
 }
 
-__device__ __forceinline__ float decode_e2m1(uint32_t c) {
-  const uint32_t m = c & 7u;
-  const float v = m < 2 ? 0.5f * (float)m : pow2f((int)(m >> 1) - 1) * (m & 1u ? 1.5f : 1.0f);
-  return __uint_as_float(__float_as_uint(v) | (c & 8u) << 28);
-}
-
 template <class T, int kFmt>
 __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;

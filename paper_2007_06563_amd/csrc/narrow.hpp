@@ -107,6 +107,13 @@ __device__ __forceinline__ f32x4 decode4(uint32_t w) {
   return f32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
+// The value of a (2, 1) code, unscaled.
+__device__ __forceinline__ float decode_e2m1(uint32_t c) {
+  const uint32_t m = c & 7u;
+  const float v = m < 2 ? 0.5f * (float)m : pow2f((int)(m >> 1) - 1) * (m & 1u ? 1.5f : 1.0f);
+  return __uint_as_float(__float_as_uint(v) | (c & 8u) << 28);
+}
+
 __device__ __forceinline__ float pow2_scale_of(uint32_t b) {
   return __uint_as_float(b == 255u ? 0x7FC00000u : b == 0u ? 0x00400000u : b << 23);
 }

@@ -3,8 +3,8 @@
 // h = act(x Wg^T) * (x Wu^T).
 //
 // What must move is the weights, half a byte each and read once, so they go straight
-// from global memory to registers, 16 bytes (32 codes of a row) a lane. A workgroup has
-// 16 rows of W and all of K, its waves a part of K each; their sums meet in LDS. The
+// from global memory to registers, 16 bytes (32 codes of a row) a lane. A wave has 16
+// rows of W, all of K or a part; the sums of the parts meet in LDS. The
 // 16x16x32 matrix instruction does the products for up to 16 tokens at a time whatever
 // their number: its A operand is x (rows: tokens), its B operand the weights, whose column
 // (a row of W) stays in the lane that loaded the codes, so that the lane's own scale
@@ -25,197 +25,442 @@
 namespace hobflops {
 namespace {
 
-constexpr int kSpan = 128;  // k of a step: 32 of each of the four lanes of a row
+constexpr int kUnit = 256;   // k of a unit: two times 32 of each of the four lanes of a row
+constexpr int kWaves = 8;    // of a workgroup
+constexpr int kStreamUnits = 4;  // of a wave, at most, in the streaming kernel: their scales are in registers
+constexpr int kCUs = 256;
+constexpr int kLds = 160 * 1024;
 
 #ifdef __HIP_DEVICE_COMPILE__
+// Eight codes times a power of two.
 template <class T>
-__device__ __forceinline__ typename T::vec8 decode8(uint32_t w);
+__device__ __forceinline__ typename T::vec8 decode8(uint32_t w, float s);
 template <>
-__device__ __forceinline__ TypeBF16::vec8 decode8<TypeBF16>(uint32_t w) {
-  TypeBF16::vec2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3)};
+__device__ __forceinline__ TypeBF16::vec8 decode8<TypeBF16>(uint32_t w, float s) {
+  TypeBF16::vec2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3)};
   return __builtin_bit_cast(TypeBF16::vec8, v);
 }
 template <>
-__device__ __forceinline__ TypeF16::vec8 decode8<TypeF16>(uint32_t w) {
-  TypeF16::vec2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2),
-                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3)};
+__device__ __forceinline__ TypeF16::vec8 decode8<TypeF16>(uint32_t w, float s) {
+  TypeF16::vec2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2),
+                        __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3)};
   return __builtin_bit_cast(TypeF16::vec8, v);
 }
 
-// The codes of a lane for one step (32 of its row) and the scales of the step's groups.
-template <int kScale, int kGroup>
-struct Step {
-  static constexpr int kScales = kSpan / kGroup;
-  u32x4v codes;
-  float scale[kScales];
+// Whether all four bytes are scales 2^k with which the weights themselves, code times 2^k, are exact in the
+// type: k of -63..64 in bfloat16, -19..12 in float16 (0.5 * 2^-19 is one of its subnormal values).
+template <class T>
+__device__ __forceinline__ bool exact_scales(uint32_t w) {
+  if constexpr (std::is_same_v<T, TypeBF16>)
+    return ((w ^ (w << 1)) & 0x80808080u) == 0x80808080u;
+  else
+    return ((w + 0x14141414u) & 0xE0E0E0E0u) == 0x80808080u;
+}
 
-  __device__ __forceinline__ void load(const W4Matrix& m, int64_t row, int64_t K, int64_t row_bytes,
-                                       int64_t groups, int64_t step, int q, bool whole) {
-    const uint8_t* c = m.codes + row * row_bytes + step * (kSpan / 2) + 16 * q;
-    const int64_t g0 = row * groups + step * kScales;
-    if (whole) {
-      __builtin_memcpy(&codes, c, 16);
-      if constexpr (kScale == HOBFLOPS_SCALE_POW2) {
-        uint8_t s[kScales];
-        __builtin_memcpy(s, (const uint8_t*)m.scales + g0, sizeof s);
+// The scales of a row's groups of a unit (256 k), as they are in memory until they are used: a
+// conversion next to the load would wait for it.
+template <int kScale, int kGroup>
+struct Scales {
+  static constexpr int kCount = kUnit / kGroup;
+  static constexpr int kBytes = kScale == HOBFLOPS_SCALE_POW2 ? 1 : kScale == HOBFLOPS_SCALE_BF16 ? 2 : 4;
+  static constexpr int kWords = (kCount * kBytes + 3) / 4;
+  uint32_t word[kWords];
+  int left;  // groups of the row from the first on; those beyond count as zero, their codes meet zeros of x
+  __device__ __forceinline__ void load(const void* scales, int64_t row, int groups, int unit, int64_t N) {
+    const int g0 = unit * kCount;
+    left = groups - g0;
+    const int64_t at = row * groups + g0;
+    const uint8_t* p = (const uint8_t*)scales + at * kBytes;
+    if (at + kCount <= N * groups) {  // beyond a row's end there are the next row's
+      word[kWords - 1] = 0;
+      __builtin_memcpy(word, p, kCount * kBytes);
+    } else {
 #pragma unroll
-        for (int i = 0; i < kScales; ++i) scale[i] = pow2_scale_of(s[i]);
-      } else if constexpr (kScale == HOBFLOPS_SCALE_BF16) {
-        uint16_t s[kScales];
-        __builtin_memcpy(s, (const uint16_t*)m.scales + g0, sizeof s);
+      for (int i = 0; i < kWords; ++i) word[i] = 0;
 #pragma unroll
-        for (int i = 0; i < kScales; ++i) scale[i] = __uint_as_float((uint32_t)s[i] << 16);
-      } else {
-        __builtin_memcpy(scale, (const float*)m.scales + g0, sizeof scale);
-      }
-    } else {  // the end of a row: no byte and no scale beyond it
-      const int64_t first = step * (kSpan / 2) + 16 * q;
-      uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (first + i < row_bytes) w[i >> 2] |= (uint32_t)c[i] << (8 * (i & 3));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) codes[i] = w[i];
-#pragma unroll
-      for (int i = 0; i < kScales; ++i)
-        scale[i] = step * kScales + i < groups ? load_scale(m.scales, g0 + i, kScale) : 0.0f;
+      for (int i = 0; i < kCount; ++i)
+        if (at + i < N * groups) {
+          uint32_t v = 0;
+          __builtin_memcpy(&v, p + i * kBytes, kBytes);
+          word[i * kBytes / 4] |= v << (8 * (i * kBytes & 3));
+        }
     }
   }
-  // word[m]: 8 codes of the step's 32 k from 32 m on
-  __device__ __forceinline__ void words(uint32_t (&word)[4]) const {
-    const auto a = __builtin_amdgcn_permlane32_swap(codes[0], codes[1], false, false);
-    const auto b = __builtin_amdgcn_permlane32_swap(codes[2], codes[3], false, false);
-    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-    const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    word[0] = c[0];
-    word[1] = c[1];
-    word[2] = d[0];
-    word[3] = d[1];
+  // whether the scales can go into the weights (bytes that only fill the last word count as 1)
+  template <class T>
+  __device__ __forceinline__ bool exact() const {
+    bool all = kScale == HOBFLOPS_SCALE_POW2;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+      all = all && exact_scales<T>(kCount < 4 ? word[i] | 0x7F7F0000u : word[i]);
+    return all;
+  }
+  __device__ __forceinline__ float exact_get(int i) const {
+    const int at = i / (kGroup / 32);
+    return __uint_as_float((word[at / 4] >> (8 * (at & 3)) & 255u) << 23);
+  }
+  // of the 32 k from 32 i on
+  __device__ __forceinline__ float get(int i) const {
+    const int g = i / (kGroup / 32), at = g * kBytes;
+    const uint32_t w = word[at / 4] >> (8 * (at & 3));
+    float f = __uint_as_float(w);
+    if constexpr (kScale == HOBFLOPS_SCALE_POW2) f = pow2_scale_of(w & 255u);
+    if constexpr (kScale == HOBFLOPS_SCALE_BF16) f = __uint_as_float(w << 16);
+    return g < left ? f : 0.0f;
   }
 };
 
+// Of the codes of a step that the four lanes of a row hold, 32 each: word[m] is this lane's 8 of those
+// from 32 m on.
+__device__ __forceinline__ void turn_codes(u32x4v codes, uint32_t (&word)[4]) {
+  const auto a = __builtin_amdgcn_permlane32_swap(codes[0], codes[1], false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(codes[2], codes[3], false, false);
+  const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+  const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+  word[0] = c[0];
+  word[1] = c[1];
+  word[2] = d[0];
+  word[3] = d[1];
+}
+
 // 8 values of a token's row from k on; zeros beyond the row's end.
 template <class T>
-__device__ __forceinline__ typename T::vec8 load_x(const typename T::elem* row, int64_t k,
-                                                   int64_t K, bool whole) {
-  typename T::vec8 v;
-  if (whole) {
+__device__ __forceinline__ typename T::vec8 load_x(const typename T::elem* row, int k, int K) {
+  typename T::vec8 v = {};
+  if (k + 8 <= K) {
     __builtin_memcpy(&v, row + k, 16);
-  } else {
+  } else if (k < K) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : (typename T::elem)0.0f;
+    for (int i = 0; i < 7; ++i)
+      if (k + i < K) v[i] = row[k + i];
   }
   return v;
 }
 #endif
 
-// NT: groups of 16 tokens of a workgroup.
-template <class T, int kScale, int kGroup, int NT, bool kGated>
-__global__ __launch_bounds__(512) void w4_kernel(W4Product p) {
 #ifdef __HIP_DEVICE_COMPILE__
-  typedef typename T::elem E;
-  constexpr int kMats = kGated ? 2 : 1, U = NT == 1 ? 2 : 1, kPer = kGroup / 32;
-  extern __shared__ __align__(16) uint8_t lds[];
-  f32x4* sums = (f32x4*)lds;  // [wave][matrix][token group][lane]
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x >> 6;
-  const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
-  const int64_t n = (int64_t)blockIdx.x * 16 + col, t0 = (int64_t)blockIdx.y * (16 * NT);
-  const int64_t row = n < p.N ? n : p.N - 1;
-  const int64_t row_bytes = (p.K + 1) / 2, groups = (p.K + kGroup - 1) / kGroup;
-  const int64_t steps = (p.K + kSpan - 1) / kSpan, per = (steps + waves - 1) / waves;
-  const int64_t first = wave * per, last = first + per < steps ? first + per : steps;
-  f32x4 acc[kMats][NT] = {};
-
-  const auto load_xs = [&](int64_t step, int m, int j, bool whole) {
-    const int64_t t = t0 + 16 * j + col;
-    typename T::vec8 v = {};
-    if (t < p.T) v = load_x<T>((const E*)p.x + t * p.ldx, step * kSpan + 32 * m + 8 * turn, p.K, whole);
-    return v;
-  };
-  const auto run = [&](int64_t step, auto count, bool whole) {
-    constexpr int N = decltype(count)::value;
-    Step<kScale, kGroup> s[N][kMats];
-    typename T::vec8 x[N][4];
+// A unit's products: codes[c] its 16 rows of 128 bytes in LDS, x(i, j) the x of the 32 k from 32 i on
+// of token group j. Scales that are exact powers of two go into the weights, whose products then sum up
+// in place; others multiply the sums of a group.
+template <class T, int kScale, int kGroup, int NT, int kMats, class X>
+__device__ __forceinline__ void multiply_unit(const uint8_t* const (&codes)[kMats],
+                                              const Scales<kScale, kGroup> (&scale)[kMats], int lane,
+                                              X x, f32x4 (&acc)[kMats][NT]) {
+  typedef typename T::vec8 Vec;
+  constexpr int kPer = kGroup / 32;
+  const int col = lane & 15, q = lane >> 4;
+  bool exact = true;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[i][0].load(p.w, row, p.K, row_bytes, groups, step + i, q, whole);
-      if constexpr (kGated) s[i][1].load(p.w_up, row, p.K, row_bytes, groups, step + i, q, whole);
-    }
-    if constexpr (NT == 1) {
+  for (int c = 0; c < kMats; ++c) exact = exact && scale[c].template exact<T>();
+  const bool inside = kScale == HOBFLOPS_SCALE_POW2 && __all(exact);
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+  for (int h = 0; h < 2; ++h) {
+    uint32_t word[kMats][4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) x[i][m] = load_xs(step + i, m, 0, whole);
-    }
+    for (int c = 0; c < kMats; ++c)
+      turn_codes(*(const u32x4v*)(codes[c] + col * 128 + (((4 * h + q) ^ (col >> 1)) << 4)), word[c]);
+    if (inside) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t word[kMats][4];
-#pragma unroll
-      for (int c = 0; c < kMats; ++c) s[i][c].words(word[c]);
-      f32x4 part[kMats][NT];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        typename T::vec8 w[kMats];
-#pragma unroll
-        for (int c = 0; c < kMats; ++c) w[c] = decode8<T>(word[c][m]);
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          const typename T::vec8 v = NT == 1 ? x[i][m] : load_xs(step + i, m, j, whole);
+          const Vec v = x(4 * h + m, j);
+#pragma unroll
+          for (int c = 0; c < kMats; ++c)
+            acc[c][j] = T::mfma(v, decode8<T>(word[c][m], scale[c].exact_get(4 * h + m)), acc[c][j]);
+          if (NT > 1) __builtin_amdgcn_sched_barrier(0);  // else x of all of them takes registers at once
+        }
+    } else {
+      f32x4 sum[kMats][NT];
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const Vec v = x(4 * h + m, j);
 #pragma unroll
           for (int c = 0; c < kMats; ++c) {
             const f32x4 zero = {};
-            part[c][j] = T::mfma(v, w[c], m % kPer == 0 ? zero : part[c][j]);
+            sum[c][j] = T::mfma(v, decode8<T>(word[c][m], 1.0f), m % kPer == 0 ? zero : sum[c][j]);
             if (m % kPer == kPer - 1) {
-              const float f = s[i][c].scale[m / kPer];
+              const float f = scale[c].get(4 * h + m);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[c][j][r] += f * part[c][j][r];
+              for (int r = 0; r < 4; ++r) acc[c][j][r] += f * sum[c][j][r];
             }
           }
+          if (NT > 1) __builtin_amdgcn_sched_barrier(0);
         }
-      }
     }
-  };
-  const int64_t whole = p.K / kSpan < last ? p.K / kSpan : last;  // steps before it are whole
-  int64_t s = first;
-  for (; s + U <= whole; s += U) run(s, std::integral_constant<int, U>(), true);
-  for (; s < whole; ++s) run(s, std::integral_constant<int, 1>(), true);
-  if (s < last) run(s, std::integral_constant<int, 1>(), false);
+  }
+}
 
+// Loads of a tile's codes into LDS: two a unit and matrix. They are written as assembly since the
+// compiler, which knows what a load into LDS is, would wait for all of them before each read of LDS;
+// loaded() is the wait. (M0, the target's place, has no other use here.)
+template <int kMats>
+struct CodeLoads {
+  u32x4v rows[kMats];  // descriptors: address, range, raw 32-bit data
+  uint32_t off[2];
+  __device__ __forceinline__ void start(const W4Product& p, int64_t tile, int row_bytes, int lane) {
+    const int left = (int)(p.N - tile * 16 < 16 ? p.N - tile * 16 : 16);
 #pragma unroll
-  for (int c = 0; c < kMats; ++c)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) sums[((wave * kMats + c) * NT + j) * 64 + lane] = acc[c][j];
-  __syncthreads();
-  for (int j = wave; j < NT; j += waves) {
-    f32x4 y[kMats] = {};
-    for (int w = 0; w < waves; ++w)
-#pragma unroll
-      for (int c = 0; c < kMats; ++c) y[c] += sums[((w * kMats + c) * NT + j) * 64 + lane];
-    if (n < p.N) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t t = t0 + 16 * j + 4 * q + r;
-        if (t >= p.T) continue;
-        const float v = kGated ? gate_act(y[0][r], p.act) * y[kMats - 1][r] : y[0][r];
-        ((E*)p.y)[t * p.ldy + n] = (E)v;
-      }
+    for (int c = 0; c < kMats; ++c) {
+      const uint64_t at = (uint64_t)(uintptr_t)((c ? p.w_up : p.w).codes + tile * 16 * row_bytes);
+      rows[c] = u32x4v{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)(left * row_bytes),
+                       0x00020000u};
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = 8 * i + (lane >> 3);
+      off[i] = (uint32_t)(r * row_bytes + (((lane & 7) ^ (r >> 1)) << 4));
+    }
+  }
+  __device__ __forceinline__ void fetch(int unit, uint8_t* slot) const {
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)slot;
+#pragma unroll
+    for (int c = 0; c < kMats; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :
+                     : "s"(lds + (uint32_t)(c * 2048 + h * 1024)), "v"(off[h] + (uint32_t)unit * 128),
+                       "s"(rows[c])
+                     : "memory");
+  }
+  static __device__ __forceinline__ void loaded() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // no load under way; the compiler counts this one
+    asm volatile("" ::: "memory");
+  }
+};
+
+// Output of 16 rows for 16 tokens: y the sums of a lane's column, its tokens 4 (lane / 16) + 0..3.
+template <class T, int kMats>
+__device__ __forceinline__ void store_tokens(const W4Product& p, int64_t n, int64_t t0, int lane,
+                                             const f32x4 (&y)[kMats]) {
+  if (n >= p.N) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t t = t0 + 4 * (lane >> 4) + r;
+    if (t >= p.T) continue;
+    const float v = kMats > 1 ? gate_act(y[0][r], p.act) * y[kMats - 1][r] : y[0][r];
+    ((typename T::elem*)p.y)[t * p.ldy + n] = (typename T::elem)v;
+  }
+}
+#endif
+
+// A workgroup's eight waves have a part of K each, in units of 256 k (128 bytes of a row: a whole cache
+// line). Codes go into LDS first: loads into it can take 128 bytes of each of 8 rows, where registers
+// would need 64 of 16 (the column of the matrix instruction is the lane), and hold no registers while they
+// are under way.
+//
+// Up to 16 tokens whose x fits LDS: as many workgroups as run at a time, each with the tiles
+// (16 rows) that are a grid apart. x is loaded once; a tile's codes and scales are under way while
+// the tile before is multiplied.
+template <class T, int kScale, int kGroup, bool kGated>
+__global__ __launch_bounds__(512, 2) void w4_stream_kernel(W4Product p, int slots) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef typename T::vec8 Vec;
+  typedef Scales<kScale, kGroup> Sc;
+  constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048;
+  extern __shared__ __align__(1024) uint8_t lds[];  // two sets of sums, two of the waves' units, x
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
+  const int K = (int)p.K, row_bytes = K / 2, groups = (K + kGroup - 1) / kGroup;
+  const int units = (K + kUnit - 1) / kUnit;
+  const int first = units * wave / kWaves, count = units * (wave + 1) / kWaves - first;
+  const int x_row = units * kUnit * 2;  // bytes of a token in LDS
+  const int tokens = (int)p.T;
+  const uint32_t tiles = (uint32_t)((p.N + 15) / 16);
+  constexpr int kSums = kWaves * kMats * 1024;
+  uint8_t* const mine = lds + 2 * kSums + wave * 2 * slots * kSlot;
+  uint8_t* const xs = lds + 2 * kSums + kWaves * 2 * slots * kSlot;
+  const auto fetch = [&](uint32_t tile, int set, Sc(&s)[kStreamUnits][kMats]) {
+    CodeLoads<kMats> loads;
+    loads.start(p, tile, row_bytes, lane);
+    const int64_t n = (int64_t)tile * 16 + col, row = n < p.N ? n : p.N - 1;
+#pragma unroll
+    for (int i = 0; i < kStreamUnits; ++i)
+      if (i < count) {
+        loads.fetch(first + i, mine + (set * slots + i) * kSlot);
+        s[i][0].load(p.w.scales, row, groups, first + i, p.N);
+        if constexpr (kGated) s[i][1].load(p.w_up.scales, row, groups, first + i, p.N);
+      }
+  };
+  Sc now[kStreamUnits][kMats], next[kStreamUnits][kMats];
+  uint32_t tile = blockIdx.x;
+  fetch(tile, 0, now);
+  {
+    const int chunks = x_row / 16;
+    for (int i = threadIdx.x; i < tokens * chunks; i += 64 * kWaves) {
+      const int t = i / chunks, c = i - t * chunks;
+      *(Vec*)(xs + t * x_row + ((c ^ t) << 4)) =
+          load_x<T>((const typename T::elem*)p.x + t * p.ldx, 8 * c, K);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+  const int t = col < tokens ? col : tokens - 1;  // tokens beyond the last are computed and not stored
+  const uint8_t* const x_of = xs + t * x_row;
+  for (int set = 0; tile < tiles; set ^= 1) {
+    CodeLoads<kMats>::loaded();
+    const uint32_t after = tile + gridDim.x;
+    if (after < tiles) fetch(after, set ^ 1, next);
+    f32x4 acc[kMats][1] = {};
+#pragma unroll
+    for (int i = 0; i < kStreamUnits; ++i)
+      if (i < count) {
+        const uint8_t* const s = mine + (set * slots + i) * kSlot;
+        const uint8_t* codes[kMats];
+#pragma unroll
+        for (int c = 0; c < kMats; ++c) codes[c] = s + c * 2048;
+        const int k8 = (first + i) * (kUnit / 8) + turn;
+        multiply_unit<T, kScale, kGroup, 1, kMats>(
+            codes, now[i], lane,
+            [&](int m, int) { return *(const Vec*)(x_of + (((k8 + 4 * m) ^ t) << 4)); }, acc);
+      }
+    // The waves' sums meet in LDS, one wave after the other adds a tile's. The set is written again
+    // two tiles on, after a barrier that this tile's adding wave has reached, too.
+    uint8_t* const sums = lds + set * kSums;
+#pragma unroll
+    for (int c = 0; c < kMats; ++c) *(f32x4*)(sums + ((wave * kMats + c) * 64 + lane) * 16) = acc[c][0];
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (wave == (int)(tile / gridDim.x % kWaves)) {
+      f32x4 y[kMats] = {};
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int c = 0; c < kMats; ++c) y[c] += *(const f32x4*)(sums + ((w * kMats + c) * 64 + lane) * 16);
+      store_tokens<T, kMats>(p, (int64_t)tile * 16 + col, 0, lane, y);
+    }
+#pragma unroll
+    for (int i = 0; i < kStreamUnits; ++i)
+#pragma unroll
+      for (int c = 0; c < kMats; ++c) now[i][c] = next[i][c];
+    tile = after;
   }
 #endif
 }
 
+// More tokens, or an x that does not fit: a workgroup a tile, x from the caches. The codes of up to
+// `ring` units of a wave are under way at a time. NT: groups of 16 tokens.
+template <class T, int kScale, int kGroup, int NT, bool kGated>
+__global__ __launch_bounds__(512, 2) void w4_kernel(W4Product p, int ring) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef typename T::vec8 Vec;
+  typedef Scales<kScale, kGroup> Sc;
+  constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048, A = NT == 1 ? 8 : 1;
+  extern __shared__ __align__(1024) uint8_t lds[];  // each wave's units
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
+  const int64_t n = (int64_t)blockIdx.x * 16 + col, row = n < p.N ? n : p.N - 1;
+  const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
+  const int K = (int)p.K, row_bytes = K / 2, groups = (K + kGroup - 1) / kGroup;
+  const int units = (K + kUnit - 1) / kUnit;
+  const int first = units * wave / kWaves, last = units * (wave + 1) / kWaves;
+  uint8_t* const mine = lds + wave * ring * kSlot;
+  f32x4 acc[kMats][NT] = {};
+  CodeLoads<kMats> loads;
+  loads.start(p, blockIdx.x, row_bytes, lane);
+  const auto get_x = [&](int unit, int i, int j) {
+    const int64_t t = t0 + 16 * j + col;
+    Vec v = {};
+    if (t < p.T)
+      v = load_x<T>((const typename T::elem*)p.x + t * p.ldx, unit * kUnit + 32 * i + 8 * turn, K);
+    return v;
+  };
+  // a unit's scales and, for one group of tokens, its x, a unit ahead
+  const auto ahead = [&](int unit, Sc(&s)[kMats], Vec(&x)[A]) {
+    s[0].load(p.w.scales, row, groups, unit, p.N);
+    if constexpr (kGated) s[1].load(p.w_up.scales, row, groups, unit, p.N);
+    if constexpr (NT == 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = get_x(unit, i, 0);
+    }
+  };
+  const auto multiply = [&](int unit, int slot, const Sc(&s)[kMats], const Vec(&x)[A]) {
+    const uint8_t* codes[kMats];
+#pragma unroll
+    for (int c = 0; c < kMats; ++c) codes[c] = mine + slot * kSlot + c * 2048;
+    multiply_unit<T, kScale, kGroup, NT, kMats>(
+        codes, s, lane, [&](int i, int j) { return NT == 1 ? x[i % A] : get_x(unit, i, j); }, acc);
+  };
+  for (int begin = first; begin < last; begin += ring) {
+    const int end = begin + ring < last ? begin + ring : last;
+    for (int u = begin; u < end; ++u) loads.fetch(u, mine + (u - begin) * kSlot);
+    Sc s0[kMats], s1[kMats];
+    Vec x0[A], x1[A];
+    ahead(begin, s0, x0);
+    CodeLoads<kMats>::loaded();
+    for (int u = begin; u < end; u += 2) {
+      if (u + 1 < end) ahead(u + 1, s1, x1);
+      multiply(u, u - begin, s0, x0);
+      if (u + 1 < end) {
+        if (u + 2 < end) ahead(u + 2, s0, x0);
+        multiply(u + 1, u + 1 - begin, s1, x1);
+      }
+    }
+  }
+  // the waves' sums, each where its codes were
+#pragma unroll
+  for (int c = 0; c < kMats; ++c)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) *(f32x4*)(mine + ((c * NT + j) * 64 + lane) * 16) = acc[c][j];
+  __syncthreads();
+  if (wave < NT) {
+    f32x4 y[kMats] = {};
+    for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+      for (int c = 0; c < kMats; ++c)
+        y[c] += *(const f32x4*)(lds + w * ring * kSlot + ((c * NT + wave) * 64 + lane) * 16);
+    store_tokens<T, kMats>(p, n, t0 + 16 * wave, lane, y);
+  }
+#endif
+}
+
+// Any K and alignment, byte by byte: a wave a row of W and token.
+template <class T>
+__global__ __launch_bounds__(256) void w4_bytes_kernel(W4Product p) {
+  typedef typename T::elem E;
+  const int lane = threadIdx.x & 63;
+  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = blockIdx.y;
+  if (n >= p.N) return;
+  const int64_t groups = (p.K + p.group - 1) / p.group;
+  float sum[2] = {0.0f, 0.0f};
+  for (int w = 0; w < (p.w_up.codes ? 2 : 1); ++w) {
+    const W4Matrix& m = w ? p.w_up : p.w;
+    for (int64_t k = lane; k < p.K; k += 64) {
+      const uint32_t c = m.codes[n * ((p.K + 1) / 2) + k / 2] >> (4 * (k & 1));
+      sum[w] += (float)((const E*)p.x)[t * p.ldx + k] *
+                (decode_e2m1(c) * load_scale(m.scales, n * groups + k / p.group, p.scale));
+    }
+    for (int o = 32; o; o >>= 1) sum[w] += __shfl_xor(sum[w], o);
+  }
+  if (lane == 0)
+    ((E*)p.y)[t * p.ldy + n] = (E)(p.w_up.codes ? gate_act(sum[0], p.act) * sum[1] : sum[0]);
+}
+
 template <class T, int kScale, int kGroup, int NT, bool kGated>
 void launch_tiles(const W4Product& p, hipStream_t stream) {
-  const int waves = 8;
-  const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((p.T + 16 * NT - 1) / (16 * NT)));
+  constexpr int kSlot = kWaves * (kGated ? 2 : 1) * 2048;  // LDS of a unit of all waves
+  const int64_t tiles = (p.N + 15) / 16, parts = (p.T + 16 * NT - 1) / (16 * NT);
+  const int units = (int)((p.K + kUnit - 1) / kUnit), each = (units + kWaves - 1) / kWaves;
+  if constexpr (NT == 1) {
+    const int64_t bytes = kSlot + 2 * each * kSlot + p.T * units * kUnit * 2;
+    if (each <= kStreamUnits && bytes <= kLds) {
+      const int64_t run = kCUs * (bytes <= kLds / 2 ? 2 : 1);
+      w4_stream_kernel<T, kScale, kGroup, kGated>
+          <<<(unsigned)(tiles < run ? tiles : run), 512, (unsigned)bytes, stream>>>(p, each);
+      return;
+    }
+  }
+  // two workgroups a CU where there are enough of them; as many units under way as fit then
+  const int room = (tiles * parts > kCUs ? kLds / 2 : kLds) / kSlot;
+  int ring = room < each ? room : each;
+  if (NT > 1 && ring < NT / 2) ring = NT / 2;  // the sums take the place of the codes
   w4_kernel<T, kScale, kGroup, NT, kGated>
-      <<<grid, 64 * waves, waves * NT * (kGated ? 2 : 1) * 1024, stream>>>(p);
+      <<<dim3((unsigned)tiles, (unsigned)parts), 512, (unsigned)(ring * kSlot), stream>>>(p, ring);
 }
 template <class T, int kScale, int kGroup>
 void launch_tokens(const W4Product& p, hipStream_t stream) {
@@ -234,6 +479,12 @@ void launch_group(const W4Product& p, hipStream_t stream) {
 }
 template <class T>
 void launch_scale(const W4Product& p, hipStream_t stream) {
+  // rows of codes 4-byte aligned, a unit's rows less than 2^31 bytes apart (K is at most 2^24)
+  const bool words = p.K % 8 == 0 && ((uintptr_t)p.w.codes & 3u) == 0 && ((uintptr_t)p.w_up.codes & 3u) == 0;
+  if (!words) {
+    w4_bytes_kernel<T><<<dim3((unsigned)((p.N + 3) / 4), (unsigned)p.T), 256, 0, stream>>>(p);
+    return;
+  }
   if (p.scale == HOBFLOPS_SCALE_POW2) launch_group<T, HOBFLOPS_SCALE_POW2>(p, stream);
   if (p.scale == HOBFLOPS_SCALE_BF16) launch_group<T, HOBFLOPS_SCALE_BF16>(p, stream);
   if (p.scale == HOBFLOPS_SCALE_F32) launch_group<T, HOBFLOPS_SCALE_F32>(p, stream);
@@ -243,7 +494,7 @@ void launch_scale(const W4Product& p, hipStream_t stream) {
 
 hipError_t launch_w4(const W4Product& all, hipStream_t stream) {
   // tokens in parts, for the grid's second axis
-  constexpr int64_t kTokens = (int64_t)1 << 21;
+  constexpr int64_t kTokens = 65520;
   for (int64_t t = 0; t < all.T; t += kTokens) {
     W4Product p = all;
     p.T = all.T - t < kTokens ? all.T - t : kTokens;

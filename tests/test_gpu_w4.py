@@ -139,3 +139,55 @@ def test_arguments():
         hf.w4_linear(x[:, ::2], codes, scales)
     with pytest.raises(hf.HobflopsError):
         hf.w4_linear(x.float(), codes, scales)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T,N,K", [(1, 260, 256), (3, 300, 96), (20, 257, 256), (16, 256, 16640)])
+def test_every_power_of_two(dtype, T, N, K):
+    """Scale bytes from 0 to 255, one a row, mixed within a row and alone: weights picked one by one are
+    the code's value times the scale, rounded to the type once."""
+    hf = need_gpu()
+    rng = np.random.default_rng(9)
+    packed = torch.from_numpy(rng.integers(0, 256, (N, K // 2), dtype=np.uint8)).cuda()
+    groups = K // 32
+    b = np.repeat((np.arange(N) % 256)[:, None], groups, 1)
+    b[:, 1::3] = 127                 # ordinary scales between them
+    b[200:] = np.minimum(b[200:], 254)
+    scales = torch.from_numpy(b.astype(np.uint8)).cuda()
+    f = np.where(b == 255, np.nan, np.exp2(b - 127.0))
+    codes = ref.nibbles(packed.cpu().numpy(), K)
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = ref.unpack(codes, f, (2, 1)).astype(np.float32)
+    for k0 in list(range(0, min(K, 256) - T, max(T, 16))) + [K - T]:
+        x = torch.zeros(T, K, dtype=TYPES[dtype])
+        x[torch.arange(T), k0 + torch.arange(T)] = 1.0
+        y = hf.w4_linear(x.cuda(), packed, scales).cpu()
+        want = torch.from_numpy(w[:, k0:k0 + T].T.copy()).to(TYPES[dtype])
+        nan = torch.from_numpy(np.isnan(f).any(1))  # a NaN scale is its whole row's
+        assert y[:, nan].isnan().all()
+        assert torch.equal(y[:, ~nan], want[:, ~nan])
+
+
+@pytest.mark.parametrize("T,K,N,group,scale", [
+    (1, 4096, 11300, 32, "pow2"), (5, 4104, 9001, 64, "f32"), (16, 1280, 20000, 128, "bf16"),
+    (2, 8192, 5000, 32, "f32"), (16, 11264, 600, 32, "pow2"), (40, 2048, 1500, 64, "bf16")])
+def test_many_tiles(T, K, N, group, scale):
+    """Sizes at which a workgroup takes several tiles, or a wave several rounds."""
+    hf = need_gpu()
+    say("w4 many tiles", T, K, N, group, scale)
+    for dtype in TYPES:
+        cg, sg, wg = _weights(hf, N, K, group, scale, 11)
+        cu, su, wu = _weights(hf, N, K, group, scale, 12)
+        xt = _x(T, K, dtype, 13)
+        x = xt.double()
+        wg, wu = torch.from_numpy(wg).cuda(), torch.from_numpy(wu).cuda()
+        g, u = x @ wg.T, x @ wu.T
+        eg, eu = ((K + 4) * EPS * (x.abs() @ w.abs().T) for w in (wg, wu))
+        y = hf.w4_linear(xt, cg, sg, group=group).double()
+        assert ((y - g).abs() <= eg + UNIT[dtype] * g.abs() + TINY[dtype]).all()
+        s = torch.sigmoid(g)
+        h = hf.w4_gated(xt, cg, sg, cu, su, 0, group=group).double()
+        e = (1.13 * eg + ACT * g.abs()) * (u.abs() + eu) + (g * s).abs() * eu
+        want = g * s * u
+        assert ((h - want).abs() <= e + UNIT[dtype] * want.abs() + TINY[dtype]).all()
+        assert torch.equal(hf.w4_linear(xt, cg, sg, group=group).double(), y)
