@@ -26,8 +26,8 @@ namespace hobflops {
 namespace {
 
 constexpr int kUnit = 256;   // k of a unit: two times 32 of each of the four lanes of a row
-constexpr int kWaves = 8;    // of a workgroup
-constexpr int kStreamUnits = 4;  // of a wave, at most, in the streaming kernel: their scales are in registers
+constexpr int kWaves = 8;    // of a workgroup of w4_kernel
+constexpr int kStreamUnits = 2;  // of a wave, at most, in the streaming kernel: their scales are in registers
 constexpr int kCUs = 256;
 constexpr int kLds = 160 * 1024;
 
@@ -128,29 +128,16 @@ __device__ __forceinline__ void turn_codes(u32x4v codes, uint32_t (&word)[4]) {
   word[3] = d[1];
 }
 
-// 8 values of a token's row from k on; zeros beyond the row's end.
-template <class T>
-__device__ __forceinline__ typename T::vec8 load_x(const typename T::elem* row, int k, int K) {
-  typename T::vec8 v = {};
-  if (k + 8 <= K) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else if (k < K) {
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-      if (k + i < K) v[i] = row[k + i];
-  }
-  return v;
-}
 #endif
 
 #ifdef __HIP_DEVICE_COMPILE__
-// A unit's products: codes[c] its 16 rows of 128 bytes in LDS, x(i, j) the x of the 32 k from 32 i on
-// of token group j. Scales that are exact powers of two go into the weights, whose products then sum up
-// in place; others multiply the sums of a group.
-template <class T, int kScale, int kGroup, int NT, int kMats, class X>
+// A unit's products: codes[c] its 16 rows of 128 bytes in LDS, x(i) the x of the 32 k from 32 i on.
+// Scales that are exact powers of two go into the weights, whose products then sum up in place; others
+// multiply the sums of a group.
+template <class T, int kScale, int kGroup, int kMats, class X>
 __device__ __forceinline__ void multiply_unit(const uint8_t* const (&codes)[kMats],
                                               const Scales<kScale, kGroup> (&scale)[kMats], int lane,
-                                              X x, f32x4 (&acc)[kMats][NT]) {
+                                              X x, f32x4 (&acc)[kMats]) {
   typedef typename T::vec8 Vec;
   constexpr int kPer = kGroup / 32;
   const int col = lane & 15, q = lane >> 4;
@@ -166,74 +153,99 @@ __device__ __forceinline__ void multiply_unit(const uint8_t* const (&codes)[kMat
       turn_codes(*(const u32x4v*)(codes[c] + col * 128 + (((4 * h + q) ^ (col >> 1)) << 4)), word[c]);
     if (inside) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
+      for (int m = 0; m < 4; ++m) {
+        const Vec v = x(4 * h + m);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const Vec v = x(4 * h + m, j);
-#pragma unroll
-          for (int c = 0; c < kMats; ++c)
-            acc[c][j] = T::mfma(v, decode8<T>(word[c][m], scale[c].exact_get(4 * h + m)), acc[c][j]);
-          if (NT > 1) __builtin_amdgcn_sched_barrier(0);  // else x of all of them takes registers at once
-        }
+        for (int c = 0; c < kMats; ++c)
+          acc[c] = T::mfma(v, decode8<T>(word[c][m], scale[c].exact_get(4 * h + m)), acc[c]);
+      }
     } else {
-      f32x4 sum[kMats][NT];
+      f32x4 sum[kMats];
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
+      for (int m = 0; m < 4; ++m) {
+        const Vec v = x(4 * h + m);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const Vec v = x(4 * h + m, j);
+        for (int c = 0; c < kMats; ++c) {
+          const f32x4 zero = {};
+          sum[c] = T::mfma(v, decode8<T>(word[c][m], 1.0f), m % kPer == 0 ? zero : sum[c]);
+          if (m % kPer == kPer - 1) {
+            const float f = scale[c].get(4 * h + m);
 #pragma unroll
-          for (int c = 0; c < kMats; ++c) {
-            const f32x4 zero = {};
-            sum[c][j] = T::mfma(v, decode8<T>(word[c][m], 1.0f), m % kPer == 0 ? zero : sum[c][j]);
-            if (m % kPer == kPer - 1) {
-              const float f = scale[c].get(4 * h + m);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) acc[c][j][r] += f * sum[c][j][r];
-            }
+            for (int r = 0; r < 4; ++r) acc[c][r] += f * sum[c][r];
           }
-          if (NT > 1) __builtin_amdgcn_sched_barrier(0);
         }
+      }
     }
   }
 }
 
-// Loads of a tile's codes into LDS: two a unit and matrix. They are written as assembly since the
-// compiler, which knows what a load into LDS is, would wait for all of them before each read of LDS;
-// loaded() is the wait. (M0, the target's place, has no other use here.)
+// A load into LDS, 16 bytes a lane, at `lds` on; zeros from offsets out of the descriptor's range. These are
+// assembly since the compiler, which knows what a load into LDS is, would wait for all of them
+// before each read of LDS; loaded() is the wait. (M0, the target's place, has no other use here.)
+__device__ __forceinline__ void load_lds(u32x4v rows, uint32_t off, const uint8_t* to) {
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(off), "s"(rows)
+               : "memory");
+}
+__device__ __forceinline__ void loaded() {
+  __builtin_amdgcn_s_waitcnt(0x0070);  // no load and no LDS read under way; the compiler counts this one
+  asm volatile("" ::: "memory");
+}
+// Before a load into LDS that was just read.
+__device__ __forceinline__ void reads_done() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
+// The descriptor of `bytes` of raw 32-bit data.
+__device__ __forceinline__ u32x4v raw_rows(const void* p, uint32_t bytes) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  return u32x4v{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+}
+
+// Loads of a tile's codes: 16 rows of 128 bytes a unit and matrix. The 16-byte chunks of a row stand at a
+// place XORed with bits of the row's number, so that a read of 16 rows falls on different banks.
 template <int kMats>
 struct CodeLoads {
-  u32x4v rows[kMats];  // descriptors: address, range, raw 32-bit data
+  u32x4v rows[kMats];
   uint32_t off[2];
   __device__ __forceinline__ void start(const W4Product& p, int64_t tile, int row_bytes, int lane) {
     const int left = (int)(p.N - tile * 16 < 16 ? p.N - tile * 16 : 16);
 #pragma unroll
-    for (int c = 0; c < kMats; ++c) {
-      const uint64_t at = (uint64_t)(uintptr_t)((c ? p.w_up : p.w).codes + tile * 16 * row_bytes);
-      rows[c] = u32x4v{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)(left * row_bytes),
-                       0x00020000u};
-    }
+    for (int c = 0; c < kMats; ++c)
+      rows[c] = raw_rows((c ? p.w_up : p.w).codes + tile * 16 * row_bytes, (uint32_t)(left * row_bytes));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = 8 * i + (lane >> 3);
       off[i] = (uint32_t)(r * row_bytes + (((lane & 7) ^ (r >> 1)) << 4));
     }
   }
-  __device__ __forceinline__ void fetch(int unit, uint8_t* slot) const {
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)slot;
+  __device__ __forceinline__ void fetch(int unit, const uint8_t* slot) const {
 #pragma unroll
     for (int c = 0; c < kMats; ++c)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     :
-                     : "s"(lds + (uint32_t)(c * 2048 + h * 1024)), "v"(off[h] + (uint32_t)unit * 128),
-                       "s"(rows[c])
-                     : "memory");
+        load_lds(rows[c], off[h] + (uint32_t)unit * 128, slot + c * 2048 + h * 1024);
   }
-  static __device__ __forceinline__ void loaded() {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // no load under way; the compiler counts this one
-    asm volatile("" ::: "memory");
+};
+
+// Loads of x, a unit (512 bytes) of two tokens at a time, the chunks' places XORed with the token's number.
+struct XLoads {
+  u32x4v rows;
+  uint32_t ld2;
+  int tokens, K;
+  __device__ __forceinline__ void start(const W4Product& p, int64_t t0) {
+    tokens = (int)(p.T - t0 < 16 ? p.T - t0 : 16);
+    K = (int)p.K;
+    ld2 = (uint32_t)(p.ldx * 2);
+    rows = raw_rows((const uint8_t*)p.x + t0 * p.ldx * 2, (uint32_t)(tokens - 1) * ld2 + (uint32_t)K * 2);
+  }
+  __device__ __forceinline__ void fetch(int token, int unit, int lane, const uint8_t* to) const {
+    const int k = unit * kUnit + ((lane & 31) ^ (token & 15)) * 8;
+    const bool in = token < tokens && k < K;
+    load_lds(rows, in ? (uint32_t)token * ld2 + (uint32_t)k * 2 : 0x80000000u, to);
   }
 };
 
@@ -252,32 +264,38 @@ __device__ __forceinline__ void store_tokens(const W4Product& p, int64_t n, int6
 }
 #endif
 
-// A workgroup's eight waves have a part of K each, in units of 256 k (128 bytes of a row: a whole cache
-// line). Codes go into LDS first: loads into it can take 128 bytes of each of 8 rows, where registers
+// A workgroup's waves have a part of K each, in units of 256 k (128 bytes of a row: a whole cache
+// line). Codes and x go into LDS first: loads into it can take 128 bytes of each of 8 rows, where registers
 // would need 64 of 16 (the column of the matrix instruction is the lane), and hold no registers while they
-// are under way.
-//
-// Up to 16 tokens whose x fits LDS: as many workgroups as run at a time, each with the tiles
-// (16 rows) that are a grid apart. x is loaded once; a tile's codes and scales are under way while
-// the tile before is multiplied.
+// are under way. A workgroup has up to 16 tokens, those of neighbouring numbers the same tiles' other tokens.
+
+// The part of K of a wave.
+__device__ __forceinline__ int part_of(int units, int wave, int waves) { return units * wave / waves; }
+
+// x of all K fits LDS: as many workgroups as run at a time, each with the tiles (16 rows) that are
+// `stride` apart. x is loaded once; a tile's codes and scales are under way while the tile before is
+// multiplied.
 template <class T, int kScale, int kGroup, bool kGated>
-__global__ __launch_bounds__(512, 2) void w4_stream_kernel(W4Product p, int slots) {
+__global__ __launch_bounds__(1024) void w4_stream_kernel(W4Product p, int parts, int stride) {
 #ifdef __HIP_DEVICE_COMPILE__
   typedef typename T::vec8 Vec;
   typedef Scales<kScale, kGroup> Sc;
   constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048;
-  extern __shared__ __align__(1024) uint8_t lds[];  // two sets of sums, two of the waves' units, x
+  extern __shared__ __align__(1024) uint8_t lds[];  // two sets of sums, two of the units, x
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6;
   const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
   const int K = (int)p.K, row_bytes = K / 2, groups = (K + kGroup - 1) / kGroup;
   const int units = (K + kUnit - 1) / kUnit;
-  const int first = units * wave / kWaves, count = units * (wave + 1) / kWaves - first;
-  const int x_row = units * kUnit * 2;  // bytes of a token in LDS
-  const int tokens = (int)p.T;
+  const int first = part_of(units, wave, waves), count = part_of(units, wave + 1, waves) - first;
+  const int64_t t0 = (int64_t)(blockIdx.x % parts) * 16;
+  XLoads x;
+  x.start(p, t0);
+  const int tokens = x.tokens, lanes = (tokens + 3) / 4 * 16;  // that hold sums of tokens
+  const int sum_bytes = waves * kMats * lanes * 16;
+  uint8_t* const sums0 = lds + 2 * units * kSlot;
+  uint8_t* const xs = sums0 + 2 * sum_bytes;
   const uint32_t tiles = (uint32_t)((p.N + 15) / 16);
-  constexpr int kSums = kWaves * kMats * 1024;
-  uint8_t* const mine = lds + 2 * kSums + wave * 2 * slots * kSlot;
-  uint8_t* const xs = lds + 2 * kSums + kWaves * 2 * slots * kSlot;
   const auto fetch = [&](uint32_t tile, int set, Sc(&s)[kStreamUnits][kMats]) {
     CodeLoads<kMats> loads;
     loads.start(p, tile, row_bytes, lane);
@@ -285,54 +303,53 @@ __global__ __launch_bounds__(512, 2) void w4_stream_kernel(W4Product p, int slot
 #pragma unroll
     for (int i = 0; i < kStreamUnits; ++i)
       if (i < count) {
-        loads.fetch(first + i, mine + (set * slots + i) * kSlot);
+        loads.fetch(first + i, lds + (set * units + first + i) * kSlot);
         s[i][0].load(p.w.scales, row, groups, first + i, p.N);
         if constexpr (kGated) s[i][1].load(p.w_up.scales, row, groups, first + i, p.N);
       }
   };
   Sc now[kStreamUnits][kMats], next[kStreamUnits][kMats];
-  uint32_t tile = blockIdx.x;
+  uint32_t tile = blockIdx.x / parts;
   fetch(tile, 0, now);
-  {
-    const int chunks = x_row / 16;
-    for (int i = threadIdx.x; i < tokens * chunks; i += 64 * kWaves) {
-      const int t = i / chunks, c = i - t * chunks;
-      *(Vec*)(xs + t * x_row + ((c ^ t) << 4)) =
-          load_x<T>((const typename T::elem*)p.x + t * p.ldx, 8 * c, K);
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  for (int i = 2 * wave; i < tokens * units; i += 2 * waves) {
+    const int pair = i + (lane >> 5);
+    x.fetch(pair / units, pair % units, lane, xs + i * 512);
   }
+  loaded();
+  __syncthreads();
   const int t = col < tokens ? col : tokens - 1;  // tokens beyond the last are computed and not stored
-  const uint8_t* const x_of = xs + t * x_row;
-  for (int set = 0; tile < tiles; set ^= 1) {
-    CodeLoads<kMats>::loaded();
-    const uint32_t after = tile + gridDim.x;
+  const uint8_t* const x_of = xs + t * units * 512;
+  for (int n = 0; tile < tiles; ++n) {
+    const int set = n & 1;
+    loaded();
+    const uint32_t after = tile + stride;
     if (after < tiles) fetch(after, set ^ 1, next);
-    f32x4 acc[kMats][1] = {};
+    f32x4 acc[kMats] = {};
 #pragma unroll
     for (int i = 0; i < kStreamUnits; ++i)
       if (i < count) {
-        const uint8_t* const s = mine + (set * slots + i) * kSlot;
+        const uint8_t* const s = lds + (set * units + first + i) * kSlot;
         const uint8_t* codes[kMats];
 #pragma unroll
         for (int c = 0; c < kMats; ++c) codes[c] = s + c * 2048;
         const int k8 = (first + i) * (kUnit / 8) + turn;
-        multiply_unit<T, kScale, kGroup, 1, kMats>(
-            codes, now[i], lane,
-            [&](int m, int) { return *(const Vec*)(x_of + (((k8 + 4 * m) ^ t) << 4)); }, acc);
+        multiply_unit<T, kScale, kGroup, kMats>(
+            codes, now[i], lane, [&](int m) { return *(const Vec*)(x_of + (((k8 + 4 * m) ^ t) << 4)); }, acc);
       }
     // The waves' sums meet in LDS, one wave after the other adds a tile's. The set is written again
     // two tiles on, after a barrier that this tile's adding wave has reached, too.
-    uint8_t* const sums = lds + set * kSums;
+    uint8_t* const sums = sums0 + set * sum_bytes;
+    if (lane < lanes) {
 #pragma unroll
-    for (int c = 0; c < kMats; ++c) *(f32x4*)(sums + ((wave * kMats + c) * 64 + lane) * 16) = acc[c][0];
+      for (int c = 0; c < kMats; ++c) *(f32x4*)(sums + ((wave * kMats + c) * lanes + lane) * 16) = acc[c];
+    }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (wave == (int)(tile / gridDim.x % kWaves)) {
+    if (wave == n % waves && lane < lanes) {
       f32x4 y[kMats] = {};
-      for (int w = 0; w < kWaves; ++w)
+      for (int w = 0; w < waves; ++w)
 #pragma unroll
-        for (int c = 0; c < kMats; ++c) y[c] += *(const f32x4*)(sums + ((w * kMats + c) * 64 + lane) * 16);
-      store_tokens<T, kMats>(p, (int64_t)tile * 16 + col, 0, lane, y);
+        for (int c = 0; c < kMats; ++c) y[c] += *(const f32x4*)(sums + ((w * kMats + c) * lanes + lane) * 16);
+      store_tokens<T, kMats>(p, (int64_t)tile * 16 + col, t0, lane, y);
     }
 #pragma unroll
     for (int i = 0; i < kStreamUnits; ++i)
@@ -343,78 +360,74 @@ __global__ __launch_bounds__(512, 2) void w4_stream_kernel(W4Product p, int slot
 #endif
 }
 
-// More tokens, or an x that does not fit: a workgroup a tile, x from the caches. The codes of up to
-// `ring` units of a wave are under way at a time. NT: groups of 16 tokens.
-template <class T, int kScale, int kGroup, int NT, bool kGated>
-__global__ __launch_bounds__(512, 2) void w4_kernel(W4Product p, int ring) {
+// An x that does not fit: a workgroup of eight waves a tile. The codes of up to `ring` units of a wave are
+// under way at a time; x comes a unit at a time, a unit ahead where LDS has two places for it.
+template <class T, int kScale, int kGroup, bool kGated>
+__global__ __launch_bounds__(512) void w4_kernel(W4Product p, int parts, int ring, int places) {
 #ifdef __HIP_DEVICE_COMPILE__
   typedef typename T::vec8 Vec;
   typedef Scales<kScale, kGroup> Sc;
-  constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048, A = NT == 1 ? 8 : 1;
-  extern __shared__ __align__(1024) uint8_t lds[];  // each wave's units
+  constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048;
+  extern __shared__ __align__(1024) uint8_t lds[];  // of each wave: its units' codes, x
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
-  const int64_t n = (int64_t)blockIdx.x * 16 + col, row = n < p.N ? n : p.N - 1;
-  const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
+  const uint32_t tile = blockIdx.x / parts;
+  const int64_t t0 = (int64_t)(blockIdx.x % parts) * 16;
+  const int64_t n = (int64_t)tile * 16 + col, row = n < p.N ? n : p.N - 1;
   const int K = (int)p.K, row_bytes = K / 2, groups = (K + kGroup - 1) / kGroup;
   const int units = (K + kUnit - 1) / kUnit;
-  const int first = units * wave / kWaves, last = units * (wave + 1) / kWaves;
-  uint8_t* const mine = lds + wave * ring * kSlot;
-  f32x4 acc[kMats][NT] = {};
+  const int first = part_of(units, wave, kWaves), last = part_of(units, wave + 1, kWaves);
+  XLoads x;
+  x.start(p, t0);
+  const int pairs = (x.tokens + 1) / 2, each = ring * kSlot + places * pairs * 1024;
+  uint8_t* const mine = lds + wave * each;
+  uint8_t* const xs = mine + ring * kSlot;
   CodeLoads<kMats> loads;
-  loads.start(p, blockIdx.x, row_bytes, lane);
-  const auto get_x = [&](int unit, int i, int j) {
-    const int64_t t = t0 + 16 * j + col;
-    Vec v = {};
-    if (t < p.T)
-      v = load_x<T>((const typename T::elem*)p.x + t * p.ldx, unit * kUnit + 32 * i + 8 * turn, K);
-    return v;
-  };
-  // a unit's scales and, for one group of tokens, its x, a unit ahead
-  const auto ahead = [&](int unit, Sc(&s)[kMats], Vec(&x)[A]) {
+  loads.start(p, tile, row_bytes, lane);
+  const int t = col < x.tokens ? col : x.tokens - 1;  // tokens beyond the last are not stored
+  const auto ahead = [&](int unit, Sc(&s)[kMats]) {
+    for (int i = 0; i < pairs; ++i)
+      x.fetch(2 * i + (lane >> 5), unit, lane, xs + ((unit % places) * pairs + i) * 1024);
     s[0].load(p.w.scales, row, groups, unit, p.N);
     if constexpr (kGated) s[1].load(p.w_up.scales, row, groups, unit, p.N);
-    if constexpr (NT == 1) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = get_x(unit, i, 0);
-    }
   };
-  const auto multiply = [&](int unit, int slot, const Sc(&s)[kMats], const Vec(&x)[A]) {
+  f32x4 acc[kMats] = {};
+  const auto multiply = [&](int unit, int slot, const Sc(&s)[kMats]) {
     const uint8_t* codes[kMats];
 #pragma unroll
     for (int c = 0; c < kMats; ++c) codes[c] = mine + slot * kSlot + c * 2048;
-    multiply_unit<T, kScale, kGroup, NT, kMats>(
-        codes, s, lane, [&](int i, int j) { return NT == 1 ? x[i % A] : get_x(unit, i, j); }, acc);
+    const uint8_t* const x_of = xs + (unit % places) * pairs * 1024 + t * 512;
+    multiply_unit<T, kScale, kGroup, kMats>(
+        codes, s, lane, [&](int m) { return *(const Vec*)(x_of + (((4 * m + turn) ^ t) << 4)); }, acc);
   };
   for (int begin = first; begin < last; begin += ring) {
     const int end = begin + ring < last ? begin + ring : last;
+    reads_done();
     for (int u = begin; u < end; ++u) loads.fetch(u, mine + (u - begin) * kSlot);
-    Sc s0[kMats], s1[kMats];
-    Vec x0[A], x1[A];
-    ahead(begin, s0, x0);
-    CodeLoads<kMats>::loaded();
-    for (int u = begin; u < end; u += 2) {
-      if (u + 1 < end) ahead(u + 1, s1, x1);
-      multiply(u, u - begin, s0, x0);
-      if (u + 1 < end) {
-        if (u + 2 < end) ahead(u + 2, s0, x0);
-        multiply(u + 1, u + 1 - begin, s1, x1);
+    Sc now[kMats], next[kMats];
+    ahead(begin, now);
+    for (int u = begin; u < end; ++u) {
+      loaded();
+      if (places > 1 && u + 1 < end) ahead(u + 1, next);
+      multiply(u, u - begin, now);
+      if (places == 1 && u + 1 < end) {
+        reads_done();
+        ahead(u + 1, next);
       }
+#pragma unroll
+      for (int c = 0; c < kMats; ++c) now[c] = next[c];
     }
   }
   // the waves' sums, each where its codes were
 #pragma unroll
-  for (int c = 0; c < kMats; ++c)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) *(f32x4*)(mine + ((c * NT + j) * 64 + lane) * 16) = acc[c][j];
+  for (int c = 0; c < kMats; ++c) *(f32x4*)(mine + (c * 64 + lane) * 16) = acc[c];
   __syncthreads();
-  if (wave < NT) {
+  if (wave == 0) {
     f32x4 y[kMats] = {};
     for (int w = 0; w < kWaves; ++w)
 #pragma unroll
-      for (int c = 0; c < kMats; ++c)
-        y[c] += *(const f32x4*)(lds + w * ring * kSlot + ((c * NT + wave) * 64 + lane) * 16);
-    store_tokens<T, kMats>(p, n, t0 + 16 * wave, lane, y);
+      for (int c = 0; c < kMats; ++c) y[c] += *(const f32x4*)(lds + w * each + (c * 64 + lane) * 16);
+    store_tokens<T, kMats>(p, n, t0, lane, y);
   }
 #endif
 }
@@ -441,46 +454,54 @@ __global__ __launch_bounds__(256) void w4_bytes_kernel(W4Product p) {
     ((E*)p.y)[t * p.ldy + n] = (E)(p.w_up.codes ? gate_act(sum[0], p.act) * sum[1] : sum[0]);
 }
 
-template <class T, int kScale, int kGroup, int NT, bool kGated>
+template <class T, int kScale, int kGroup, bool kGated>
 void launch_tiles(const W4Product& p, hipStream_t stream) {
-  constexpr int kSlot = kWaves * (kGated ? 2 : 1) * 2048;  // LDS of a unit of all waves
-  const int64_t tiles = (p.N + 15) / 16, parts = (p.T + 16 * NT - 1) / (16 * NT);
-  const int units = (int)((p.K + kUnit - 1) / kUnit), each = (units + kWaves - 1) / kWaves;
-  if constexpr (NT == 1) {
-    const int64_t bytes = kSlot + 2 * each * kSlot + p.T * units * kUnit * 2;
+  constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048;  // LDS of a unit
+  const int64_t tiles = (p.N + 15) / 16, parts = (p.T + 15) / 16;
+  const int units = (int)((p.K + kUnit - 1) / kUnit), tokens = (int)(p.T < 16 ? p.T : 16);
+  {
+    // the fewest units a wave that 16 waves make possible, and as few waves as that needs
+    const int each = (units + 15) / 16, waves = (units + each - 1) / each;
+    const int64_t bytes = (int64_t)2 * units * kSlot + 2 * waves * kMats * ((tokens + 3) / 4) * 256 +
+                          ((int64_t)tokens * units + 1) * 512;
     if (each <= kStreamUnits && bytes <= kLds) {
-      const int64_t run = kCUs * (bytes <= kLds / 2 ? 2 : 1);
+      const int64_t run = kCUs * (bytes <= kLds / 2 && waves <= 8 ? 2 : 1);  // workgroups at a time
+      int64_t stride = run / parts < 1 ? 1 : run / parts;
+      if (stride > tiles) stride = tiles;
       w4_stream_kernel<T, kScale, kGroup, kGated>
-          <<<(unsigned)(tiles < run ? tiles : run), 512, (unsigned)bytes, stream>>>(p, each);
+          <<<(unsigned)(stride * parts), 64 * waves, (unsigned)bytes, stream>>>(p, (int)parts, (int)stride);
       return;
     }
   }
-  // two workgroups a CU where there are enough of them; as many units under way as fit then
-  const int room = (tiles * parts > kCUs ? kLds / 2 : kLds) / kSlot;
-  int ring = room < each ? room : each;
-  if (NT > 1 && ring < NT / 2) ring = NT / 2;  // the sums take the place of the codes
-  w4_kernel<T, kScale, kGroup, NT, kGated>
-      <<<dim3((unsigned)tiles, (unsigned)parts), 512, (unsigned)(ring * kSlot), stream>>>(p, ring);
+  const int each = (units + kWaves - 1) / kWaves, x = (tokens + 1) / 2 * 1024;
+  // As many units under way as fit, and a second place for x only beside all of them. Two workgroups a
+  // CU where there are enough of them and half of LDS still has three units, or all.
+  const int half = kLds / 2 / kWaves, some = each < 3 ? each : 3;
+  const int wave = tiles * parts > kCUs && (half - x) / kSlot >= some ? half : kLds / kWaves;
+  const int places = (wave - 2 * x) / kSlot >= each ? 2 : 1;
+  int ring = (wave - places * x) / kSlot;
+  if (ring > each) ring = each;
+  w4_kernel<T, kScale, kGroup, kGated>
+      <<<(unsigned)(tiles * parts), 64 * kWaves, (unsigned)(kWaves * (ring * kSlot + places * x)), stream>>>(
+          p, (int)parts, ring, places);
 }
 template <class T, int kScale, int kGroup>
-void launch_tokens(const W4Product& p, hipStream_t stream) {
-  if (p.w_up.codes)
-    p.T <= 16 ? launch_tiles<T, kScale, kGroup, 1, true>(p, stream)
-              : launch_tiles<T, kScale, kGroup, 4, true>(p, stream);
-  else
-    p.T <= 16 ? launch_tiles<T, kScale, kGroup, 1, false>(p, stream)
-              : launch_tiles<T, kScale, kGroup, 4, false>(p, stream);
+void launch_mats(const W4Product& p, hipStream_t stream) {
+  p.w_up.codes ? launch_tiles<T, kScale, kGroup, true>(p, stream)
+               : launch_tiles<T, kScale, kGroup, false>(p, stream);
 }
 template <class T, int kScale>
 void launch_group(const W4Product& p, hipStream_t stream) {
-  if (p.group == 32) launch_tokens<T, kScale, 32>(p, stream);
-  if (p.group == 64) launch_tokens<T, kScale, 64>(p, stream);
-  if (p.group == 128) launch_tokens<T, kScale, 128>(p, stream);
+  if (p.group == 32) launch_mats<T, kScale, 32>(p, stream);
+  if (p.group == 64) launch_mats<T, kScale, 64>(p, stream);
+  if (p.group == 128) launch_mats<T, kScale, 128>(p, stream);
 }
 template <class T>
 void launch_scale(const W4Product& p, hipStream_t stream) {
-  // rows of codes 4-byte aligned, a unit's rows less than 2^31 bytes apart (K is at most 2^24)
-  const bool words = p.K % 8 == 0 && ((uintptr_t)p.w.codes & 3u) == 0 && ((uintptr_t)p.w_up.codes & 3u) == 0;
+  // rows of codes and of x 4-byte aligned, 16 of x less than 2^31 bytes apart (of codes they are, K is at
+  // most 2^24); fewer than 2^31 workgroups
+  const bool words = p.K % 8 == 0 && ((uintptr_t)p.w.codes & 3u) == 0 && ((uintptr_t)p.w_up.codes & 3u) == 0 &&
+                     ((uintptr_t)p.x & 3u) == 0 && p.ldx % 2 == 0 && p.ldx < (int64_t)1 << 26;
   if (!words) {
     w4_bytes_kernel<T><<<dim3((unsigned)((p.N + 3) / 4), (unsigned)p.T), 256, 0, stream>>>(p);
     return;
@@ -494,7 +515,7 @@ void launch_scale(const W4Product& p, hipStream_t stream) {
 
 hipError_t launch_w4(const W4Product& all, hipStream_t stream) {
   // tokens in parts, for the grid's second axis
-  constexpr int64_t kTokens = 65520;
+  constexpr int64_t kTokens = 4096;
   for (int64_t t = 0; t < all.T; t += kTokens) {
     W4Product p = all;
     p.T = all.T - t < kTokens ? all.T - t : kTokens;
