@@ -26,15 +26,15 @@ struct BlockParams {
   void* scales;
   int64_t rows, cols, ld, row_bytes;  // row_bytes: codes of a row
   int64_t chunks;                     // threads a row: whole groups
-  int group_log, scale, vec;          // vec: whole chunks move in 16-byte accesses
+  int group_log, scale;
 };
 
 template <class T>
 __device__ __forceinline__ void load8(const BlockParams& p, int64_t row, int64_t col, float (&v)[8]) {
   const typename T::elem* src = (const typename T::elem*)p.values + row * p.ld + col;
-  if (p.vec && col + kPer <= p.cols) {
+  if (col + kPer <= p.cols) {  // 16 bytes at a time whatever the alignment
     typename T::elem e[8];
-    __builtin_memcpy(e, __builtin_assume_aligned(src, 16), sizeof e);
+    __builtin_memcpy(e, src, sizeof e);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)e[i];
   } else {
@@ -159,11 +159,11 @@ __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
     }
   }
   typename T::elem* dst = (typename T::elem*)p.values + row * p.ld + col;
-  if (p.vec && whole) {
+  if (whole) {
     typename T::elem e[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) e[j] = round_product<T>(v[j], s);
-    __builtin_memcpy(__builtin_assume_aligned(dst, 16), e, sizeof e);
+    __builtin_memcpy(dst, e, sizeof e);
   } else {
     for (int j = 0; j < 8 && col + j < p.cols; ++j) dst[j] = round_product<T>(v[j], s);
   }
@@ -208,8 +208,6 @@ hipError_t run(const BlockTensor& t, int fmt, bool pack, hipStream_t stream) {
   p.group_log = t.group == 32 ? 5 : t.group == 64 ? 6 : 7;
   p.chunks = (t.cols + t.group - 1) / t.group * (t.group / kPer);
   p.scale = t.scale;
-  const int64_t bytes = t.type == HOBFLOPS_TYPE_F32 ? 4 : 2;
-  p.vec = ((uintptr_t)t.values & 15u) == 0 && t.ld * bytes % 16 == 0;
   if (t.type == HOBFLOPS_TYPE_F32) launch_fmt<TypeF32>(p, fmt, pack, stream);
   if (t.type == HOBFLOPS_TYPE_BF16) launch_fmt<TypeBF16>(p, fmt, pack, stream);
   if (t.type == HOBFLOPS_TYPE_F16) launch_fmt<TypeF16>(p, fmt, pack, stream);

@@ -15,32 +15,47 @@
 namespace hobflops {
 namespace {
 
+constexpr int64_t kCUs = 256;
+
 // ---- the products ------------------------------------------------------------
 
-// Rows of an operand as the products need them: 16-byte aligned, zeros from cols up to ldd.
+// Rows of operands as the products need them: 16-byte aligned, zeros from cols up to ldd. Up to three
+// tensors of one width in a launch. (Whole chunks are read 16 bytes at a time whatever their alignment.)
+struct AlignArgs {
+  const void* src[3];
+  void* dst[3];
+  int64_t ld[3], rows[3];  // rows: of this tensor and those before
+  int64_t cols, ldd;
+};
 template <class T>
-__global__ __launch_bounds__(256) void align_kernel(const void* src, int64_t ld, int64_t rows,
-                                                    int64_t cols, void* dst, int64_t ldd) {
+__global__ __launch_bounds__(256) void align_kernel(AlignArgs p) {
   typedef typename T::elem E;
-  const int64_t per = ldd / 8, n = rows * per;
+  const int64_t per = p.ldd / 8, n = p.rows[2] * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / per, col = (i - row * per) * 8;
-    const E* s = (const E*)src + row * ld;
-    typename T::vec8 v;
+    const int64_t all = i / per, col = (i - all * per) * 8;
+    const int which = all < p.rows[0] ? 0 : all < p.rows[1] ? 1 : 2;
+    const int64_t row = all - (which == 0 ? 0 : which == 1 ? p.rows[0] : p.rows[1]);
+    const E* s = (const E*)p.src[which] + row * p.ld[which] + col;
+    typename T::vec8 v = {};
+    if (col + 8 <= p.cols) {
+      __builtin_memcpy(&v, s, 16);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = col + j < cols ? s[col + j] : (E)0.0f;
-    *(typename T::vec8*)((E*)dst + row * ldd + col) = v;
+      for (int j = 0; j < 7; ++j)
+        if (col + j < p.cols) v[j] = s[j];
+    }
+    *(typename T::vec8*)((E*)p.dst[which] + row * p.ldd + col) = v;
   }
 }
 
 // Four values of a row, those before `end` of it.
 template <class T>
-__device__ __forceinline__ void store4(typename T::elem* p, int64_t col, int64_t end, bool vec,
+__device__ __forceinline__ void store4(typename T::elem* p, int64_t col, int64_t end,
                                        const float (&v)[4]) {
   typedef typename T::elem E;
-  if (vec && col + 4 <= end) {
+  if (col + 4 <= end) {
     E e[4] = {(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
-    __builtin_memcpy(__builtin_assume_aligned(p + col, 8), e, 8);
+    __builtin_memcpy(p + col, e, 8);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -53,7 +68,7 @@ struct ForwardArgs {
   int64_t ldw, ldx, T_, F, K, ldh;
   void* h;
   GatedBlocks gate, up;
-  int act, vec;
+  int act;
   uint32_t ni, nj;
 };
 
@@ -78,7 +93,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // 32 rows of a column, from two tiles' sums, as 16-bit values at p[0..31], those before `end`:
 // 16 bytes a lane.
 template <class T>
-__device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, bool vec, bool ok, int lane,
+__device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, bool ok, int lane,
                                            f32x4 v0, f32x4 v1) {
   uint32_t a0 = pack2<T>(v0[0], v0[1]), a1 = pack2<T>(v0[2], v0[3]);
   uint32_t b0 = pack2<T>(v1[0], v1[1]), b1 = pack2<T>(v1[2], v1[3]);
@@ -87,8 +102,8 @@ __device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, boo
   if (!ok) return;
   const u32x4v w = {a0, a1, b0, b1};
   const int row = 8 * (lane >> 4);
-  if (vec && row + 8 <= end) {
-    __builtin_memcpy(__builtin_assume_aligned(p + row, 16), &w, 16);
+  if (row + 8 <= end) {
+    __builtin_memcpy(p + row, &w, 16);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -102,7 +117,7 @@ __device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, boo
 // The scale and codes of 32 rows of a column, from two tiles' sums: a group of token t from f0 on.
 template <int kFmt>
 __device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int64_t F, int64_t f0,
-                                            int lane, bool ok, bool vec, f32x4 v0, f32x4 v1) {
+                                            int lane, bool ok, f32x4 v0, f32x4 v1) {
   const int q = lane >> 4;
   uint32_t a = 0;
 #pragma unroll
@@ -125,8 +140,8 @@ __device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int
   if (q == 0) b.scales[t * ((F + 31) / 32) + f0 / 32] = (uint8_t)(k + 127);
   const int64_t f = f0 + 8 * q;
   uint8_t* p = b.codes + t * F + f;
-  if (vec && f + 8 <= F) {
-    __builtin_memcpy(__builtin_assume_aligned(p, 8), w, 8);
+  if (f + 8 <= F) {
+    __builtin_memcpy(p, w, 8);
   } else {
 #pragma unroll
     for (int r = 0; r < 8; ++r)
@@ -150,11 +165,11 @@ __device__ __forceinline__ void store_block(const GatedBlocks& b, int64_t t, int
 
 // h = act(x Wg^T) * (x Wu^T): the tile's rows are BI / 2 of w_gate and the same of w_up, a wave
 // has both sums of its outputs.
-template <class T, int kFmt, int BI, int BJ, int WJ, int S>
+template <class T, int kFmt, int BI, int BJ, int WI, int WJ, int S>
 __device__ __forceinline__ void forward_tile(const ForwardArgs& p, uint8_t* const (&sa)[S],
                                              uint8_t* const (&sb)[S]) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
+  constexpr int NW = WI * WJ, NI = BI / WI / 32, NJ = BJ / WJ / 16;  // NI of each projection
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t ti, tj;
   tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
@@ -188,10 +203,10 @@ __device__ __forceinline__ void forward_tile(const ForwardArgs& p, uint8_t* cons
 #pragma unroll
       for (int r = 0; r < 8; ++r)
         v[r >> 2][r & 3] = gate_act(acc[i + (r >> 2)][j][r & 3], p.act) * acc[NI + i + (r >> 2)][j][r & 3];
-      store_rows<T>(row + f, p.F - f, p.vec & 1, ok, lane, v[0], v[1]);
+      store_rows<T>(row + f, p.F - f, ok, lane, v[0], v[1]);
       if constexpr (kFmt >= 0) {
-        store_block<kFmt>(p.gate, t, p.F, f, lane, ok, p.vec & 2, acc[i][j], acc[i + 1][j]);
-        store_block<kFmt>(p.up, t, p.F, f, lane, ok, p.vec & 2, acc[NI + i][j], acc[NI + i + 1][j]);
+        store_block<kFmt>(p.gate, t, p.F, f, lane, ok, acc[i][j], acc[i + 1][j]);
+        store_block<kFmt>(p.up, t, p.F, f, lane, ok, acc[NI + i][j], acc[NI + i + 1][j]);
       }
     }
   }
@@ -201,12 +216,17 @@ __device__ __forceinline__ void forward_tile(const ForwardArgs& p, uint8_t* cons
 template <class T, int kFmt>
 __global__ __launch_bounds__(512, 2) void forward_kernel(ForwardArgs p) {
   HOBFLOPS_STAGES2(256, 256);
-  forward_tile<T, kFmt, 256, 256, 4, 2>(p, sa, sb);
+  forward_tile<T, kFmt, 256, 256, 2, 4, 2>(p, sa, sb);
 }
 template <class T, int kFmt>
 __global__ __launch_bounds__(256, 2) void forward_small_kernel(ForwardArgs p) {
   HOBFLOPS_STAGES3(128, 64);
-  forward_tile<T, kFmt, 128, 64, 2, 3>(p, sa, sb);
+  forward_tile<T, kFmt, 128, 64, 2, 2, 3>(p, sa, sb);
+}
+template <class T, int kFmt>
+__global__ __launch_bounds__(256, 3) void forward_few_kernel(ForwardArgs p) {
+  HOBFLOPS_STAGES3(64, 64);
+  forward_tile<T, kFmt, 64, 64, 1, 4, 3>(p, sa, sb);
 }
 
 // The gradients' products, D[i][j] with i along a row of the output:
@@ -220,7 +240,6 @@ struct GradArgs {
   void* out[2];
   float* part;  // with splits: [splits][nj_][ni_ rounded up to 4]
   int64_t per;  // k of a split, a multiple of 64
-  int vec;
   uint32_t ni, nj;
 };
 template <class T, bool kWeights, int BI, int BJ, int WJ, int S>
@@ -272,7 +291,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p, uint8_t* const (&sa
         if (ok && at < p.ni_) *(f32x4*)to = acc[i][j];
         if (ok && at + 16 < p.ni_) *(f32x4*)(to + 16) = acc[i + 1][j];
       } else {
-        store_rows<T>((typename T::elem*)p.out[half] + (ok ? row : 0) * p.ni_ + d, p.ni_ - d, p.vec, ok,
+        store_rows<T>((typename T::elem*)p.out[half] + (ok ? row : 0) * p.ni_ + d, p.ni_ - d, ok,
                       lane, acc[i][j], acc[i + 1][j]);
       }
     }
@@ -294,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs p) {
 // Sums the splits of a product in their order.
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(const float* part, int splits, int64_t rows,
-                                                   int64_t cols, typename T::elem* out, bool vec) {
+                                                   int64_t cols, typename T::elem* out) {
   const int64_t ldp = (cols + 3) & ~(int64_t)3, n = rows * ldp;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n;
        i += (int64_t)gridDim.x * 1024) {
@@ -302,7 +321,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, int splits
     for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + s * n + i);
     const int64_t row = i / ldp, col = i - row * ldp;
     const float e[4] = {v[0], v[1], v[2], v[3]};
-    store4<T>(out + row * cols, col, cols, vec, e);
+    store4<T>(out + row * cols, col, cols, e);
   }
 }
 
@@ -313,7 +332,7 @@ struct GateGradArgs {
   GatedBlocks gate, up;
   void* out;
   int64_t T_, F, Fp, ldh;
-  int act, vec;  // vec 1: dh in 16-byte accesses, 2: codes in 8-byte ones
+  int act;
 };
 template <class T, int kFmt>
 __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs p) {
@@ -328,15 +347,15 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs p) {
       uint32_t wg[2] = {0, 0}, wu[2] = {0, 0};
       typename T::vec8 d;
       const bool whole = col + 8 <= p.F;
-      if ((p.vec & 1) && whole) {
-        d = *(const typename T::vec8*)dh;
+      if (whole) {
+        __builtin_memcpy(&d, dh, 16);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] = col + j < p.F ? dh[j] : (E)0.0f;
       }
-      if ((p.vec & 2) && whole) {
-        __builtin_memcpy(wg, __builtin_assume_aligned(gc, 8), 8);
-        __builtin_memcpy(wu, __builtin_assume_aligned(uc, 8), 8);
+      if (whole) {
+        __builtin_memcpy(wg, gc, 8);
+        __builtin_memcpy(wu, uc, 8);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -426,30 +445,42 @@ BackwardPlan plan_backward(const hobflops_gated_desc& d) {
   p.small = tiles < 128;
   const int64_t n = p.small ? ((d.D + 127) / 128) * ((d.T + 127) / 128) : tiles;
   const int64_t steps = 2 * p.Fp / kStepK;
+  // parts of the long sum for as many workgroups as there are CUs, of at least six steps
   int64_t s = n < 256 ? 256 / n : 1;
   s = s < kMaxSplits ? s : kMaxSplits;
-  p.splits = (int)(s < steps / 4 ? s : steps / 4 > 1 ? steps / 4 : 1);
+  p.splits = (int)(s < steps / 6 ? s : steps / 6 > 1 ? steps / 6 : 1);
   if (p.splits > 1) p.part = take(&p.bytes, p.splits * d.T * round_up(d.D, 4) * 4);
   return p;
 }
 
+// Adds a tensor to those that a launch aligns.
+void add_rows(AlignArgs& a, int i, const void* src, int64_t ld, int64_t rows, void* dst) {
+  a.src[i] = src;
+  a.dst[i] = dst;
+  a.ld[i] = ld;
+  for (int j = i; j < 3; ++j) a.rows[j] += rows;
+}
 template <class T>
-void align_rows(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd,
-                hipStream_t s) {
-  align_kernel<T><<<grid_of(rows * ldd / 8, 65536), 256, 0, s>>>(src, ld, rows, cols, dst, ldd);
+void align_rows(const AlignArgs& a, hipStream_t s) {
+  if (a.rows[2] > 0) align_kernel<T><<<grid_of(a.rows[2] * a.ldd / 8, 65536), 256, 0, s>>>(a);
 }
 
 template <class T, int kFmt>
 void forward_tiles(ForwardArgs& p, hipStream_t s) {
   const int64_t big = ((p.F + 127) / 128) * ((p.T_ + 255) / 256);
+  const int64_t small = ((p.F + 63) / 64) * ((p.T_ + 63) / 64);
   if (big >= 192) {
     p.ni = (uint32_t)((p.F + 127) / 128);
     p.nj = (uint32_t)((p.T_ + 255) / 256);
     forward_kernel<T, kFmt><<<p.ni * p.nj, 512, 0, s>>>(p);
-  } else {
+  } else if (small > kCUs / 2) {
     p.ni = (uint32_t)((p.F + 63) / 64);
     p.nj = (uint32_t)((p.T_ + 63) / 64);
     forward_small_kernel<T, kFmt><<<p.ni * p.nj, 256, 0, s>>>(p);
+  } else {
+    p.ni = (uint32_t)((p.F + 31) / 32);
+    p.nj = (uint32_t)((p.T_ + 63) / 64);
+    forward_few_kernel<T, kFmt><<<p.ni * p.nj, 256, 0, s>>>(p);
   }
 }
 
@@ -465,19 +496,22 @@ hipError_t forward(const hobflops_gated_desc& d, const GatedForward& c, int fmt,
   p.ldx = d.ldx;
   p.ldw = d.ldw;
   p.K = d.D;
+  AlignArgs align{};
+  align.cols = d.D;
+  align.ldd = Dp;
   if (plan.x >= 0) {
-    align_rows<T>(c.x, d.ldx, d.T, d.D, ws + plan.x, Dp, s);
     p.x = ws + plan.x;
-    p.ldx = Dp;
-    p.K = Dp;
+    p.ldx = p.K = Dp;
+    add_rows(align, 0, c.x, d.ldx, d.T, ws + plan.x);
   }
   if (plan.wg >= 0) {
-    align_rows<T>(c.w_gate, d.ldw, d.F, d.D, ws + plan.wg, Dp, s);
-    align_rows<T>(c.w_up, d.ldw, d.F, d.D, ws + plan.wu, Dp, s);
     p.w[0] = ws + plan.wg;
     p.w[1] = ws + plan.wu;
-    p.ldw = Dp;
+    p.ldw = p.K = Dp;
+    add_rows(align, 1, c.w_gate, d.ldw, d.F, ws + plan.wg);
+    add_rows(align, 2, c.w_up, d.ldw, d.F, ws + plan.wu);
   }
+  align_rows<T>(align, s);
   p.T_ = d.T;
   p.F = d.F;
   p.ldh = d.ldh;
@@ -485,8 +519,6 @@ hipError_t forward(const hobflops_gated_desc& d, const GatedForward& c, int fmt,
   p.gate = c.gate;
   p.up = c.up;
   p.act = d.act;
-  p.vec = (aligned16(c.h) && d.ldh % 8 == 0 ? 1 : 0) |
-          (((uintptr_t)c.gate.codes & 7u) == 0 && ((uintptr_t)c.up.codes & 7u) == 0 && d.F % 8 == 0 ? 2 : 0);
   if (fmt == kE4M3)
     forward_tiles<T, kE4M3>(p, s);
   else if (fmt == kE5M2)
@@ -522,9 +554,7 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
                       HOBFLOPS_SCALE_POW2};
   const hipError_t e = launch_block_unpack(t, fmt, s);
   if (e != hipSuccess) return e;
-  GateGradArgs gg{c.dh, c.gate, c.up, ws + plan.dgu, d.T, d.F, plan.Fp, d.ldh, d.act, 0};
-  gg.vec = (aligned16(c.dh) && d.ldh % 8 == 0 ? 1 : 0) |
-           (((uintptr_t)c.gate.codes & 7u) == 0 && ((uintptr_t)c.up.codes & 7u) == 0 && d.F % 8 == 0 ? 2 : 0);
+  GateGradArgs gg{c.dh, c.gate, c.up, ws + plan.dgu, d.T, d.F, plan.Fp, d.ldh, d.act};
   const unsigned grid = grid_of(d.T * plan.Fp / 8, 1 << 20);
   if (fmt == kE4M3)
     gate_grad_kernel<T, kE4M3><<<grid, 256, 0, s>>>(gg);
@@ -537,7 +567,6 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.ldb = 2 * plan.Fp;
   p.ni_ = d.D;
   p.cols = plan.Dp;
-  const bool rows8 = d.D % 8 == 0;  // the outputs are dense
   GradArgs w = p;
   w.a[0] = ws + plan.x;
   w.lda = plan.Dp;
@@ -546,15 +575,18 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   w.per = round_up(d.T, kStepK);
   w.out[0] = c.dw_gate;
   w.out[1] = c.dw_up;
-  w.vec = rows8 && aligned16(c.dw_gate) && aligned16(c.dw_up);
   const int64_t wt = ((d.D + 255) / 256) * ((2 * plan.Fp + 255) / 256);
   grad_tiles<T, true>(w, wt < 192, 1, s);
   p.a[0] = c.w_gate;
   p.a[1] = c.w_up;
   p.lda = d.ldw;
   if (plan.wg >= 0) {
-    align_rows<T>(c.w_gate, d.ldw, d.F, d.D, ws + plan.wg, plan.Dp, s);
-    align_rows<T>(c.w_up, d.ldw, d.F, d.D, ws + plan.wu, plan.Dp, s);
+    AlignArgs align{};
+    align.cols = d.D;
+    align.ldd = plan.Dp;
+    add_rows(align, 0, c.w_gate, d.ldw, d.F, ws + plan.wg);
+    add_rows(align, 1, c.w_up, d.ldw, d.F, ws + plan.wu);
+    align_rows<T>(align, s);
     p.a[0] = ws + plan.wg;
     p.a[1] = ws + plan.wu;
     p.lda = plan.Dp;
@@ -562,14 +594,13 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.nj_ = d.T;
   p.K = 2 * plan.Fp;
   p.out[0] = c.dx;
-  p.vec = rows8 && aligned16(c.dx);
   p.per = round_up((p.K + plan.splits - 1) / plan.splits, kStepK);
   const int splits = (int)((p.K + p.per - 1) / p.per);
   if (plan.part >= 0) p.part = (float*)(ws + plan.part);
   grad_tiles<T, false>(p, plan.small, splits, s);
   if (p.part)
     join_kernel<T><<<grid_of(d.T * round_up(d.D, 4) / 4, 4096), 256, 0, s>>>(p.part, splits, d.T,
-                                                                             d.D, (E*)c.dx, p.vec);
+                                                                             d.D, (E*)c.dx);
   return hipGetLastError();
 }
 
