@@ -62,11 +62,11 @@ __device__ __forceinline__ bool exact_scales(uint32_t w) {
     return ((w + 0x14141414u) & 0xE0E0E0E0u) == 0x80808080u;
 }
 
-// The scales of a row's groups of a unit (256 k), as they are in memory until they are used: a
+// The scales of a row's groups of a unit (256 k, or kSpan), as they are in memory until they are used: a
 // conversion next to the load would wait for it.
-template <int kScale, int kGroup>
+template <int kScale, int kGroup, int kSpan = kUnit>
 struct Scales {
-  static constexpr int kCount = kUnit / kGroup;
+  static constexpr int kCount = kSpan / kGroup;
   static constexpr int kBytes = kScale == HOBFLOPS_SCALE_POW2 ? 1 : kScale == HOBFLOPS_SCALE_BF16 ? 2 : 4;
   static constexpr int kWords = (kCount * kBytes + 3) / 4;
   uint32_t word[kWords];
@@ -97,7 +97,9 @@ struct Scales {
     bool all = kScale == HOBFLOPS_SCALE_POW2;
 #pragma unroll
     for (int i = 0; i < kWords; ++i)
-      all = all && exact_scales<T>(kCount < 4 ? word[i] | 0x7F7F0000u : word[i]);
+      all = all && exact_scales<T>(kCount == 1   ? word[i] | 0x7F7F7F00u
+                                   : kCount == 2 ? word[i] | 0x7F7F0000u
+                                                 : word[i]);
     return all;
   }
   __device__ __forceinline__ float exact_get(int i) const {
@@ -432,6 +434,136 @@ __global__ __launch_bounds__(512) void w4_kernel(W4Product p, int parts, int rin
 #endif
 }
 
+// Many tokens: a tile of 64 rows and 64 tokens a workgroup, all of K, 128 at a time through three
+// stages of LDS. A wave has 16 rows for all the tokens, so that a code is converted once for 64.
+constexpr int kStep = 128, kTileTokens = 64, kTileWaves = 4;
+template <class T, int kScale, int kGroup, bool kGated>
+__global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef typename T::vec8 Vec;
+  typedef Scales<kScale, kGroup, kStep> Sc;
+  constexpr int kMats = kGated ? 2 : 1, NT = kTileTokens / 16, kPer = kGroup / 32, W = kTileWaves, S = 3;
+  constexpr int kX = kTileTokens * kStep * 2, kXLoads = kX / 1024 / W, kCodes = kMats * 1024;
+  // An array a stage, so that the compiler knows that loads into one do not touch the others, counts
+  // them and waits for no more than the scales it needs.
+  __shared__ __align__(1024) uint8_t x0[kX], x1[kX], x2[kX], c0[W * kCodes], c1[W * kCodes], c2[W * kCodes];
+  uint8_t* const xs[3] = {x0, x1, x2};
+  uint8_t* const cs[3] = {c0, c1, c2};
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, q = lane >> 4, turn = (q & 1) << 1 | q >> 1;
+  const int64_t n0 = ((int64_t)blockIdx.x * W + wave) * 16, n = n0 + col, row = n < p.N ? n : p.N - 1;
+  const int64_t t0 = (int64_t)blockIdx.y * kTileTokens;
+  const int K = (int)p.K, row_bytes = K / 2, groups = (K + kGroup - 1) / kGroup;
+  const int tokens = (int)(p.T - t0 < kTileTokens ? p.T - t0 : kTileTokens);
+  const int left = (int)(p.N - n0 < 0 ? 0 : p.N - n0 < 16 ? p.N - n0 : 16);
+  typedef __attribute__((address_space(3))) uint8_t lds_byte;
+  const auto raw = [](const void* at, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(at), 0, (int)bytes, 0x00020000);
+  };
+  __amdgpu_buffer_rsrc_t rows[kMats];
+#pragma unroll
+  for (int c = 0; c < kMats; ++c)  // no rows: an empty range, all zeros
+    rows[c] = raw((c ? p.w_up : p.w).codes + (left ? n0 : 0) * row_bytes, (uint32_t)(left * row_bytes));
+  const uint32_t code_off = (uint32_t)((lane >> 2) * row_bytes + (((lane & 3) ^ (-(lane >> 4) & 3)) << 4));
+  const uint32_t ld2 = (uint32_t)(p.ldx * 2);
+  const auto x_rows = raw((const uint8_t*)p.x + t0 * p.ldx * 2, (uint32_t)(tokens - 1) * ld2 + (uint32_t)K * 2);
+  Sc scale[S][kMats];
+  const auto load = [&](int step, int stage, Sc(&s)[kMats]) {
+    s[0].load(p.w.scales, row, groups, step, p.N);
+    if constexpr (kGated) s[1].load(p.w_up.scales, row, groups, step, p.N);
+#pragma unroll
+    for (int c = 0; c < kMats; ++c)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rows[c], (lds_byte*)(cs[stage] + wave * kCodes + c * 1024), 16,
+                                               code_off + (uint32_t)step * (kStep / 2), 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) {  // four tokens of 256 bytes
+      const int t = 4 * (wave * kXLoads + i) + (lane >> 4), k = step * kStep + ((lane & 15) ^ (t & 15)) * 8;
+      const bool in = t < tokens && k < K;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rows, (lds_byte*)(xs[stage] + (wave * kXLoads + i) * 1024), 16,
+                                               in ? (uint32_t)t * ld2 + (uint32_t)k * 2 : 0x80000000u, 0, 0, 0);
+    }
+  };
+  f32x4 acc[kMats][NT] = {};
+  const auto multiply = [&](int stage, const Sc(&s)[kMats]) {
+    uint32_t word[kMats][4];
+    bool exact = true;
+#pragma unroll
+    for (int c = 0; c < kMats; ++c) {
+      turn_codes(*(const u32x4v*)(cs[stage] + wave * kCodes + c * 1024 + col * 64 +
+                                  ((q ^ (-(col >> 2) & 3)) << 4)),
+                 word[c]);
+      exact = exact && s[c].template exact<T>();
+    }
+    const auto x = [&](int m, int j) {
+      return *(const Vec*)(xs[stage] + (16 * j + col) * 256 + (((4 * m + turn) ^ col) << 4));
+    };
+    if (kScale == HOBFLOPS_SCALE_POW2 && __all(exact)) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        Vec w[kMats];
+#pragma unroll
+        for (int c = 0; c < kMats; ++c) w[c] = decode8<T>(word[c][m], s[c].exact_get(m));
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const Vec v = x(m, j);
+#pragma unroll
+          for (int c = 0; c < kMats; ++c) acc[c][j] = T::mfma(v, w[c], acc[c][j]);
+        }
+      }
+    } else {
+      f32x4 sum[kMats][NT];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        Vec w[kMats];
+#pragma unroll
+        for (int c = 0; c < kMats; ++c) w[c] = decode8<T>(word[c][m], 1.0f);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const Vec v = x(m, j);
+#pragma unroll
+          for (int c = 0; c < kMats; ++c) {
+            const f32x4 zero = {};
+            sum[c][j] = T::mfma(v, w[c], m % kPer == 0 ? zero : sum[c][j]);
+          }
+        }
+        if (m % kPer == kPer - 1) {
+#pragma unroll
+          for (int c = 0; c < kMats; ++c) {
+            const float f = s[c].get(m);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[c][j][r] += f * sum[c][j][r];
+          }
+        }
+      }
+    }
+  };
+  // A step's loads are issued S - 1 steps ahead, into the stage that all waves have read when the barrier is
+  // passed. Its wait counts the loads into LDS alone; the scales' loads between them only make it
+  // stricter. Steps beyond the last are of zeros.
+  const int steps = (K + kStep - 1) / kStep;
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i) load(i, i, scale[i]);
+  for (int k = 0; k < steps; k += S) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kMats + kXLoads))
+                   : "memory");
+      load(k + i + S - 1, (i + S - 1) % S, scale[(i + S - 1) % S]);
+      multiply(i, scale[i]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    f32x4 y[kMats];
+#pragma unroll
+    for (int c = 0; c < kMats; ++c) y[c] = acc[c][j];
+    store_tokens<T, kMats>(p, n, t0 + 16 * j, lane, y);
+  }
+#endif
+}
+
 // Any K and alignment, byte by byte: a wave a row of W and token.
 template <class T>
 __global__ __launch_bounds__(256) void w4_bytes_kernel(W4Product p) {
@@ -459,6 +591,14 @@ void launch_tiles(const W4Product& p, hipStream_t stream) {
   constexpr int kMats = kGated ? 2 : 1, kSlot = kMats * 2048;  // LDS of a unit
   const int64_t tiles = (p.N + 15) / 16, parts = (p.T + 15) / 16;
   const int units = (int)((p.K + kUnit - 1) / kUnit), tokens = (int)(p.T < 16 ? p.T : 16);
+  // Tokens in tiles of 64 where that leaves a workgroup for half of the CUs: 64 tokens, both projections of
+  // 8192 -> 16384: 71 us against 236 in tokens of 16; with 64 workgroups (4096 -> 4096) 22.6 against 19.4.
+  const int64_t many = (p.T + kTileTokens - 1) / kTileTokens, rows = (p.N + 16 * kTileWaves - 1) / (16 * kTileWaves);
+  if (p.T > 16 && rows * many >= kCUs / 2) {
+    w4_tile_kernel<T, kScale, kGroup, kGated>
+        <<<dim3((unsigned)rows, (unsigned)many), 64 * kTileWaves, 0, stream>>>(p);
+    return;
+  }
   {
     // the fewest units a wave that 16 waves make possible, and as few waves as that needs
     const int each = (units + 15) / 16, waves = (units + each - 1) / each;

@@ -170,7 +170,9 @@ def test_every_power_of_two(dtype, T, N, K):
 
 @pytest.mark.parametrize("T,K,N,group,scale", [
     (1, 4096, 11300, 32, "pow2"), (5, 4104, 9001, 64, "f32"), (16, 1280, 20000, 128, "bf16"),
-    (2, 8192, 5000, 32, "f32"), (16, 11264, 600, 32, "pow2"), (40, 2048, 1500, 64, "bf16")])
+    (2, 8192, 5000, 32, "f32"), (16, 11264, 600, 32, "pow2"), (40, 2048, 1500, 64, "bf16"),
+    (40, 2048, 8300, 64, "bf16"), (70, 264, 9001, 32, "pow2"), (64, 1096, 8192, 128, "f32"),
+    (17, 136, 8185, 32, "f32"), (130, 4096, 4104, 32, "pow2")])
 def test_many_tiles(T, K, N, group, scale):
     """Sizes at which a workgroup takes several tiles, or a wave several rounds."""
     hf = need_gpu()
