@@ -306,8 +306,8 @@ __global__ __launch_bounds__(512, 2) void grad_kernel(GradArgs p) {
 }
 template <class T, bool kWeights>
 __global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs p) {
-  HOBFLOPS_STAGES3(128, 128);
-  grad_tile<T, kWeights, 128, 128, 2, 3>(p, sa, sb);
+  HOBFLOPS_STAGES2(128, 128);
+  grad_tile<T, kWeights, 128, 128, 2, 2>(p, sa, sb);
 }
 
 // Sums the splits of a product in their order.
@@ -424,11 +424,42 @@ ForwardPlan plan_forward(const hobflops_gated_desc& d) {
   return p;
 }
 
+// The tiles of a gradient's product and the parts of its sum, by an estimate of their time in microseconds:
+// rounds of workgroups (of 256 x 256 tiles one on a CU, of 128 x 128 two), each its steps of 64 k and about
+// five more to start and end, at 1.42 and 0.8 a step; the parts of a sum are written and read once
+// more in float32, 4 TB/s, and joined in a launch. Measured, us: dx 1000 x 4096, sums of 22528, in
+// one part 222 (128 x 128), in parts 180 (256 x 256); 333 x 4096, in 128 x 128: one part 118, parts 97;
+// 3000 x 2048, sums of 11264: 128 x 128 one on a CU 183, two 138; dW of 1000 x 4096 x 22528: 256 x 256 172,
+// 128 x 128 191, of 1 x 512 x 2816 7.5 and 5.5.
+struct Tiling {
+  bool small;
+  int splits;
+};
 constexpr int kMaxSplits = 32;
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, bool may_split) {
+  const int64_t steps = (K + kStepK - 1) / kStepK;
+  Tiling best{false, 1};
+  double least = -1.0;
+  for (int small = 0; small < 2; ++small) {
+    const int64_t side = small ? 128 : 256, slots = small ? 2 * kCUs : kCUs;
+    const int64_t tiles = ((rows + side - 1) / side) * ((cols + side - 1) / side);
+    const double step = small ? 0.8 : 1.42;
+    for (int n = 1; n <= (may_split ? kMaxSplits : 1) && (n == 1 || steps / n >= 6); ++n) {
+      const double rounds = (double)((tiles * n + slots - 1) / slots);
+      double us = rounds * ((double)((steps + n - 1) / n) + 5.0) * step;
+      if (n > 1) us += 4.0 + (double)(n + 1) * rows * cols * 4.0 / 4e6;
+      if (least < 0.0 || us < least) {
+        least = us;
+        best = Tiling{small != 0, n};
+      }
+    }
+  }
+  return best;
+}
 struct BackwardPlan {
   int64_t x = -1, wg = -1, wu = -1, dgu = -1, part = -1, bytes = 0;
   int64_t Dp, Fp;
-  int splits, small;  // of dx; 128 x 128 tiles
+  Tiling dx, dw;
 };
 BackwardPlan plan_backward(const hobflops_gated_desc& d) {
   BackwardPlan p;
@@ -441,15 +472,9 @@ BackwardPlan plan_backward(const hobflops_gated_desc& d) {
     p.wg = take(&p.bytes, d.F * p.Dp * 2);
     p.wu = take(&p.bytes, d.F * p.Dp * 2);
   }
-  const int64_t tiles = ((d.D + 255) / 256) * ((d.T + 255) / 256);
-  p.small = tiles < 128;
-  const int64_t n = p.small ? ((d.D + 127) / 128) * ((d.T + 127) / 128) : tiles;
-  const int64_t steps = 2 * p.Fp / kStepK;
-  // parts of the long sum for as many workgroups as there are CUs, of at least six steps
-  int64_t s = n < 256 ? 256 / n : 1;
-  s = s < kMaxSplits ? s : kMaxSplits;
-  p.splits = (int)(s < steps / 6 ? s : steps / 6 > 1 ? steps / 6 : 1);
-  if (p.splits > 1) p.part = take(&p.bytes, p.splits * d.T * round_up(d.D, 4) * 4);
+  p.dx = plan_tiles(d.T, d.D, 2 * p.Fp, true);
+  p.dw = plan_tiles(2 * p.Fp, d.D, d.T, false);
+  if (p.dx.splits > 1) p.part = take(&p.bytes, p.dx.splits * d.T * round_up(d.D, 4) * 4);
   return p;
 }
 
@@ -575,8 +600,7 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   w.per = round_up(d.T, kStepK);
   w.out[0] = c.dw_gate;
   w.out[1] = c.dw_up;
-  const int64_t wt = ((d.D + 255) / 256) * ((2 * plan.Fp + 255) / 256);
-  grad_tiles<T, true>(w, wt < 192, 1, s);
+  grad_tiles<T, true>(w, plan.dw.small, 1, s);
   p.a[0] = c.w_gate;
   p.a[1] = c.w_up;
   p.lda = d.ldw;
@@ -594,10 +618,10 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.nj_ = d.T;
   p.K = 2 * plan.Fp;
   p.out[0] = c.dx;
-  p.per = round_up((p.K + plan.splits - 1) / plan.splits, kStepK);
+  p.per = round_up((p.K + plan.dx.splits - 1) / plan.dx.splits, kStepK);
   const int splits = (int)((p.K + p.per - 1) / p.per);
   if (plan.part >= 0) p.part = (float*)(ws + plan.part);
-  grad_tiles<T, false>(p, plan.small, splits, s);
+  grad_tiles<T, false>(p, plan.dx.small, splits, s);
   if (p.part)
     join_kernel<T><<<grid_of(d.T * round_up(d.D, 4) / 4, 4096), 256, 0, s>>>(p.part, splits, d.T,
                                                                              d.D, (E*)c.dx);
