@@ -165,6 +165,9 @@ __device__ __forceinline__ void stage_ready() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kPending) : "memory");
 }
 
+// Before a wave ends, and with its workgroup LDS becomes another's.
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // The order of a quarter step's instructions: LDS reads behind the first of the matrix instructions, so
 // that they are done when the quarter is, loads spread over all of them.
 template <int kMfma, int kReads, int kLoads>
@@ -239,6 +242,7 @@ __device__ __forceinline__ void sum_tiles(f32x4 (&acc)[NI][NJ], uint8_t* const (
       interleave<H * NJ, kReadsA + kReadsB, kLoads>();
     }
   }
+  loads_done();
 }
 
 #endif  // __HIP_DEVICE_COMPILE__
