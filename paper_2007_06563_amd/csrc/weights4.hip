@@ -554,6 +554,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
       multiply(i, scale[i]);
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // LDS becomes another workgroup's
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     f32x4 y[kMats];
@@ -654,11 +655,11 @@ void launch_scale(const W4Product& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_w4(const W4Product& all, hipStream_t stream) {
-  // tokens in parts, for the grid's second axis
-  constexpr int64_t kTokens = 4096;
-  for (int64_t t = 0; t < all.T; t += kTokens) {
+  // tokens in parts, for the grid's second axis; where 64 of x may be 2^31 bytes apart, in single tiles of 16
+  const int64_t tokens = all.ldx < (int64_t)1 << 24 ? 4096 : 16;
+  for (int64_t t = 0; t < all.T; t += tokens) {
     W4Product p = all;
-    p.T = all.T - t < kTokens ? all.T - t : kTokens;
+    p.T = all.T - t < tokens ? all.T - t : tokens;
     p.x = (const uint16_t*)all.x + t * all.ldx;
     p.y = (uint16_t*)all.y + t * all.ldy;
     if (p.type == HOBFLOPS_TYPE_BF16)

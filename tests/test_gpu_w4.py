@@ -193,3 +193,21 @@ def test_many_tiles(T, K, N, group, scale):
         want = g * s * u
         assert ((h - want).abs() <= e + UNIT[dtype] * want.abs() + TINY[dtype]).all()
         assert torch.equal(hf.w4_linear(xt, cg, sg, group=group).double(), y)
+
+
+@pytest.mark.parametrize("T,ld", [(3, (1 << 26) - 2), (16, (1 << 25) + 2), (40, (1 << 25) + 2), (40, 1 << 24)])
+def test_rows_far_apart(T, ld):
+    """Rows of x and y whose offsets pass 31 bits, K that ends inside a step."""
+    hf = need_gpu()
+    say("w4 rows far apart", T, ld)
+    K, N, group = 136, 8200, 32
+    cg, sg, wg = _weights(hf, N, K, group, "f32", 21)
+    near = _x(T, K, "bf16", 22)
+    x = torch.full((T * ld,), float("nan"), dtype=torch.bfloat16, device="cuda").view(T, ld)[:, :K]
+    x.copy_(near)
+    out = torch.empty((T * ld,), dtype=torch.bfloat16, device="cuda").view(T, ld)[:, :N]
+    y = hf.w4_linear(x, cg, sg, group=group, out=out).double()
+    wg = torch.from_numpy(wg).cuda()
+    want = near.double() @ wg.T
+    e = (K + 4) * EPS * (near.double().abs() @ wg.abs().T)
+    assert ((y - want).abs() <= e + UNIT["bf16"] * want.abs()).all()
