@@ -27,11 +27,12 @@ struct AlignArgs {
   int64_t ld[3], rows[3];  // rows: of this tensor and those before
   int64_t cols, ldd;
 };
+// (i: the thread's number, of `stride` of them; so below)
 template <class T>
-__global__ __launch_bounds__(256) void align_kernel(AlignArgs p) {
+__device__ __forceinline__ void align_rows_of(const AlignArgs& p, int64_t i, int64_t stride) {
   typedef typename T::elem E;
   const int64_t per = p.ldd / 8, n = p.rows[2] * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  for (; i < n; i += stride) {
     const int64_t all = i / per, col = (i - all * per) * 8;
     const int which = all < p.rows[0] ? 0 : all < p.rows[1] ? 1 : 2;
     const int64_t row = all - (which == 0 ? 0 : which == 1 ? p.rows[0] : p.rows[1]);
@@ -46,6 +47,10 @@ __global__ __launch_bounds__(256) void align_kernel(AlignArgs p) {
     }
     *(typename T::vec8*)((E*)p.dst[which] + row * p.ldd + col) = v;
   }
+}
+template <class T>
+__global__ __launch_bounds__(256) void align_kernel(AlignArgs p) {
+  align_rows_of<T>(p, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
 // Four values of a row, those before `end` of it.
@@ -244,14 +249,14 @@ struct GradArgs {
 };
 template <class T, bool kWeights, int BI, int BJ, int WJ, int S>
 __device__ __forceinline__ void grad_tile(const GradArgs& p, uint8_t* const (&sa)[S],
-                                          uint8_t* const (&sb)[S]) {
+                                          uint8_t* const (&sb)[S], uint32_t tile, uint32_t split) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WI = 2, NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t ti, tj;
-  tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
+  tile_of(tile, p.ni, p.nj, ti, tj);
   const int64_t i0 = (int64_t)ti * BI, j0 = (int64_t)tj * BJ;
-  const int64_t k0 = (int64_t)blockIdx.y * p.per;
+  const int64_t k0 = (int64_t)split * p.per;
   const int64_t k1 = k0 + p.per < p.K ? k0 + p.per : p.K;
   const int steps = (int)((k1 - k0 + kStepK - 1) / kStepK);
   LoadColumns<BI, NW, kWeights ? 1 : 2> la;
@@ -287,7 +292,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p, uint8_t* const (&sa
       const int64_t d = i0 + wi * NI * 16 + 16 * i;
       if (p.part) {
         const int64_t ldp = (p.ni_ + 3) & ~(int64_t)3, at = d + 4 * (lane >> 4);
-        float* to = p.part + ((int64_t)blockIdx.y * p.nj_ + c) * ldp + at;
+        float* to = p.part + ((int64_t)split * p.nj_ + c) * ldp + at;
         if (ok && at < p.ni_) *(f32x4*)to = acc[i][j];
         if (ok && at + 16 < p.ni_) *(f32x4*)(to + 16) = acc[i + 1][j];
       } else {
@@ -299,15 +304,27 @@ __device__ __forceinline__ void grad_tile(const GradArgs& p, uint8_t* const (&sa
 #endif
 }
 
-template <class T, bool kWeights>
-__global__ __launch_bounds__(512, 2) void grad_kernel(GradArgs p) {
-  HOBFLOPS_STAGES2(256, 256);
-  grad_tile<T, kWeights, 256, 256, 4, 2>(p, sa, sb);
+// Workgroups of dx, as many as `parts`, then those of the weights' gradients: in one launch they fill each
+// other's last rounds.
+template <class T, int B, int WJ>
+__device__ __forceinline__ void grad_tiles_of(const GradArgs& dx, const GradArgs& dw, uint32_t parts,
+                                              uint8_t* const (&sa)[2], uint8_t* const (&sb)[2]) {
+  if (blockIdx.x < parts) {
+    const uint32_t tiles = dx.ni * dx.nj;
+    grad_tile<T, false, B, B, WJ, 2>(dx, sa, sb, blockIdx.x % tiles, blockIdx.x / tiles);
+  } else {
+    grad_tile<T, true, B, B, WJ, 2>(dw, sa, sb, blockIdx.x - parts, 0);
+  }
 }
-template <class T, bool kWeights>
-__global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs p) {
+template <class T>
+__global__ __launch_bounds__(512, 2) void grad_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
+  HOBFLOPS_STAGES2(256, 256);
+  grad_tiles_of<T, 256, 4>(dx, dw, parts, sa, sb);
+}
+template <class T>
+__global__ __launch_bounds__(256, 2) void grad_small_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
   HOBFLOPS_STAGES2(128, 128);
-  grad_tile<T, kWeights, 128, 128, 2, 2>(p, sa, sb);
+  grad_tiles_of<T, 128, 2>(dx, dw, parts, sa, sb);
 }
 
 // Sums the splits of a product in their order.
@@ -325,6 +342,18 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, int splits
   }
 }
 
+// Up to eight codes, `left` of them.
+__device__ __forceinline__ void load_codes(const uint8_t* p, int64_t left, uint32_t (&w)[2]) {
+  if (left >= 8) {
+    __builtin_memcpy(w, p, 8);
+  } else {
+    w[0] = w[1] = 0;
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < left) w[j >> 2] |= (uint32_t)p[j] << (8 * (j & 3));
+  }
+}
+
 // dg and du, rows [t][2 Fp] (du from Fp on, zeros from F to Fp), from dh and the blocks of g and u:
 // 8 values a thread.
 struct GateGradArgs {
@@ -335,35 +364,25 @@ struct GateGradArgs {
   int act;
 };
 template <class T, int kFmt>
-__global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs p) {
+__device__ __forceinline__ void gate_grad_of(const GateGradArgs& p, int64_t i, int64_t stride) {
   typedef typename T::elem E;
   const int64_t per = p.Fp / 8, n = p.T_ * per, groups = (p.F + 31) / 32;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  for (; i < n; i += stride) {
     const int64_t row = i / per, col = (i - row * per) * 8;
     typename T::vec8 dg, du;
     if (col < p.F) {
       const E* dh = (const E*)p.dh + row * p.ldh + col;
       const uint8_t *gc = p.gate.codes + row * p.F + col, *uc = p.up.codes + row * p.F + col;
-      uint32_t wg[2] = {0, 0}, wu[2] = {0, 0};
+      uint32_t wg[2], wu[2];
       typename T::vec8 d;
-      const bool whole = col + 8 <= p.F;
-      if (whole) {
+      if (col + 8 <= p.F) {
         __builtin_memcpy(&d, dh, 16);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] = col + j < p.F ? dh[j] : (E)0.0f;
       }
-      if (whole) {
-        __builtin_memcpy(wg, gc, 8);
-        __builtin_memcpy(wu, uc, 8);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col + j < p.F) {
-            wg[j >> 2] |= (uint32_t)gc[j] << (8 * (j & 3));
-            wu[j >> 2] |= (uint32_t)uc[j] << (8 * (j & 3));
-          }
-      }
+      load_codes(gc, p.F - col, wg);
+      load_codes(uc, p.F - col, wu);
       const int64_t s = row * groups + col / 32;
       const float sg = load_scale(p.gate.scales, s, HOBFLOPS_SCALE_POW2);
       const float su = load_scale(p.up.scales, s, HOBFLOPS_SCALE_POW2);
@@ -388,6 +407,47 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(GateGradArgs p) {
     *(typename T::vec8*)out = dg;
     *(typename T::vec8*)(out + p.Fp) = du;
   }
+}
+
+// Rows [t][ldd] of the values of blocks, zeros from cols on: 8 a thread.
+struct UnpackArgs {
+  GatedBlocks blocks;
+  void* out;
+  int64_t rows, cols, ldd;
+};
+template <class T, int kFmt>
+__device__ __forceinline__ void unpack_of(const UnpackArgs& p, int64_t i, int64_t stride) {
+  typedef typename T::elem E;
+  const int64_t per = p.ldd / 8, n = p.rows * per, groups = (p.cols + 31) / 32;
+  for (; i < n; i += stride) {
+    const int64_t row = i / per, col = (i - row * per) * 8;
+    uint32_t w[2];
+    load_codes(p.blocks.codes + row * p.cols + col, p.cols - col, w);
+    const float s = load_scale(p.blocks.scales, row * groups + col / 32, HOBFLOPS_SCALE_POW2);
+    typename T::vec8 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 d = decode4<kFmt>(w[h]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[4 * h + j] = col + 4 * h + j < p.cols ? round_product<T>(d[j], s) : (E)0.0f;
+    }
+    *(typename T::vec8*)((E*)p.out + row * p.ldd + col) = v;
+  }
+}
+
+// What the gradients' products read, in one launch: the first workgroups write dg and du, the next the values of
+// x, the last the weights' rows if they must be aligned.
+template <class T, int kFmt>
+__global__ __launch_bounds__(256) void prepare_kernel(GateGradArgs gate, UnpackArgs x, AlignArgs w, uint32_t gates,
+                                                      uint32_t xs) {
+  const uint32_t b = blockIdx.x;
+  if (b < gates)
+    gate_grad_of<T, kFmt>(gate, (int64_t)b * 256 + threadIdx.x, (int64_t)gates * 256);
+  else if (b < gates + xs)
+    unpack_of<T, kFmt>(x, (int64_t)(b - gates) * 256 + threadIdx.x, (int64_t)xs * 256);
+  else
+    align_rows_of<T>(w, (int64_t)(b - gates - xs) * 256 + threadIdx.x, (int64_t)(gridDim.x - gates - xs) * 256);
 }
 
 __global__ void zero_kernel(uint16_t* p, int64_t n) {
@@ -553,16 +613,21 @@ hipError_t forward(const hobflops_gated_desc& d, const GatedForward& c, int fmt,
   return hipGetLastError();
 }
 
-template <class T, bool kWeights>
-void grad_tiles(GradArgs& p, bool small, int splits, hipStream_t s) {
+// The tiles of a product, in p.ni and p.nj; their number.
+uint32_t count_tiles(GradArgs& p, bool small) {
   const int64_t b = small ? 128 : 256;
   p.ni = (uint32_t)((p.ni_ + b - 1) / b);
   p.nj = (uint32_t)((p.nj_ + b - 1) / b);
-  const dim3 grid(p.ni * p.nj, (unsigned)splits);
+  return p.ni * p.nj;
+}
+// dx in `parts` workgroups and dw in `tiles`, either may be none.
+template <class T>
+void grad_products(const GradArgs& dx, uint32_t parts, const GradArgs& dw, uint32_t tiles, bool small,
+                   hipStream_t s) {
   if (small)
-    grad_small_kernel<T, kWeights><<<grid, 256, 0, s>>>(p);
+    grad_small_kernel<T><<<parts + tiles, 256, 0, s>>>(dx, dw, parts);
   else
-    grad_kernel<T, kWeights><<<grid, 512, 0, s>>>(p);
+    grad_kernel<T><<<parts + tiles, 512, 0, s>>>(dx, dw, parts);
 }
 
 template <class T>
@@ -575,16 +640,21 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   }
   const BackwardPlan plan = plan_backward(d);
   uint8_t* ws = (uint8_t*)c.workspace;
-  const BlockTensor t{ws + plan.x, d.type, d.T, d.D, plan.Dp, c.x.codes, c.x.scales, 32,
-                      HOBFLOPS_SCALE_POW2};
-  const hipError_t e = launch_block_unpack(t, fmt, s);
-  if (e != hipSuccess) return e;
-  GateGradArgs gg{c.dh, c.gate, c.up, ws + plan.dgu, d.T, d.F, plan.Fp, d.ldh, d.act};
-  const unsigned grid = grid_of(d.T * plan.Fp / 8, 1 << 20);
+  const GateGradArgs gate{c.dh, c.gate, c.up, ws + plan.dgu, d.T, d.F, plan.Fp, d.ldh, d.act};
+  const UnpackArgs x{c.x, ws + plan.x, d.T, d.D, plan.Dp};
+  AlignArgs align{};
+  if (plan.wg >= 0) {
+    align.cols = d.D;
+    align.ldd = plan.Dp;
+    add_rows(align, 0, c.w_gate, d.ldw, d.F, ws + plan.wg);
+    add_rows(align, 1, c.w_up, d.ldw, d.F, ws + plan.wu);
+  }
+  const unsigned gates = grid_of(d.T * plan.Fp / 8, 1 << 20), xs = grid_of(d.T * plan.Dp / 8, 65536);
+  const unsigned grid = gates + xs + grid_of(align.rows[2] * align.ldd / 8, 65536);
   if (fmt == kE4M3)
-    gate_grad_kernel<T, kE4M3><<<grid, 256, 0, s>>>(gg);
+    prepare_kernel<T, kE4M3><<<grid, 256, 0, s>>>(gate, x, align, gates, xs);
   else
-    gate_grad_kernel<T, kE5M2><<<grid, 256, 0, s>>>(gg);
+    prepare_kernel<T, kE5M2><<<grid, 256, 0, s>>>(gate, x, align, gates, xs);
   GradArgs p{};
   p.F = d.F;
   p.Fp = plan.Fp;
@@ -600,17 +670,10 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   w.per = round_up(d.T, kStepK);
   w.out[0] = c.dw_gate;
   w.out[1] = c.dw_up;
-  grad_tiles<T, true>(w, plan.dw.small, 1, s);
   p.a[0] = c.w_gate;
   p.a[1] = c.w_up;
   p.lda = d.ldw;
   if (plan.wg >= 0) {
-    AlignArgs align{};
-    align.cols = d.D;
-    align.ldd = plan.Dp;
-    add_rows(align, 0, c.w_gate, d.ldw, d.F, ws + plan.wg);
-    add_rows(align, 1, c.w_up, d.ldw, d.F, ws + plan.wu);
-    align_rows<T>(align, s);
     p.a[0] = ws + plan.wg;
     p.a[1] = ws + plan.wu;
     p.lda = plan.Dp;
@@ -621,7 +684,13 @@ hipError_t backward(const hobflops_gated_desc& d, const GatedBackward& c, int fm
   p.per = round_up((p.K + plan.dx.splits - 1) / plan.dx.splits, kStepK);
   const int splits = (int)((p.K + p.per - 1) / p.per);
   if (plan.part >= 0) p.part = (float*)(ws + plan.part);
-  grad_tiles<T, false>(p, plan.dx.small, splits, s);
+  const uint32_t parts = count_tiles(p, plan.dx.small) * splits, tiles = count_tiles(w, plan.dw.small);
+  if (plan.dx.small == plan.dw.small) {
+    grad_products<T>(p, parts, w, tiles, plan.dx.small, s);
+  } else {
+    grad_products<T>(p, 0, w, tiles, plan.dw.small, s);
+    grad_products<T>(p, parts, w, 0, plan.dx.small, s);
+  }
   if (p.part)
     join_kernel<T><<<grid_of(d.T * round_up(d.D, 4) / 4, 4096), 256, 0, s>>>(p.part, splits, d.T,
                                                                              d.D, (E*)c.dx);
