@@ -552,9 +552,13 @@ void align_rows(const AlignArgs& a, hipStream_t s) {
 
 template <class T, int kFmt>
 void forward_tiles(ForwardArgs& p, hipStream_t s) {
+  // Large tiles where there are about as many as 160: with 176 (512, or 333, x 4096 x 11264) 105 and 100 us against the
+  // small ones' 141 and 111, with 88 (1 x 4096 x 11264) 89 against 44. The smallest where small ones leave half of the
+  // CUs without one: with 88 of them (1 x 2048 x 5632) 17.0 us against 19.0, with 176 (128 x 2048 x 5632) 22.4
+  // against 20.3.
   const int64_t big = ((p.F + 127) / 128) * ((p.T_ + 255) / 256);
   const int64_t small = ((p.F + 63) / 64) * ((p.T_ + 63) / 64);
-  if (big >= 192) {
+  if (big >= 160) {
     p.ni = (uint32_t)((p.F + 127) / 128);
     p.nj = (uint32_t)((p.T_ + 255) / 256);
     forward_kernel<T, kFmt><<<p.ni * p.nj, 512, 0, s>>>(p);
