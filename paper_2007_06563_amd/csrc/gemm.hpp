@@ -2,8 +2,8 @@
 //
 // A workgroup computes a tile of BI x BJ sums, D[i][j] = sum_k A[i][k] B[j][k], 64 of
 // k at a time. The tiles of A and B go from global memory straight into LDS (buffer
-// loads with the LDS as their target, 16 bytes a lane), into one of two stages while the
-// matrix instructions work on the other. Two layouts of an operand in memory:
+// loads with the LDS as their target, 16 bytes a lane), into one of two or three stages while the
+// matrix instructions work on another. Two layouts of an operand in memory:
 //  - K-contiguous ([row][k], the weights and x of the forward product): an LDS row is 64
 //    k (128 bytes), and a fragment (8 k of a row a lane) is one 16-byte LDS read.
 //  - K-major ([k][column], the weights of dx, both operands of the weight gradients): an
