@@ -370,8 +370,10 @@ int hobflops_gated_forward(const hobflops_gated_desc* d, const void* x, const vo
  * rows of D values: hobflops_block_pack), g and u:
  *   dg = dh * u * act'(g), du = dh * act(g)   (act' of max(g, 0) is 0 at 0)
  *   dx = dg w_gate + du w_up [T][D], dw_gate = dg^T x, dw_up = du^T x [F][D]
- * all dense and of d->type. dg and du are rounded to d->type before the products,
- * whose sums are float32. With T = 0 the gradients of the weights are zero.
+ * all dense and of d->type. dg, du and the values of x's blocks are rounded to d->type
+ * before the products, whose sums are float32. Blocks of x of d->type hold values of that type, but for
+ * 2^16 in float16 (|x| >= 63488 becomes it in (4, 3), >= 61440 in (5, 2)) and 2^128 in bfloat16 (likewise):
+ * the type's largest value is taken for them. With T = 0 the gradients of the weights are zero.
  * Sums run in a fixed order: the same inputs give the same bits. */
 int hobflops_gated_backward(const hobflops_gated_desc* d, const void* dh, const uint8_t* x_codes,
                             const uint8_t* x_scales, const uint8_t* g_codes,

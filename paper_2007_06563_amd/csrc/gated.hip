@@ -6,8 +6,8 @@
 // cycles but took longer: at these rates power sets the clock. 8192 x 22528 x 4096 with values of
 // 0 runs in 0.92 ms, with normal ones in 1.10 ms.)
 //
-// Roundings to 16 bits: h once, from float32 products; dg, du, as operands of the matrix
-// instruction; dx and the weights' gradients once, from float32 sums. g and u in float32
+// Roundings to 16 bits: h once, from float32 products; dg, du and the values of x's blocks, as operands
+// of the matrix instruction; dx and the weights' gradients once, from float32 sums. g and u in float32
 // become 8-bit blocks directly. Every sum has a fixed order: results do not change between runs.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -428,6 +428,18 @@ __device__ __forceinline__ void gate_grad_of(const GateGradArgs& p, int64_t i, i
   }
 }
 
+// A code times its scale as an operand of the type. What blocks of x stand for is one of its values, but that x near
+// the type's top may have been rounded up to 2^16 (2^128), where float16 ends at 65504 (bfloat16 at
+// 255 * 2^120) and has infinity: the largest value, within the type's rounding, is taken for it. What is larger
+// (only blocks of another type's values are) and what is not finite go where the type's rounding takes them.
+template <class T>
+__device__ __forceinline__ typename T::elem operand_of(float d, float s) {
+  const float half = d * (0.5f * s);  // (2^128 is beyond float32)
+  if (__builtin_fabsf(half) == 0.5f * T::kMax + 0.5f * T::kStep)
+    return (typename T::elem)__builtin_copysignf(T::kMax, half);
+  return round_product<T>(d, s);
+}
+
 // Rows [t][ldd] of the values of blocks, zeros from cols on: 8 a thread.
 struct UnpackArgs {
   GatedBlocks blocks;
@@ -449,7 +461,7 @@ __device__ __forceinline__ void unpack_of(const UnpackArgs& p, int64_t i, int64_
       const f32x4 d = decode4<kFmt>(w[h]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        v[4 * h + j] = col + 4 * h + j < p.cols ? round_product<T>(d[j], s) : (E)0.0f;
+        v[4 * h + j] = col + 4 * h + j < p.cols ? operand_of<T>(d[j], s) : (E)0.0f;
     }
     *(typename T::vec8*)((E*)p.out + row * p.ldd + col) = v;
   }

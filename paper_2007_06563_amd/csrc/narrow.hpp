@@ -20,6 +20,7 @@ struct TypeF32 {
 };
 struct TypeBF16 {
   typedef __bf16 elem;
+  static constexpr float kMax = 0x1.FEp127f, kStep = 0x1p120f;  // the largest value and its step
   typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
   typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x4 mfma(vec8 a, vec8 b, f32x4 c) {
@@ -31,6 +32,7 @@ struct TypeBF16 {
 };
 struct TypeF16 {
   typedef _Float16 elem;
+  static constexpr float kMax = 65504.0f, kStep = 32.0f;
   typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
   typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x4 mfma(vec8 a, vec8 b, f32x4 c) {
