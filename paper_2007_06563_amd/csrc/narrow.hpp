@@ -133,9 +133,8 @@ __device__ __forceinline__ float load_scale(const void* s, int64_t i, int kind) 
 __device__ __forceinline__ float sigmoidf(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __expf(-g));
 }
-__device__ __forceinline__ float normal_cdf(float g) {
-  return 0.5f * (1.0f + erff(g * 0.70710678118654752f));
-}
+// (erfc: 1 + erf would cancel where the result is small, below -2)
+__device__ __forceinline__ float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678118654752f); }
 __device__ __forceinline__ float gate_act(float g, int act) {
   if (act == HOBFLOPS_GATE_SILU) return g * sigmoidf(g);
   if (act == HOBFLOPS_GATE_GELU) return g * normal_cdf(g);
