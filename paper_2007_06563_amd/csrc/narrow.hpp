@@ -128,27 +128,44 @@ __device__ __forceinline__ float load_scale(const void* s, int64_t i, int kind) 
 }
 
 // The gate's activation and its derivative.
-// (the reciprocal instruction is within one unit in the last place, the division around it would
-// cost ten instructions)
-__device__ __forceinline__ float sigmoidf(float g) {
-  return __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+struct Sigmoid {
+  float s, c;  // sigmoid(g) and 1 - sigmoid(g) = sigmoid(-g)
+};
+// exp(a), a <= 0, to a few units in the last place, subnormal results too: 2^n 2^f with n + f = a / ln 2, f in
+// [-1/2, 1/2] from 1 / ln 2 in two parts. A NaN counts as -150. (__expf, 2^(a / ln 2) rounded, loses
+// digits with a and everything below 2^-126; expf takes five instructions more for a > 0 and NaN.)
+__device__ __forceinline__ float exp_down(float a) {
+  a = __builtin_fmaxf(a, -150.0f);
+  const float n = __builtin_rintf(a * 1.44269502f);
+  const float f = __builtin_fmaf(a, 1.92596299e-8f, __builtin_fmaf(a, 1.44269502f, -n));
+  return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+}
+// From e = exp(-|g|), which does not overflow, so that s and c keep their digits where they are small; the
+// reciprocal instruction's last place by one Newton step (1 + e is in [1, 2]; a division would cost ten
+// instructions). Of a NaN: numbers, which are multiplied by g.
+__device__ __forceinline__ Sigmoid sigmoid_of(float g) {
+  const float e = exp_down(-__builtin_fabsf(g)), d = 1.0f + e;
+  float r = __builtin_amdgcn_rcpf(d);
+  r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+  const float far = e * r;
+  return g < 0.0f ? Sigmoid{far, r} : Sigmoid{r, far};
 }
 // (erfc: 1 + erf would cancel where the result is small, below -2)
 __device__ __forceinline__ float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678118654752f); }
 __device__ __forceinline__ float gate_act(float g, int act) {
-  if (act == HOBFLOPS_GATE_SILU) return g * sigmoidf(g);
+  if (act == HOBFLOPS_GATE_SILU) return g * sigmoid_of(g).s;
   if (act == HOBFLOPS_GATE_GELU) return g * normal_cdf(g);
   return g > 0.0f || g != g ? g : 0.0f;
 }
 __device__ __forceinline__ void gate_act_grad(float g, int act, float& a, float& da) {
   if (act == HOBFLOPS_GATE_SILU) {
-    const float s = sigmoidf(g);
-    a = g * s;
-    da = s * (1.0f + g * (1.0f - s));
+    const Sigmoid v = sigmoid_of(g);
+    a = g * v.s;
+    da = v.s * (1.0f + g * v.c);
   } else if (act == HOBFLOPS_GATE_GELU) {
     const float p = normal_cdf(g);
     a = g * p;
-    da = p + g * __expf(-0.5f * g * g) * 0.39894228040143268f;
+    da = p + g * exp_down(-0.5f * g * g) * 0.39894228040143268f;
   } else {
     a = g > 0.0f || g != g ? g : 0.0f;
     da = g > 0.0f ? 1.0f : g != g ? g : 0.0f;

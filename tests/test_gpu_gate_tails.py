@@ -18,9 +18,9 @@ from test_gpu_gated import TINY, TYPES, UNIT, _blocks
 
 pytestmark = pytest.mark.gpu
 REL, STEP = 2.0 ** -14, 2.0 ** -149
-LOW = {1: (-9.0, -2.0)}   # GELU
+LOW = {0: (-100.0, -2.0), 1: (-9.0, -2.0)}   # SiLU, GELU
 # what the up projection multiplies by, to bring small values into the type
-UP = {("bf16", 1): 2.0 ** 12, ("f16", 1): 2.0 ** 14}
+UP = {("bf16", 0): 2.0 ** 60, ("bf16", 1): 2.0 ** 12, ("f16", 0): 2.0 ** 14, ("f16", 1): 2.0 ** 14}
 
 
 def _g(act, dtype, n=257):
@@ -35,7 +35,7 @@ def _check(got, want, dtype, u, roundings=1):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("act", [1])
+@pytest.mark.parametrize("act", [0, 1])
 def test_forward(act, dtype):
     hf = need_gpu()
     say("tails forward", act, dtype)
@@ -51,7 +51,7 @@ def test_forward(act, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("act", [1])
+@pytest.mark.parametrize("act", [0, 1])
 def test_gradients(act, dtype):
     """One token with x = 1: the weights' gradients are dg and du."""
     hf = need_gpu()
@@ -74,7 +74,7 @@ def test_gradients(act, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("act", [1])
+@pytest.mark.parametrize("act", [0, 1])
 @pytest.mark.parametrize("T,N", [(1, 16), (16, 40), (20, 8200)])
 def test_w4_gated(T, N, act, dtype):
     hf = need_gpu()
