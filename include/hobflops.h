@@ -332,8 +332,9 @@ int hobflops_block_pack(const void* src, int type, int64_t rows, int64_t cols, i
                         hobflops_fmt f, int group, int scale, uint8_t* codes, void* scales,
                         void* stream);
 
-/* Blocks to values, rounded to nearest even in dst's type (exact in float32 and
- * bfloat16 but for values of 2^128 and above, which go to infinity). */
+/* Blocks to values: the code's value times the scale, rounded to nearest even in dst's type once. Of
+ * blocks that hobflops_block_pack makes with power-of-two scales that is exact in float32 and bfloat16 but
+ * for values of 2^128, which go to infinity. */
 int hobflops_block_unpack(const uint8_t* codes, const void* scales, int64_t rows, int64_t cols,
                           hobflops_fmt f, int group, int scale, void* dst, int type, int64_t ld,
                           void* stream);

@@ -127,6 +127,28 @@ __global__ __launch_bounds__(kThreads) void block_pack_kernel(BlockParams p) {
   }
 }
 
+// A (2, 1) code's value times a float32 scale, rounded to a 16-bit type once: the product needs 25 bits, and
+// rounded to float32 first it could fall on the midpoint of two of the type's values. So where it is not
+// exact, its float32 takes an odd last place, of the two around it, which keeps it off the midpoints. What
+// the float32 is off comes from a multiply-add, or (kSmall) where that could be below 2^-149 from 64 bits.
+template <class T, bool kSmall>
+__device__ __forceinline__ typename T::elem round_wide_product(float v, float s) {
+  const float f = v * s;
+  // the sign of product - f (an f that overflowed goes down to the largest float32, which rounds to
+  // infinity again)
+  float off;
+  if constexpr (kSmall) {
+    const double d = (double)v * (double)s - (double)f;
+    off = d > 0.0 ? 1.0f : d < 0.0 ? -1.0f : 0.0f;
+  } else {
+    off = __builtin_fmaf(v, s, -f);
+  }
+  // one step up or down in magnitude from an even last place
+  const uint32_t b = __float_as_uint(f), step = (__float_as_uint(off) ^ b) >> 31 ? 0xFFFFFFFFu : 1u;
+  const bool move = __builtin_fabsf(off) > 0.0f && !(b & 1u);
+  return (typename T::elem)__uint_as_float(move ? b + step : b);
+}
+
 template <class T, int kFmt>
 __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -164,13 +186,24 @@ __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
     }
   }
   typename T::elem* dst = (typename T::elem*)p.values + row * p.ld + col;
-  if (whole) {
-    typename T::elem e[8];
+  const auto store = [&](auto round) {
+    if (whole) {
+      typename T::elem e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = round_product<T>(v[j], s);
-    __builtin_memcpy(dst, e, sizeof e);
+      for (int j = 0; j < 8; ++j) e[j] = round(v[j]);
+      __builtin_memcpy(dst, e, sizeof e);
+    } else {
+      for (int j = 0; j < 8 && col + j < p.cols; ++j) dst[j] = round(v[j]);
+    }
+  };
+  // (the other scales' products with (2, 1) are exact in float32)
+  if (kFmt == kE2M1 && sizeof(typename T::elem) == 2 && p.scale == HOBFLOPS_SCALE_F32) {
+    if (__all(__builtin_fabsf(s) >= 0x1p-100f))
+      store([&](float a) { return round_wide_product<T, false>(a, s); });
+    else
+      store([&](float a) { return round_wide_product<T, true>(a, s); });
   } else {
-    for (int j = 0; j < 8 && col + j < p.cols; ++j) dst[j] = round_product<T>(v[j], s);
+    store([&](float a) { return round_product<T>(a, s); });
   }
 }
 
