@@ -62,6 +62,25 @@ __device__ __forceinline__ bool exact_scales(uint32_t w) {
     return ((w + 0x14141414u) & 0xE0E0E0E0u) == 0x80808080u;
 }
 
+// A bfloat16 x may be so large, from 2^117 on, that a sum of it times bare codes leaves float32's range where the
+// formula's terms, with a small scale, are far within. So a scale is taken in two factors: a power of two with
+// which the weights are exact (its own, or the nearest of exact_scales), which goes into them, and the
+// rest, which multiplies a group's sum. (Four instructions a scale. One token, both projections of 4096 -> 11264
+// in groups of 32: 15.7 us with bfloat16 x, 14.7 with float16, whose sums with bare codes do not come near 2^128.)
+template <class T>
+constexpr bool kWide = std::is_same_v<T, TypeBF16>;
+struct ScaleParts {
+  float inside, rest;
+};
+template <bool kSplit>
+__device__ __forceinline__ ScaleParts parts_of(float s) {
+  if constexpr (!kSplit) return {1.0f, s};
+  constexpr uint32_t lo = 64u << 23, hi = 191u << 23;
+  uint32_t e = __float_as_uint(s) & 0x7F800000u;
+  e = e < lo ? lo : e > hi ? hi : e;
+  return {__uint_as_float(e), s * __uint_as_float((254u << 23) - e)};
+}
+
 // The scales of a row's groups of a unit (256 k, or kSpan), as they are in memory until they are used: a
 // conversion next to the load would wait for it.
 template <int kScale, int kGroup, int kSpan = kUnit>
@@ -169,11 +188,11 @@ __device__ __forceinline__ void multiply_unit(const uint8_t* const (&codes)[kMat
 #pragma unroll
         for (int c = 0; c < kMats; ++c) {
           const f32x4 zero = {};
-          sum[c] = T::mfma(v, decode8<T>(word[c][m], 1.0f), m % kPer == 0 ? zero : sum[c]);
+          const ScaleParts f = parts_of<kWide<T>>(scale[c].get(4 * h + m));
+          sum[c] = T::mfma(v, decode8<T>(word[c][m], f.inside), m % kPer == 0 ? zero : sum[c]);
           if (m % kPer == kPer - 1) {
-            const float f = scale[c].get(4 * h + m);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[c][r] += f * sum[c][r];
+            for (int r = 0; r < 4; ++r) acc[c][r] += f.rest * sum[c][r];
           }
         }
       }
@@ -442,10 +461,13 @@ __global__ __launch_bounds__(512) void w4_kernel(W4Product p, int parts, int rin
 // Many tokens: a tile of 64 rows and 64 tokens a workgroup, all of K, 128 at a time through three
 // stages of LDS. A wave has 16 rows for all the tokens, so that a code is converted once for 64.
 // Bound by the conversions and the matrix instructions of a wave, one after the other: 64 tokens, both
-// projections of 8192 -> 16384, 71 us, 0.48 PFLOP/s.
+// projections of 8192 -> 16384, 61 us, 0.56 PFLOP/s.
 constexpr int kStep = 128, kTileTokens = 64, kTileWaves = 4;
+// Two workgroups on a CU where the registers for groups' sums and scales allow it.
+template <int kScale, int kGroup, bool kGated>
+constexpr int kTilesOnCU = kScale == HOBFLOPS_SCALE_POW2 || kGroup == 128 || (kGroup == 64 && !kGated) ? 2 : 1;
 template <class T, int kScale, int kGroup, bool kGated>
-__global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
+__global__ __launch_bounds__(64 * kTileWaves, (kTilesOnCU<kScale, kGroup, kGated>)) void w4_tile_kernel(W4Product p) {
 #ifdef __HIP_DEVICE_COMPILE__
   typedef typename T::vec8 Vec;
   typedef Scales<kScale, kGroup, kStep> Sc;
@@ -490,8 +512,8 @@ __global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
                                                in ? (uint32_t)t * ld2 + (uint32_t)k * 2 : 0x80000000u, 0, 0, 0);
     }
   };
-  f32x4 acc[kMats][NT] = {};
-  const auto multiply = [&](int stage, const Sc(&s)[kMats]) {
+  f32x4 acc[kMats][NT];
+  const auto multiply = [&](auto split, int stage, const Sc(&s)[kMats]) {
     uint32_t word[kMats][4];
     bool exact = true;
 #pragma unroll
@@ -522,8 +544,12 @@ __global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         Vec w[kMats];
+        ScaleParts f[kMats];
 #pragma unroll
-        for (int c = 0; c < kMats; ++c) w[c] = decode8<T>(word[c][m], 1.0f);
+        for (int c = 0; c < kMats; ++c) {
+          f[c] = parts_of<decltype(split)::value>(s[c].get(m));
+          w[c] = decode8<T>(word[c][m], f[c].inside);
+        }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           const Vec v = x(m, j);
@@ -535,13 +561,11 @@ __global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
         }
         if (m % kPer == kPer - 1) {
 #pragma unroll
-          for (int c = 0; c < kMats; ++c) {
-            const float f = s[c].get(m);
+          for (int c = 0; c < kMats; ++c)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[c][j][r] += f * sum[c][j][r];
-          }
+              for (int r = 0; r < 4; ++r) acc[c][j][r] += f[c].rest * sum[c][j][r];
         }
       }
     }
@@ -550,18 +574,37 @@ __global__ __launch_bounds__(64 * kTileWaves) void w4_tile_kernel(W4Product p) {
   // passed. Its wait counts the loads into LDS alone; the scales' loads between them only make it
   // stricter. Steps beyond the last are of zeros.
   const int steps = (K + kStep - 1) / kStep;
+  const auto sum_up = [&](auto split) {
 #pragma unroll
-  for (int i = 0; i < S - 1; ++i) load(i, i, scale[i]);
-  for (int k = 0; k < steps; k += S) {
+    for (int c = 0; c < kMats; ++c)
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kMats + kXLoads))
-                   : "memory");
-      load(k + i + S - 1, (i + S - 1) % S, scale[(i + S - 1) % S]);
-      multiply(i, scale[i]);
+      for (int j = 0; j < NT; ++j) acc[c][j] = f32x4{};
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) load(i, i, scale[i]);
+    for (int k = 0; k < steps; k += S) {
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kMats + kXLoads))
+                     : "memory");
+        load(k + i + S - 1, (i + S - 1) % S, scale[(i + S - 1) % S]);
+        multiply(split, i, scale[i]);
+      }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // LDS becomes another workgroup's, or these sums' again
+  };
+  sum_up(std::false_type());
+  if constexpr (kWide<T>) {
+    // The scales in two factors only where a sum is not finite, all of it again: in every sum they would cost
+    // more here (64 tokens, both projections of 8192 -> 16384 in groups of 32: 111 us, not 100).
+    float z = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kMats; ++c)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z = __builtin_fmaf(acc[c][j][r], 0.0f, z);
+    if (__syncthreads_or(z != z)) sum_up(std::true_type());
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // LDS becomes another workgroup's
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     f32x4 y[kMats];
@@ -600,7 +643,7 @@ void launch_tiles(const W4Product& p, hipStream_t stream) {
   const int64_t tiles = (p.N + 15) / 16, parts = (p.T + 15) / 16;
   const int units = (int)((p.K + kUnit - 1) / kUnit), tokens = (int)(p.T < 16 ? p.T : 16);
   // Tokens in tiles of 64 where that leaves a workgroup for half of the CUs: 64 tokens, both projections of
-  // 8192 -> 16384: 71 us against 236 in tokens of 16; with 64 workgroups (4096 -> 4096) 22.6 against 19.4.
+  // 8192 -> 16384: 61 us against 236 in tokens of 16; with 64 workgroups (4096 -> 4096) 22.6 against 19.4.
   const int64_t many = (p.T + kTileTokens - 1) / kTileTokens, rows = (p.N + 16 * kTileWaves - 1) / (16 * kTileWaves);
   if (p.T > 16 && rows * many >= kCUs / 2) {
     w4_tile_kernel<T, kScale, kGroup, kGated>
