@@ -21,7 +21,8 @@
  *  - Pointers are device pointers (HBM) owned by the caller; the library
  *    allocates no device memory. Inputs and outputs of one call must not
  *    overlap. Pointers must be 4-byte aligned, unless a call says otherwise.
- *  - `stream` is a hipStream_t (NULL = the default stream). Calls enqueue work
+ *  - `stream` is a hipStream_t (NULL = the default stream) of the current device,
+ *    which is the one that the pointers belong to. Calls enqueue work
  *    on it and return without synchronising.
  *  - Arguments are checked before anything is launched; a rejected call
  *    launches nothing and returns a negative status (see below).

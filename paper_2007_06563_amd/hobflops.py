@@ -153,8 +153,18 @@ def _require(t, nbytes, name):
         raise ValueError(f"{name}: {have} bytes, the call needs {nbytes}")
 
 
-def _stream(t):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+def _call(device, function, *args):
+    """function(*args, stream) on the device's current stream, with the device as the current one: a
+    launch on the default stream goes to whichever device is current. (The raw handle:
+    torch.cuda.current_stream would make an object of it, at 2 us a call.)"""
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch._C._cuda_getDevice() == device.index:
+        rc = function(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args, stream)
+    if rc:
+        _check(rc)
 
 
 def plane_words(rows, length, f):
@@ -186,7 +196,7 @@ def pack(src, f, rows=None, length=None, out=None):
     if out is None:
         out = torch.empty(plane_shape(rows, length, f), dtype=torch.int32, device=src.device)
     _require(out, 4 * plane_words(rows, length, f), "pack out")
-    _check(lib().hobflops_pack(_ptr(src), kind, rows, length, f, _ptr(out), _stream(src)))
+    _call(src.device, lib().hobflops_pack, _ptr(src), kind, rows, length, f, _ptr(out))
     return out
 
 
@@ -217,7 +227,7 @@ def pack_batch(items, f):
         return outs
     arr = (PackJob * len(jobs))(*jobs)
     first = items[0][0] if isinstance(items[0], (tuple, list)) else items[0]
-    _check(lib().hobflops_pack_batch(arr, len(jobs), f, _stream(first)))
+    _call(first.device, lib().hobflops_pack_batch, arr, len(jobs), f)
     return outs
 
 
@@ -230,7 +240,7 @@ def unpack(planes, rows, length, f, kind="f32", out=None):
                           device=planes.device)
     _require(planes, 4 * plane_words(rows, length, f), "unpack planes")
     _require(out, 4 * rows * length, "unpack out")
-    _check(lib().hobflops_unpack(_ptr(planes), rows, length, f, k, _ptr(out), _stream(planes)))
+    _call(planes.device, lib().hobflops_unpack, _ptr(planes), rows, length, f, k, _ptr(out))
     return out
 
 
@@ -267,7 +277,7 @@ def conv2d(ifm, w, d, out=None):
     -> ofm planes [N*OH*OW, ceil(M/32), NB_out]; with d.ofm_kind OFM_F32 / OFM_CODE,
     float32 values / int32 codes [N*OH*OW, M]."""
     out = _conv_out(ifm, w, d, out)
-    _check(lib().hobflops_conv2d(_ptr(ifm), _ptr(w), _ptr(out), ctypes.byref(d), _stream(ifm)))
+    _call(ifm.device, lib().hobflops_conv2d, _ptr(ifm), _ptr(w), _ptr(out), ctypes.byref(d))
     return out
 
 
@@ -306,8 +316,8 @@ def conv2d_on_values(ifm, w, d, tile, out=None):
     """conv2d on float32 values in the given tile (TILE_*), whichever kernel
     ALGO_AUTO would pick: the same results."""
     out = _conv_out(ifm, w, d, out)
-    _check(lib().hobflops_conv2d_on_values(_ptr(ifm), _ptr(w), _ptr(out), ctypes.byref(d), tile,
-                                           _stream(ifm)))
+    _call(ifm.device, lib().hobflops_conv2d_on_values, _ptr(ifm), _ptr(w), _ptr(out), ctypes.byref(d),
+          tile)
     return out
 
 
@@ -319,8 +329,8 @@ def muladd(a, b, c, n, in_fmt, acc_fmt, out=None, round=ROUND_NEAREST_EVEN):
     for t, name in ((a, "a"), (b, "b"), (c, "c")):
         _require(t, 4 * plane_words(1, n, in_fmt), f"muladd {name}")
     _require(out, 4 * plane_words(1, n, acc_fmt), "muladd out")
-    _check(lib().hobflops_muladd(_ptr(a), _ptr(b), _ptr(c), _ptr(out), n, in_fmt, acc_fmt, round,
-                                 _stream(a)))
+    _call(a.device, lib().hobflops_muladd, _ptr(a), _ptr(b), _ptr(c), _ptr(out), n, in_fmt, acc_fmt,
+          round)
     return out
 
 
@@ -347,8 +357,8 @@ def avgpool(planes, N, H, W, C, in_fmt, acc_fmt, out_fmt, out=None, round=ROUND_
     if N > 0 and H > 0 and W > 0 and C > 0:
         _require(planes, 4 * plane_words(N * H * W, C, in_fmt), "avgpool planes")
         _require(out, 4 * plane_words(N, C, out_fmt), "avgpool out")
-    _check(lib().hobflops_avgpool(_ptr(planes), _ptr(out), N, H, W, C, in_fmt, acc_fmt, out_fmt,
-                                  round, _stream(planes)))
+    _call(planes.device, lib().hobflops_avgpool, _ptr(planes), _ptr(out), N, H, W, C, in_fmt, acc_fmt,
+          out_fmt, round)
     return out
 
 
@@ -431,12 +441,6 @@ def _out_rows(t, shape, dtype, device, name):
     return t, ptr, ld
 
 
-def _raw_stream(device):
-    """The handle of torch's current stream (torch.cuda.current_stream would make an object of it,
-    at 2 us a call)."""
-    return torch._C._cuda_getCurrentRawStream(device.index)
-
-
 def block_shapes(rows, cols, f, group=32):
     """The shapes of the codes and of the scales of a [rows, cols] matrix in blocks."""
     bits = 1 + sum(f) if isinstance(f, tuple) else 1 + f.wE + f.wF
@@ -467,10 +471,7 @@ def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
         ps = scales.data_ptr()
     else:
         ps = _dense(scales, sshape, stype, dev, "block_pack scales")
-    rc = lib().hobflops_block_pack(ptr, kind, rows, cols, ld, f, group, scale, pc, ps,
-                                   _raw_stream(dev))
-    if rc:
-        _check(rc)
+    _call(dev, lib().hobflops_block_pack, ptr, kind, rows, cols, ld, f, group, scale, pc, ps)
     return codes, scales
 
 
@@ -488,10 +489,8 @@ def block_unpack(codes, scales, cols, f, group=32, dtype=torch.float32, out=None
     if out is not None:
         dtype = out.dtype
     out, ptr, ld = _out_rows(out, (rows, cols), dtype, dev, "block_unpack out")
-    rc = lib().hobflops_block_unpack(pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
-                                     _type(out, "block_unpack out"), ld, _raw_stream(dev))
-    if rc:
-        _check(rc)
+    _call(dev, lib().hobflops_block_unpack, pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
+          _type(out, "block_unpack out"), ld)
     return out
 
 
@@ -538,16 +537,14 @@ def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
     d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f,
                   _align(px, pg, pu))
     ws, pw, nw = _workspace(d, 0, x.device)
-    stream = _raw_stream(x.device)
+    forward = lib().hobflops_gated_forward
     if ckpt is None:
-        _check(lib().hobflops_gated_forward(ctypes.byref(d), px, pg, pu, ph, None, None, None,
-                                            None, pw, nw, stream))
+        _call(x.device, forward, ctypes.byref(d), px, pg, pu, ph, None, None, None, None, pw, nw)
         return h
     cshape, sshape = block_shapes(T, F, f)
     blocks = [torch.empty(s, dtype=torch.uint8, device=x.device)
               for s in (cshape, sshape, cshape, sshape)]
-    _check(lib().hobflops_gated_forward(ctypes.byref(d), px, pg, pu, ph,
-                                        *[b.data_ptr() for b in blocks], pw, nw, stream))
+    _call(x.device, forward, ctypes.byref(d), px, pg, pu, ph, *[b.data_ptr() for b in blocks], pw, nw)
     return h, GatedSaved(block_pack(x, f), tuple(blocks[:2]), tuple(blocks[2:]), f)
 
 
@@ -570,9 +567,8 @@ def gated_backward(dh, saved, w_gate, w_up, act=GATE_SILU):
     dx = torch.empty((T, D), dtype=dtype, device=dev)
     dw_gate = torch.empty((F, D), dtype=dtype, device=dev)
     dw_up = torch.empty((F, D), dtype=dtype, device=dev)
-    _check(lib().hobflops_gated_backward(ctypes.byref(d), ph, *ptrs, pg, pu, dx.data_ptr(),
-                                         dw_gate.data_ptr(), dw_up.data_ptr(), pw, nw,
-                                         _raw_stream(dev)))
+    _call(dev, lib().hobflops_gated_backward, ctypes.byref(d), ph, *ptrs, pg, pu, dx.data_ptr(),
+          dw_gate.data_ptr(), dw_up.data_ptr(), pw, nw)
     return dx, dw_gate, dw_up
 
 
@@ -591,23 +587,19 @@ def _w4(x, weights, group, out, name):
             for i, w in enumerate(weights)]
     y, py, ldy = _out_rows(out, (T, N), x.dtype, dev, name)
     return (y, (px, _type(x, name), T, K, N, ldx, *ptrs, group, _SCALES[scale]),
-            (py, ldy, _raw_stream(dev)))
+            (py, ldy))
 
 
 def w4_linear(x, codes, scales, group=32, out=None):
     """y = x W^T for few tokens: x [T, K] bfloat16 or float16, W [N, K] as 4-bit codes and scales
     (block_pack with the format (2, 1)) -> y [T, N]."""
     y, head, tail = _w4(x, (codes, scales), group, out, "w4_linear")
-    rc = lib().hobflops_w4_linear(*head, *tail)
-    if rc:
-        _check(rc)
+    _call(x.device, lib().hobflops_w4_linear, *head, *tail)
     return y
 
 
 def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, out=None):
     """h = act(x Wg^T) * (x Wu^T) for few tokens, both weights as 4-bit codes and scales."""
     y, head, tail = _w4(x, (g_codes, g_scales, u_codes, u_scales), group, out, "w4_gated")
-    rc = lib().hobflops_w4_gated(*head, act, *tail)
-    if rc:
-        _check(rc)
+    _call(x.device, lib().hobflops_w4_gated, *head, act, *tail)
     return y
