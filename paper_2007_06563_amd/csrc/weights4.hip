@@ -202,13 +202,13 @@ __device__ __forceinline__ void multiply_unit(const uint8_t* const (&codes)[kMat
 
 // A load into LDS, 16 bytes a lane, at `lds` on; zeros from offsets out of the descriptor's range. These are
 // assembly since the compiler, which knows what a load into LDS is, would wait for all of them
-// before each read of LDS; loaded() is the wait. (M0, the target's place, has no other use here.)
+// before each read of LDS; loaded() is the wait. M0 is the target's place.
 __device__ __forceinline__ void load_lds(u32x4v rows, uint32_t off, const uint8_t* to) {
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(lds), "v"(off), "s"(rows)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void loaded() {
   __builtin_amdgcn_s_waitcnt(0x0070);  // no load and no LDS read under way; the compiler counts this one
