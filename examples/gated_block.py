@@ -16,6 +16,7 @@ import os
 import sys
 
 import torch
+from torch.autograd.function import once_differentiable
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
@@ -27,7 +28,8 @@ E4M3, E2M1 = (4, 3), (2, 1)
 
 
 class Gated(torch.autograd.Function):
-    """act(x w_gate^T) * (x w_up^T), whose backward pass starts from 8-bit checkpoints."""
+    """act(x w_gate^T) * (x w_up^T), whose backward pass starts from 8-bit checkpoints. It has no second
+    derivative: asking for one is an error."""
 
     @staticmethod
     def forward(ctx, x, w_gate, w_up):
@@ -37,6 +39,7 @@ class Gated(torch.autograd.Function):
         return h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         t = ctx.saved_tensors
         saved = hf.GatedSaved(t[0:2], t[2:4], t[4:6], ctx.fmt)
