@@ -8,6 +8,7 @@ Plane tensors are int32 (the bit patterns of PL32 words).
 import collections
 import ctypes
 import os
+import warnings
 
 import torch
 
@@ -515,6 +516,14 @@ def _align(*ptrs):
     return bits & -bits
 
 
+def _no_gradient(name, *tensors):
+    """Says that autograd records nothing of a call whose inputs it follows."""
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        warnings.warn(f"{name}: its result carries no gradient to its inputs; wrap it in a "
+                      "torch.autograd.Function (gated_backward has the gated block's gradients), or "
+                      "call it under torch.no_grad()", stacklevel=3)
+
+
 def _workspace(d, backward, device):
     n = ctypes.c_int64()
     _check(lib().hobflops_gated_workspace(ctypes.byref(d), backward, ctypes.byref(n)))
@@ -527,11 +536,12 @@ def _workspace(d, backward, device):
 def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
     """h = act(x w_gate^T) * (x w_up^T): x [T, D], w_gate and w_up [F, D], bfloat16 or float16 ->
     h [T, F]. With ckpt, an 8-bit format: (h, saved), the blocks of x, g and u in that format, for
-    gated_backward."""
+    gated_backward. Autograd records nothing of it."""
     px, T, D, ldx = _rows(x, "gated_forward x")
     pg, pu, F, Dw, ldw = _gated_weights(x, w_gate, w_up)
     if Dw != D:
         raise ValueError("gated_forward: x and the weights differ in D")
+    _no_gradient("gated_forward", x, w_gate, w_up)
     h, ph, ldh = _out_rows(out, (T, F), x.dtype, x.device, "gated_forward out")
     f = Fmt(0, 0) if ckpt is None else fmt(ckpt)
     d = GatedDesc(T, D, F, ldx, ldw, ldh, _type(x, "gated_forward x"), act, f,
@@ -594,6 +604,7 @@ def w4_linear(x, codes, scales, group=32, out=None):
     """y = x W^T for few tokens: x [T, K] bfloat16 or float16, W [N, K] as 4-bit codes and scales
     (block_pack with the format (2, 1)) -> y [T, N]."""
     y, head, tail = _w4(x, (codes, scales), group, out, "w4_linear")
+    _no_gradient("w4_linear", x)
     _call(x.device, lib().hobflops_w4_linear, *head, *tail)
     return y
 
@@ -601,5 +612,6 @@ def w4_linear(x, codes, scales, group=32, out=None):
 def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, out=None):
     """h = act(x Wg^T) * (x Wu^T) for few tokens, both weights as 4-bit codes and scales."""
     y, head, tail = _w4(x, (g_codes, g_scales, u_codes, u_scales), group, out, "w4_gated")
+    _no_gradient("w4_gated", x)
     _call(x.device, lib().hobflops_w4_gated, *head, act, *tail)
     return y
