@@ -375,7 +375,9 @@ int hobflops_gated_forward(const hobflops_gated_desc* d, const void* x, const vo
  * all dense and of d->type. dg, du and the values of x's blocks are rounded to d->type
  * before the products, whose sums are float32. Blocks of x of d->type hold values of that type, but for
  * 2^16 in float16 (|x| >= 63488 becomes it in (4, 3), >= 61440 in (5, 2)) and 2^128 in bfloat16 (likewise):
- * the type's largest value is taken for them. With T = 0 the gradients of the weights are zero.
+ * the type's largest value is taken for them. In float16 |dg| and |du| above 65504 become
+ * infinite and those below 2^-14 lose digits; gradients are linear in dh, so that a power of two on dh, and
+ * its inverse on the gradients, brings them into range. With T = 0 the gradients of the weights are zero.
  * Sums run in a fixed order: the same inputs give the same bits. */
 int hobflops_gated_backward(const hobflops_gated_desc* d, const void* dh, const uint8_t* x_codes,
                             const uint8_t* x_scales, const uint8_t* g_codes,

@@ -8,7 +8,14 @@
 //
 // Roundings to 16 bits: h once, from float32 products; dg, du and the values of x's blocks, as operands
 // of the matrix instruction; dx and the weights' gradients once, from float32 sums. g and u in float32
-// become 8-bit blocks directly. Every sum has a fixed order: results do not change between runs.
+// become 8-bit blocks directly.
+//
+// dg and du as one operand each: training steps are 0.0024 of their outputs' size off 64 bits in bfloat16,
+// 0.0003 in float16, of which the outputs' own rounding is 0.0017 and 0.0002. Two operands each (the
+// rounded value and what it leaves) would double the products, 1.1 ms of a step of 4096 x 4096 x 11264, which takes 1.8.
+// In float16 dg and du also have its range; gradients are linear in dh, whose scale is the caller's.
+//
+// Every sum has a fixed order: results do not change between runs.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -225,9 +232,10 @@ __device__ __forceinline__ void forward_tile(const ForwardArgs& p, uint8_t* cons
 }
 
 // 256 x 256 sums a workgroup, 128 of each projection, one workgroup of eight waves on a CU. Bound by the matrix
-// instructions, which are busy 76 % of the time: 8192 x 4096 x 11264 in 1.10 ms, 1.38 PFLOP/s. Without any
-// LDS bank conflict; HBM reads are those of a library product of these sizes, which takes 0.95 ms without the
-// activation.
+// instructions, which are busy 73 % of the time: 8192 x 4096 x 11264 in 1.09 ms, 1.38 PFLOP/s, without any
+// LDS bank conflict. (A library product of these sizes, without the activation: 0.95 ms.) With checkpoints 62 %:
+// 4096 x 4096 x 11264 in 635 us, without 569; 1408 tiles are 5.5 rounds and take 6, and a
+// tile's blocks are formed and stored with nothing beside them.
 template <class T, int kFmt>
 __global__ __launch_bounds__(512, 2) void forward_kernel(ForwardArgs p) {
   HOBFLOPS_STAGES2(256, 256);
@@ -235,7 +243,7 @@ __global__ __launch_bounds__(512, 2) void forward_kernel(ForwardArgs p) {
 }
 // 128 x 64 sums, where large tiles would be too few: two workgroups on a CU, three stages. Bound by the reads of the
 // weights for few tokens (1 x 4096 x 11264: 39 us, 4.7 TB/s), by latency, of LDS too, in between
-// (333 x 1000 x 2730: 17.5 us, of which 5 for the first and last step, 0.7 a step of 64 k).
+// (333 x 1000 x 2730: 18.0 us, of which 5 for the first and last step, 0.7 a step of 64 k).
 template <class T, int kFmt>
 __global__ __launch_bounds__(256, 2) void forward_small_kernel(ForwardArgs p) {
   HOBFLOPS_STAGES3(128, 64);
@@ -468,7 +476,7 @@ __device__ __forceinline__ void unpack_of(const UnpackArgs& p, int64_t i, int64_
 }
 
 // What the gradients' products read, in one launch. Bound by HBM: 4096 x 4096 x 11264 reads 208 and
-// writes 218 MB (by the counters) in 71 us. (Forming dg and du where the products load them would do that once for every
+// writes 218 MB (by the counters) in 73 us. (Forming dg and du where the products load them would do that once for every
 // 256 columns, and their tiles go into LDS past the registers.) With a launch for each of the three, a short step's took 3 us more. The first workgroups write dg and du, the next the values of
 // x, the last the weights' rows if they must be aligned.
 template <class T, int kFmt>
@@ -523,7 +531,8 @@ ForwardPlan plan_forward(const hobflops_gated_desc& d) {
 // more in float32, 4 TB/s, and joined in a launch. Measured, us: dx 1000 x 4096, sums of 22528, in
 // one part 222 (128 x 128), in parts 180 (256 x 256); 333 x 4096, in 128 x 128: one part 118, parts 97;
 // 3000 x 2048, sums of 11264: 128 x 128 one on a CU 183, two 138; dW of 1000 x 4096 x 22528: 256 x 256 172,
-// 128 x 128 191, of 1 x 512 x 2816 7.5 and 5.5.
+// 128 x 128 191, of 1 x 512 x 2816 7.5 and 5.5. The weights' sum over T is never in parts: of small weights a
+// few workgroups walk all of it, and a backward pass of 8192 x 256 x 512 takes 85 us, of 8192 x 512 x 1408 119.
 struct Tiling {
   bool small;
   int splits;
@@ -588,7 +597,9 @@ void forward_tiles(ForwardArgs& p, hipStream_t s) {
   // Large tiles where there are about as many as 160: with 176 (512, or 333, x 4096 x 11264) 105 and 100 us against the
   // small ones' 141 and 111, with 88 (1 x 4096 x 11264) 89 against 44. The smallest where small ones leave half of the
   // CUs without one: with 88 of them (1 x 2048 x 5632) 17.0 us against 19.0, with 176 (128 x 2048 x 5632) 22.4
-  // against 20.3.
+  // against 20.3. The rule does not look at T or K: few tokens of more than 20352 rows go to the large tiles as
+  // well, 1 x 4096 x 20480 in 103 us where 20352 rows take 71 in the small ones, and few tiles walk a long K alone,
+  // 1 x 8192 x 512 in 28 us.
   const int64_t big = ((p.F + 127) / 128) * ((p.T_ + 255) / 256);
   const int64_t small = ((p.F + 63) / 64) * ((p.T_ + 63) / 64);
   if (big >= 160) {

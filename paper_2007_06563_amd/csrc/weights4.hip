@@ -296,7 +296,7 @@ __device__ __forceinline__ int part_of(int units, int wave, int waves) { return 
 // x of all K fits LDS: as many workgroups as run at a time, each with the tiles (16 rows) that are
 // `stride` apart. x is loaded once; a tile's codes and scales are under way while the tile before is
 // multiplied.
-// Bound by HBM and, in short calls, by latency: 5 x 4104 -> 50257 in 35 us, 3.3 TB/s of codes, scales and y; one token,
+// Bound by HBM and, in short calls, by latency: 5 x 4104 -> 50257 in 36 us, 3.2 TB/s of codes, scales and y; one token,
 // both projections of 4096 -> 11264, 12.6 us, 3.9 TB/s; 4096 -> 4096 in 5.8 us, mostly a
 // launch and the loads' latency. With codes from global memory to registers (16 lines of 16 bytes a load) the
 // first two took 47 and 14.5 us.
@@ -387,7 +387,8 @@ __global__ __launch_bounds__(1024) void w4_stream_kernel(W4Product p, int parts,
 
 // An x that does not fit: a workgroup of eight waves a tile. The codes of up to `ring` units of a wave are
 // under way at a time; x comes a unit at a time, a unit ahead where LDS has two places for it.
-// 16 x 11264 -> 4096 in 12.8 us, 2.0 TB/s: a workgroup a CU and one tile each, so start and end count in full.
+// 16 x 11264 -> 4096 in 13.0 us, 1.9 TB/s: a workgroup a CU and one tile each, so start and end count in full, and
+// each reads all of x, four times the bytes of its codes, from L2.
 template <class T, int kScale, int kGroup, bool kGated>
 __global__ __launch_bounds__(512) void w4_kernel(W4Product p, int parts, int ring, int places) {
 #ifdef __HIP_DEVICE_COMPILE__
