@@ -400,6 +400,115 @@ int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, 
                       const void* u_scales, int group, int scale, int act, void* h, int64_t ldh,
                       void* stream);
 
+/* ---- Around the gated block in a training step: layer norm, a linear layer, AdamW ----
+ *
+ * Layer norm of the rows of x [rows][cols] (rows ldx apart), rows >= 0, cols >= 1:
+ *   mean, var: of a row's values (var their mean squared distance from the mean),
+ *   rstd = 1 / sqrt(var + eps), y = (x - mean) rstd weight + bias
+ * x and y (rows ldy apart) of `type`, weight and bias [cols] of `wtype`: `type` or float32; NULL: 1 and 0.
+ * Sums in float32, one rounding at the end. Any finite row has its result, also where its squares pass
+ * float32's range; NaN and infinities make their own row NaN. With eps 0 a row of one value has rstd
+ * infinity and is NaN. y may be x. mean and rstd, float32 [rows], are for the backward pass
+ * (both or neither NULL). */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ldx, ldy, ld_add; /* ldy: rows of y, or of its gradient dy */
+  int type, wtype;
+  double eps;
+} hobflops_norm_desc;
+int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* weight,
+                        const void* bias, void* y, float* mean, float* rstd, void* stream);
+
+/* Its gradients from dy, with a = dy weight, xh = (x - mean) rstd:
+ *   dx = rstd (a - mean(a) - xh mean(a xh)) + add, dweight = sum over rows of dy xh,
+ *   dbias = sum over rows of dy
+ * add (rows ld_add apart; NULL: none): a gradient that reaches x past the norm, joined before the one rounding. dx is
+ * dense, and may be add (dense, then), but not x or dy. dweight and dbias of wtype, either may be NULL. Sums run in a
+ * fixed order. The workspace is needed where one of these two is asked for. */
+int hobflops_layer_norm_workspace(const hobflops_norm_desc* d, int64_t* bytes);
+int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, const void* x,
+                                 const void* weight, const float* mean, const float* rstd,
+                                 const void* add, void* dx, void* dweight, void* dbias,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+
+/* A linear layer with its epilogue, T tokens (T >= 0):
+ *   z = x w^T + bias, y = act(z) + residual
+ * x [T][K] (rows ldx apart), w [N][K] (ldw), bias [N], residual [T][N] (ldr) and y [T][N] (ldy) of type
+ * bfloat16 or float16; bias and residual may be NULL. act: HOBFLOPS_GATE_*, or HOBFLOPS_GATE_NONE: z itself.
+ * Sums, z and the activation in float32, one rounding at the end. y may be the residual (same rows). z, if
+ * not NULL, receives z [T][N], dense, rounded to the type: what the backward pass needs of an activation.
+ * With align 16 and K, ldx and ldw multiples of 8 the kernels read x and w in place; else a call of more than a few
+ * tokens copies what it must into the workspace first. */
+enum { HOBFLOPS_GATE_NONE = -1 };
+enum { HOBFLOPS_NEED_DX = 1, HOBFLOPS_NEED_DW = 2, HOBFLOPS_NEED_DBIAS = 4 };
+typedef struct {
+  int64_t T, K, N;
+  int64_t ldx, ldw, ldy, ldr; /* ldy: rows of y, or of its gradient dy */
+  int type, act;
+  int align; /* bytes that the pointers of x, w and dy are aligned to: 2, 4, 8 or 16 */
+} hobflops_linear_desc;
+
+/* Workspace bytes of a forward call (need 0) or of a backward call that is asked for the gradients in need
+ * (HOBFLOPS_NEED_*, at least one). */
+int hobflops_linear_workspace(const hobflops_linear_desc* d, int need, int64_t* bytes);
+int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w, const void* bias,
+                    const void* residual, void* y, void* z, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+
+/* Gradients from dy [T][N] (rows ldy apart) and z:
+ *   dz = dy act'(z) (act' of max(z, 0) is 0 at 0), dx = dz w [T][K], dw = dz^T x [N][K], dbias = sum over tokens of dz
+ * all dense and of d->type; those that are NULL are not computed. The residual's gradient is dy. dz is rounded
+ * to d->type before the products (dbias is summed before that), whose sums are float32. z is needed with an
+ * activation, x for dw, w for dx. With T = 0 dw and dbias are zero. Sums run in a fixed order. */
+int hobflops_linear_backward(const hobflops_linear_desc* d, const void* dy, const void* x,
+                             const void* w, const void* z, void* dx, void* dw, void* dbias,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
+/* An AdamW step over many tensors at once. For each value, in float32, every operation rounded (none joined
+ * into a multiply-add), t the step's number, from 1 on:
+ *   g' = g grad_scale
+ *   m = m beta1 + g' (1 - beta1),  v = v beta2 + (g' g') (1 - beta2)
+ *   p = p (1 - lr weight_decay) - m / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps) (lr / (1 - beta1^t))
+ * the factors in parentheses without p, m, v computed in float64 and rounded once. A copy of p in 16 bits, rounded to
+ * nearest, can be written with it.
+ *
+ * The states m and v of all tensors are flat: tensor i's n values begin where those of the tensors before it,
+ * each rounded up to a multiple of 32, end (hobflops_adamw_state_len). With states in {0, 0}: float32, m_scales and
+ * v_scales not used. With states (4, 3) or (5, 2): blocks of 32 values as above (uint8 codes [len], power-of-two scales
+ * [len / 32]) of m and of r = sqrt(v); the step takes v = r r. Zero codes are zeros: a state begins as zeroed
+ * memory. The scale 2^k has the smallest k >= -110 for which no finite value of the group is larger than the
+ * format's largest. Between two codes a value goes to the upper one (by magnitude) where its share of the way is over u; m's share is of
+ * m, r's of r^2, so that m and v keep their means; r > 0 becomes the least code where it would become 0. u = (h + 1/2) / 65536 with 16 bits h
+ * of a counter's, the lower ones for m, the upper ones for r:
+ *   stir(x): x = (x ^ x >> 15) 0xBB67AE85; x = (x ^ x >> 13) 0x6A09E667; x ^ x >> 16   (32 bits)
+ *   key: 0; key = stir(key ^ word) for the words low t, high t, low seed, high seed
+ *   bits of place i of the states: stir(low(i) 0x9E3779B9 + (key ^ high(i) 0x6A09E667))
+ *
+ * lr_at, step_at, grad_scale_at: where not NULL, device memory that holds the value instead, so that a captured graph can
+ * be replayed with others. skip_at: a device float32; where it is not 0 the step changes nothing. Memory that the step writes
+ * must not overlap any other of its tensors (HOBFLOPS_EINVAL). */
+typedef struct {
+  float* p;
+  const void* g; /* NULL: the tensor and its states stay as they are */
+  void* copy;    /* NULL: none */
+  int64_t n;
+} hobflops_adamw_tensor;
+typedef struct {
+  int grad_type, copy_type; /* of g: any type; of the copies: bfloat16 or float16 */
+  hobflops_fmt states;
+  double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps >= 0 */
+  int64_t step;
+  uint64_t seed;
+  const float* lr_at;
+  const int64_t* step_at;
+  const float* grad_scale_at;
+  const float* skip_at;
+} hobflops_adamw_desc;
+int hobflops_adamw_state_len(const hobflops_adamw_tensor* tensors, int count, int64_t* len);
+int hobflops_adamw(const hobflops_adamw_desc* d, const hobflops_adamw_tensor* tensors, int count,
+                   void* m, uint8_t* m_scales, void* v, uint8_t* v_scales, int64_t state_len,
+                   void* stream);
+
 /* Text for a status code; for HOBFLOPS_EHIP, the last HIP error of this
  * thread. The pointer stays valid until the next call on the same thread. */
 const char* hobflops_status_string(int status);

@@ -755,7 +755,8 @@ def build(jobs=None, verbose=True):
     """Generate and compile everything; returns the library path."""
     gen_files = generate(verbose=verbose)
     srcs = [os.path.join(HERE, "csrc", n) for n in
-            ("abi.hip", "pack.hip", "block.hip", "gated.hip", "weights4.hip")] + gen_files
+            ("abi.hip", "pack.hip", "block.hip", "gated.hip", "weights4.hip", "norm.hip", "linear.hip",
+             "adamw.hip")] + gen_files
     os.makedirs(OBJ, exist_ok=True)
     jobs = jobs or min(16, os.cpu_count() or 4)
     stats = {}

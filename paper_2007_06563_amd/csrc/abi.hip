@@ -4,8 +4,10 @@
 // the kernels.
 #include <hip/hip_runtime.h>
 #include <limits.h>
+#include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <atomic>
@@ -230,6 +232,59 @@ int w4_run(W4Product p, bool gated, void* stream) {
       (gated && !aligned_to(p.w_up.scales, sb)))
     return HOBFLOPS_EALIGN;
   return hip_status(launch_w4(p, (hipStream_t)stream));
+}
+
+int align_ok(int align) { return align == 2 || align == 4 || align == 8 || align == 16; }
+
+int norm_check(const hobflops_norm_desc* d) {
+  if (!d) return HOBFLOPS_EINVAL;
+  if (d->cols < 1 || !extent_ok(d->rows, d->cols, d->ldx) || !extent_ok(d->rows, d->cols, d->ldy) ||
+      !type_ok(d->type) || !type_ok(d->wtype) || !(d->eps >= 0.0) || !isfinite(d->eps))
+    return HOBFLOPS_EINVAL;
+  return d->wtype == d->type || d->wtype == HOBFLOPS_TYPE_F32 ? HOBFLOPS_OK : HOBFLOPS_EUNSUPPORTED;
+}
+
+int linear_check(const hobflops_linear_desc* d) {
+  if (!d) return HOBFLOPS_EINVAL;
+  if (d->K < 1 || d->N < 1 || !extent_ok(d->T, d->K, d->ldx) || !extent_ok(d->N, d->K, d->ldw) ||
+      !extent_ok(d->T, d->N, d->ldy) || d->T > (int64_t)1 << 24 || d->K > (int64_t)1 << 20 ||
+      d->N > (int64_t)1 << 20)
+    return HOBFLOPS_EINVAL;
+  if (!type_ok(d->type) || d->act < HOBFLOPS_GATE_NONE || d->act > HOBFLOPS_GATE_RELU || !align_ok(d->align))
+    return HOBFLOPS_EINVAL;
+  return d->type == HOBFLOPS_TYPE_F32 ? HOBFLOPS_EUNSUPPORTED : HOBFLOPS_OK;
+}
+
+// Memory that a call writes or only reads.
+struct Range {
+  uintptr_t begin, end;
+  int written;
+};
+int range_order(const void* a, const void* b) {
+  const uintptr_t x = ((const Range*)a)->begin, y = ((const Range*)b)->begin;
+  return x < y ? -1 : x > y ? 1 : 0;
+}
+// Whether a range that is written overlaps another one; sorts them.
+int overlapping(Range* r, int64_t n) {
+  qsort(r, (size_t)n, sizeof(Range), range_order);
+  uintptr_t end = 0, written_end = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (r[i].begin < (r[i].written ? end : written_end)) return 1;
+    if (r[i].end > end) end = r[i].end;
+    if (r[i].written && r[i].end > written_end) written_end = r[i].end;
+  }
+  return 0;
+}
+
+// Length of the states of some tensors, or -1.
+int64_t state_len_of(const hobflops_adamw_tensor* t, int count) {
+  int64_t len = 0;
+  for (int i = 0; i < count; ++i) {
+    if (t[i].n < 0 || t[i].n > (int64_t)1 << 48) return -1;
+    len += (t[i].n + 31) & ~(int64_t)31;
+    if (len > (int64_t)1 << 48) return -1;
+  }
+  return len;
 }
 
 }  // namespace
@@ -716,6 +771,181 @@ int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, 
   const W4Product p{x, type, T, K, N, ldx, ldh, {g_codes, g_scales}, {u_codes, u_scales},
                     group, scale, act, h};
   return w4_run(p, true, stream);
+}
+
+int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* weight,
+                        const void* bias, void* y, float* mean, float* rstd, void* stream) {
+  const int st = norm_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  if (!mean != !rstd) return HOBFLOPS_EINVAL;
+  if (d->rows == 0) return HOBFLOPS_OK;
+  if (!x || !y) return HOBFLOPS_EINVAL;
+  const int b = type_bytes(d->type), wb = type_bytes(d->wtype);
+  if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(weight, wb) || !aligned_to(bias, wb) ||
+      !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+    return HOBFLOPS_EALIGN;
+  LayerNorm p{d->rows, d->cols, d->ldx, d->ldy, 0, d->type, d->wtype, d->eps};
+  p.x = x;
+  p.w = weight;
+  p.b = bias;
+  p.y = y;
+  p.mean = mean;
+  p.rstd = rstd;
+  return hip_status(launch_norm_forward(p, (hipStream_t)stream));
+}
+
+int hobflops_layer_norm_workspace(const hobflops_norm_desc* d, int64_t* bytes) {
+  if (!bytes) return HOBFLOPS_EINVAL;
+  const int st = norm_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  *bytes = norm_backward_workspace(d->rows, d->cols);
+  return HOBFLOPS_OK;
+}
+
+int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, const void* x,
+                                 const void* weight, const float* mean, const float* rstd,
+                                 const void* add, void* dx, void* dweight, void* dbias,
+                                 void* workspace, int64_t workspace_bytes, void* stream) {
+  const int st = norm_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  if (add && !extent_ok(d->rows, d->cols, d->ld_add)) return HOBFLOPS_EINVAL;
+  if (d->rows > 0) {
+    if (!dy || !x || !mean || !rstd || !dx) return HOBFLOPS_EINVAL;
+    if ((dweight || dbias) &&
+        (!workspace || workspace_bytes < norm_backward_workspace(d->rows, d->cols)))
+      return HOBFLOPS_EINVAL;
+  }
+  const int b = type_bytes(d->type), wb = type_bytes(d->wtype);
+  if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(add, b) || !aligned_to(dx, b) ||
+      !aligned_to(weight, wb) || !aligned_to(dweight, wb) || !aligned_to(dbias, wb) ||
+      !aligned_to(mean, 4) || !aligned_to(rstd, 4) || (d->rows > 0 && !aligned_to(workspace, 16)))
+    return HOBFLOPS_EALIGN;
+  LayerNorm p{d->rows, d->cols, d->ldx, d->ldy, d->ld_add, d->type, d->wtype, d->eps};
+  p.x = x;
+  p.w = weight;
+  p.dy = dy;
+  p.add = add;
+  p.dx = dx;
+  p.dw = dweight;
+  p.db = dbias;
+  p.mean = const_cast<float*>(mean);
+  p.rstd = const_cast<float*>(rstd);
+  p.workspace = workspace;
+  return hip_status(launch_norm_backward(p, (hipStream_t)stream));
+}
+
+int hobflops_linear_workspace(const hobflops_linear_desc* d, int need, int64_t* bytes) {
+  if (!bytes || need < 0 || need > 7) return HOBFLOPS_EINVAL;
+  const int st = linear_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  const LinearNeed n{(need & HOBFLOPS_NEED_DX) != 0, (need & HOBFLOPS_NEED_DW) != 0,
+                     (need & HOBFLOPS_NEED_DBIAS) != 0};
+  *bytes = need ? linear_backward_workspace(*d, n) : linear_forward_workspace(*d);
+  return HOBFLOPS_OK;
+}
+
+int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w, const void* bias,
+                    const void* residual, void* y, void* z, void* workspace,
+                    int64_t workspace_bytes, void* stream) {
+  const int st = linear_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  if (residual && !extent_ok(d->T, d->N, d->ldr)) return HOBFLOPS_EINVAL;
+  if (d->T == 0) return HOBFLOPS_OK;
+  if (!x || !w || !y) return HOBFLOPS_EINVAL;
+  const int64_t need = linear_forward_workspace(*d);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return HOBFLOPS_EINVAL;
+  if (!aligned_to(x, d->align) || !aligned_to(w, d->align) || !aligned_to(bias, 2) ||
+      !aligned_to(residual, 2) || !aligned_to(y, 2) || !aligned_to(z, 2) ||
+      (need > 0 && !aligned_to(workspace, 16)))
+    return HOBFLOPS_EALIGN;
+  const LinearForward p{x, w, bias, residual, y, z, workspace};
+  return hip_status(launch_linear_forward(*d, p, (hipStream_t)stream));
+}
+
+int hobflops_linear_backward(const hobflops_linear_desc* d, const void* dy, const void* x,
+                             const void* w, const void* z, void* dx, void* dw, void* dbias,
+                             void* workspace, int64_t workspace_bytes, void* stream) {
+  const int st = linear_check(d);
+  if (st != HOBFLOPS_OK) return st;
+  if (!dx && !dw && !dbias) return HOBFLOPS_EINVAL;
+  if (d->T > 0) {
+    if (!dy || (dw && !x) || (dx && !w) || (d->act != HOBFLOPS_GATE_NONE && !z)) return HOBFLOPS_EINVAL;
+    const int64_t need =
+        linear_backward_workspace(*d, LinearNeed{dx != nullptr, dw != nullptr, dbias != nullptr});
+    if (need > 0 && (!workspace || workspace_bytes < need)) return HOBFLOPS_EINVAL;
+    if (need > 0 && !aligned_to(workspace, 16)) return HOBFLOPS_EALIGN;
+  }
+  if (!aligned_to(dy, d->align) || !aligned_to(x, d->align) || !aligned_to(w, d->align) ||
+      !aligned_to(z, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(dbias, 2))
+    return HOBFLOPS_EALIGN;
+  const LinearBackward p{dy, x, w, z, dx, dw, dbias, workspace};
+  return hip_status(launch_linear_backward(*d, p, (hipStream_t)stream));
+}
+
+int hobflops_adamw_state_len(const hobflops_adamw_tensor* tensors, int count, int64_t* len) {
+  if (!len || count < 0 || (count > 0 && !tensors)) return HOBFLOPS_EINVAL;
+  const int64_t n = state_len_of(tensors, count);
+  if (n < 0) return HOBFLOPS_EINVAL;
+  *len = n;
+  return HOBFLOPS_OK;
+}
+
+int hobflops_adamw(const hobflops_adamw_desc* d, const hobflops_adamw_tensor* tensors, int count,
+                   void* m, uint8_t* m_scales, void* v, uint8_t* v_scales, int64_t state_len,
+                   void* stream) {
+  if (!d || count < 0 || (count > 0 && !tensors)) return HOBFLOPS_EINVAL;
+  if (!type_ok(d->grad_type) || !type_ok(d->copy_type) || d->copy_type == HOBFLOPS_TYPE_F32)
+    return HOBFLOPS_EINVAL;
+  int fmt = -1;
+  if (d->states.wE != 0 || d->states.wF != 0) {
+    if (d->states.wE < 1 || d->states.wF < 1) return HOBFLOPS_EINVAL;
+    fmt = narrow_format(d->states);
+    if (fmt != kE4M3 && fmt != kE5M2) return HOBFLOPS_EUNSUPPORTED;
+  }
+  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0) ||
+      !(d->eps >= 0.0) || (!d->step_at && d->step < 1))
+    return HOBFLOPS_EINVAL;
+  const int64_t len = state_len_of(tensors, count);
+  if (len < 0 || state_len < len) return HOBFLOPS_EINVAL;
+  if (len == 0) return HOBFLOPS_OK;
+  if (!m || !v || (fmt >= 0 && (!m_scales || !v_scales))) return HOBFLOPS_EINVAL;
+  const int gb = type_bytes(d->grad_type), sb = fmt < 0 ? 4 : 1;
+  if (!aligned_to(m, sb) || !aligned_to(v, sb) || !aligned_to(d->lr_at, 4) || !aligned_to(d->step_at, 8) ||
+      !aligned_to(d->grad_scale_at, 4) || !aligned_to(d->skip_at, 4))
+    return HOBFLOPS_EALIGN;
+  Range* r = (Range*)malloc((3 * (size_t)count + 8) * sizeof(Range));
+  if (!r) return HOBFLOPS_EINVAL;
+  int64_t n = 0;
+  int st2 = HOBFLOPS_OK;
+  const auto add = [&](const void* p, int64_t bytes, int written) {
+    if (p && bytes > 0) r[n++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
+  };
+  for (int i = 0; i < count && st2 == HOBFLOPS_OK; ++i) {
+    const hobflops_adamw_tensor& t = tensors[i];
+    if (t.n == 0 || !t.g) continue;
+    if (!t.p)
+      st2 = HOBFLOPS_EINVAL;
+    else if (!aligned_to(t.p, 4) || !aligned_to(t.g, gb) || !aligned_to(t.copy, 2))
+      st2 = HOBFLOPS_EALIGN;
+    add(t.p, t.n * 4, 1);
+    add(t.g, t.n * gb, 0);
+    add(t.copy, t.n * 2, 1);
+  }
+  add(m, len * sb, 1);
+  add(v, len * sb, 1);
+  if (fmt >= 0) {
+    add(m_scales, len / 32, 1);
+    add(v_scales, len / 32, 1);
+  }
+  add(d->lr_at, 4, 0);
+  add(d->step_at, 8, 0);
+  add(d->grad_scale_at, 4, 0);
+  add(d->skip_at, 4, 0);
+  if (st2 == HOBFLOPS_OK && overlapping(r, n)) st2 = HOBFLOPS_EINVAL;
+  free(r);
+  if (st2 != HOBFLOPS_OK) return st2;
+  const AdamwState s{m, v, fmt >= 0 ? m_scales : nullptr, fmt >= 0 ? v_scales : nullptr};
+  return hip_status(launch_adamw(*d, tensors, count, fmt, s, (hipStream_t)stream));
 }
 
 const char* hobflops_status_string(int status) {

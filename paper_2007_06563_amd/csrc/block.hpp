@@ -1,5 +1,6 @@
-// Launchers of the block pack / unpack kernels, the gated feed-forward block
-// and the products with 4-bit weights (block.hip, gated.hip, weights4.hip), and
+// Launchers of the block pack / unpack kernels, the gated feed-forward block,
+// the products with 4-bit weights, and what stands around the block in a training
+// step (block.hip, gated.hip, weights4.hip, norm.hip, linear.hip, adamw.hip), and
 // the element types and narrow formats that they share.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -62,5 +63,42 @@ struct W4Product {
   void* y;
 };
 hipError_t launch_w4(const W4Product& p, hipStream_t stream);
+
+struct LayerNorm {  // a forward or a backward call; dx rows are dense
+  int64_t rows, cols, ldx, ldy, ld_add;
+  int type, wtype;
+  double eps;
+  const void *x, *w, *b, *dy, *add;
+  void *y, *dx, *dw, *db;
+  float *mean, *rstd;
+  void* workspace;
+};
+int64_t norm_backward_workspace(int64_t rows, int64_t cols);
+hipError_t launch_norm_forward(const LayerNorm& p, hipStream_t stream);
+hipError_t launch_norm_backward(const LayerNorm& p, hipStream_t stream);
+
+struct LinearForward {
+  const void *x, *w, *bias, *residual;
+  void *y, *z, *workspace;
+};
+struct LinearBackward {
+  const void *dy, *x, *w, *z;
+  void *dx, *dw, *db, *workspace;  // null: not asked for
+};
+struct LinearNeed {
+  bool dx, dw, db;
+};
+int64_t linear_forward_workspace(const hobflops_linear_desc& d);
+int64_t linear_backward_workspace(const hobflops_linear_desc& d, const LinearNeed& need);
+hipError_t launch_linear_forward(const hobflops_linear_desc& d, const LinearForward& p, hipStream_t stream);
+hipError_t launch_linear_backward(const hobflops_linear_desc& d, const LinearBackward& p, hipStream_t stream);
+
+struct AdamwState {  // scales null: float32
+  void *m, *v;
+  uint8_t *m_scales, *v_scales;
+};
+// fmt: kE4M3, kE5M2 or -1
+hipError_t launch_adamw(const hobflops_adamw_desc& d, const hobflops_adamw_tensor* tensors, int count, int fmt,
+                        const AdamwState& state, hipStream_t stream);
 
 }  // namespace hobflops

@@ -1,0 +1,650 @@
+// A linear layer with its epilogue, y = act(x W^T + b) + r, and its gradients:
+//   z = x W^T + b,  dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum over rows of dz.
+// Products run on the 16x16x32 matrix instruction with float32 sums, to which bias, activation and residual are
+// applied before the one rounding of y. Few tokens read the weights once, straight to registers
+// (few_kernel); more go through LDS in tiles (gemm.hpp). Where tiles are too few for the chip, a sum is
+// split and its parts are joined in their order in a second launch, which then has the epilogue.
+//
+// Roundings to 16 bits: y, dx, dW and db once each; z, kept for the backward pass, and dz as operand of
+// both products. dz in one operand leaves gradients as far from 64 bits as their own rounding does
+// again; two operands would double the products. db is summed from dz before it is rounded.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "block.hpp"
+#include "columns.hpp"
+#include "gemm.hpp"
+#include "narrow.hpp"
+#include "tiles.hpp"
+
+namespace hobflops {
+namespace {
+
+constexpr int kNoAct = HOBFLOPS_GATE_NONE;
+
+__device__ __forceinline__ float act_of(float z, int act) { return act == kNoAct ? z : gate_act(z, act); }
+
+struct LinearArgs {
+  const void *w, *x, *bias, *residual;
+  void *y, *z;
+  float* part;  // with splits: [splits][T][N rounded up to 4]
+  int64_t ldw, ldx, ldr, ldy, T_, N, K, per;  // z: rows N apart; per: k of a split, a multiple of 64
+  int act;
+  uint32_t ni, nj;
+};
+
+// Four values of a row from `col` on, zeros from `end` on.
+template <class T>
+__device__ __forceinline__ f32x4 load4(const typename T::elem* row, int64_t col, int64_t end) {
+  typename T::elem e[4];
+  if (col + 4 <= end) {
+    __builtin_memcpy(e, row + col, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = col + i < end ? row[col + i] : (typename T::elem)0.0f;
+  }
+  return f32x4{(float)e[0], (float)e[1], (float)e[2], (float)e[3]};
+}
+
+#ifdef __HIP_DEVICE_COMPILE__
+// Rows of a wave's sums in LDS: 16 tokens, NI * 16 values of each, and 16 bytes that keep the tokens on different banks.
+template <int NI>
+constexpr int kTileBytes = 16 * (NI * 64 + 16);
+
+// What a wave wrote to LDS is read by its other lanes.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The epilogue of a wave's sums, acc[i][j] of rows f0 + 16 i.. of W and tokens t0 + 16 j..: they go through LDS, 16
+// tokens at a time, so that a lane has 8 neighbouring values of y and a token's lanes whole lines of y, z and the
+// residual. The activation is applied in a loop of its own, whose code is there once for 16 tokens (unrolled
+// over the whole tile it would not fit the instruction cache); the next 16 tokens' residual is under way meanwhile.
+template <class T, int NI, int NJ>
+__device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&acc)[NI][NJ], int64_t f0, int64_t t0,
+                                           uint8_t* lds, int lane) {
+  typedef typename T::elem E;
+  typedef typename T::vec8 Vec;
+  constexpr int kRow = NI * 64 + 16, kLanes = NI * 2, kAtOnce = 64 / kLanes, kPasses = 16 / kAtOnce;
+  const int64_t f = f0 + 8 * (lane % kLanes);
+  const int first = lane / kLanes;
+  const bool whole = f + 8 <= p.N;
+  uint8_t* const mine = lds + first * kRow + 32 * (lane % kLanes);
+  const auto load8 = [&](const E* row) {
+    Vec v = {};
+    if (whole) {
+      __builtin_memcpy(&v, row + f, 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 7; ++k)
+        if (f + k < p.N) v[k] = row[f + k];
+    }
+    return v;
+  };
+  const auto store8 = [&](E* row, const Vec& v) {
+    if (whole) {
+      __builtin_memcpy(row + f, &v, 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 7; ++k)
+        if (f + k < p.N) row[f + k] = v[k];
+    }
+  };
+  float bias[8] = {};
+  if (p.bias) {
+    const Vec b = load8((const E*)p.bias);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = (float)b[k];
+  }
+  Vec more[2][kPasses] = {};
+  const auto residual = [&](int j, Vec(&r)[kPasses]) {
+    if (!p.residual) return;
+#pragma unroll
+    for (int n = 0; n < kPasses; ++n) {
+      const int64_t t = t0 + 16 * j + n * kAtOnce + first;
+      if (t < p.T_) r[n] = load8((const E*)p.residual + t * p.ldr);
+    }
+  };
+  residual(0, more[0]);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      *(f32x4*)(lds + (lane & 15) * kRow + 64 * i + 16 * (lane >> 4)) = acc[i][j];
+    if (j + 1 < NJ) residual(j + 1, more[(j + 1) & 1]);
+    wave_sync();
+    if (p.act != kNoAct) {
+#pragma unroll 1
+      for (int n = 0; n < kPasses; ++n) {
+        f32x4* at = (f32x4*)(mine + n * kAtOnce * kRow);
+        f32x4 v[2] = {at[0], at[1]};
+        const int64_t t = t0 + 16 * j + n * kAtOnce + first;
+        Vec z;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float e = v[k >> 2][k & 3] + bias[k];
+          z[k] = (E)e;
+          v[k >> 2][k & 3] = gate_act(e, p.act);
+        }
+        if (p.z && t < p.T_) store8((E*)p.z + t * p.N, z);
+        at[0] = v[0];
+        at[1] = v[1];
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kPasses; ++n) {
+      const f32x4* at = (const f32x4*)(mine + n * kAtOnce * kRow);
+      const f32x4 v[2] = {at[0], at[1]};
+      const int64_t t = t0 + 16 * j + n * kAtOnce + first;
+      Vec y;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = v[k >> 2][k & 3] + (p.act == kNoAct ? bias[k] : 0.0f);
+        y[k] = (E)(e + (float)more[j & 1][n][k]);
+      }
+      if (t < p.T_) store8((E*)p.y + t * p.ldy, y);
+    }
+    wave_sync();
+  }
+}
+#endif
+
+template <class T, int BI, int BJ, int WI, int WJ, int S>
+__device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const (&sa)[S],
+                                            uint8_t* const (&sb)[S]) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr int NW = WI * WJ, NI = BI / WI / 16, NJ = BJ / WJ / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles = p.ni * p.nj, split = blockIdx.x / tiles;
+  uint32_t ti, tj;
+  tile_of(blockIdx.x - split * tiles, p.ni, p.nj, ti, tj);
+  const int64_t i0 = (int64_t)ti * BI, j0 = (int64_t)tj * BJ;
+  const int64_t k0 = (int64_t)split * p.per;
+  const int64_t k1 = k0 + p.per < p.K ? k0 + p.per : p.K;
+  LoadRows<BI, NW, 1> la;
+  LoadRows<BJ, NW, 1> lb;
+  const void *const ws[1] = {p.w}, *const xs[1] = {p.x};
+  la.start(ws, p.ldw, p.N, i0, k1, k0, wave, lane);
+  lb.start(xs, p.ldx, p.T_, j0, k1, k0, wave, lane);
+  const int wi = wave % WI, wj = wave / WI;
+  ReadRows<T, NI, 0> ra;
+  ReadRows<T, NJ, 0> rb;
+  ra.start(wi * NI * 16, lane);
+  rb.start(wj * NJ * 16, lane);
+  f32x4 acc[NI][NJ] = {};
+  const auto load = [&](int s) {
+    la.load(sa[s], wave);
+    lb.load(sb[s], wave);
+  };
+  sum_tiles<T, NI, NJ, (BI + BJ) / 8 / NW, S>(acc, sa, sb, ra, rb, load,
+                                              (int)((k1 - k0 + kStepK - 1) / kStepK));
+  const int64_t f0 = i0 + wi * NI * 16, t0 = j0 + wj * NJ * 16;
+  if (p.part) {
+    const int64_t ldp = (p.N + 3) & ~(int64_t)3;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int64_t t = t0 + 16 * j + (lane & 15), at = f0 + 16 * i + 4 * (lane >> 4);
+        if (t < p.T_ && at < p.N) *(f32x4*)(p.part + ((int64_t)split * p.T_ + t) * ldp + at) = acc[i][j];
+      }
+    return;
+  }
+  __syncthreads();  // the stages are free: no wave reads one or has a load into one under way
+  // (two waves, or one, an array)
+  constexpr int kEach = NW / 4;
+  uint8_t* const stage = wave / kEach == 0 ? sa[0] : wave / kEach == 1 ? sa[1] : wave / kEach == 2 ? sb[0] : sb[1];
+  store_tile<T, NI, NJ>(p, acc, f0, t0, stage + (wave % kEach) * kTileBytes<NI>, lane);
+#endif
+}
+
+// 256 x 256 sums a workgroup, eight waves, one workgroup on a CU.
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES2(256, 256);
+  linear_tile<T, 256, 256, 2, 4, 2>(p, sa, sb);
+}
+// 128 x 128 sums, two workgroups on a CU.
+template <class T>
+__global__ __launch_bounds__(256, 2) void linear_middle_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES2(128, 128);
+  linear_tile<T, 128, 128, 2, 2, 2>(p, sa, sb);
+}
+// 64 x 64 sums, three workgroups on a CU.
+template <class T>
+__global__ __launch_bounds__(256, 3) void linear_small_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES3(64, 64);
+  linear_tile<T, 64, 64, 2, 2, 3>(p, sa, sb);
+}
+
+// The parts of a sum in their order, then the epilogue: 4 values a thread.
+template <class T>
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int splits) {
+  typedef typename T::elem E;
+  const int64_t ldp = (p.N + 3) & ~(int64_t)3, n = p.T_ * ldp;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+    f32x4 v = *(const f32x4*)(p.part + i);
+    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(p.part + s * n + i);
+    const int64_t row = i / ldp, col = i - row * ldp;
+    if (p.bias) v += load4<T>((const E*)p.bias, col, p.N);
+    if (p.z) {
+      const float e[4] = {v[0], v[1], v[2], v[3]};
+      store4<T>((E*)p.z + row * p.N, col, p.N, e);
+    }
+    f32x4 r = {};
+    if (p.residual) r = load4<T>((const E*)p.residual + row * p.ldr, col, p.N);
+    float e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = act_of(v[k], p.act) + r[k];
+    store4<T>((E*)p.y + row * p.ldy, col, p.N, e);
+  }
+}
+
+// Up to 16 tokens: a workgroup has 16 rows of W, its waves every kFewWaves-th 64 k of them, the lane 16 k of one
+// row each time (32 bytes), so that the four lanes of a row read a whole line. The same k of x is the other operand: which
+// k a lane has does not matter as long as both operands agree. The waves' sums meet in LDS.
+constexpr int kFewWaves = 8;
+template <class T>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(LinearArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef typename T::elem E;
+  typedef typename T::vec8 Vec;
+  __shared__ f32x4 sums[kFewWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r = lane & 15, q = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  // rows and tokens beyond the end: the last one again, whose sums nobody stores
+  const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1, t = r < p.T_ ? r : p.T_ - 1;
+  const E *w = (const E*)p.w + n * p.ldw + 16 * q, *x = (const E*)p.x + t * p.ldx + 16 * q;
+  const int64_t whole = p.K / 64;
+  f32x4 acc = {};
+  constexpr int U = 4;
+  int64_t c = wave;
+  for (; c + (U - 1) * kFewWaves < whole; c += U * kFewWaves) {
+    Vec a[U][2], b[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      __builtin_memcpy(a[u], w + (c + u * kFewWaves) * 64, 32);
+      __builtin_memcpy(b[u], x + (c + u * kFewWaves) * 64, 32);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      acc = T::mfma(a[u][0], b[u][0], acc);
+      acc = T::mfma(a[u][1], b[u][1], acc);
+    }
+  }
+  for (; c * 64 < p.K; c += kFewWaves) {
+    Vec a[2], b[2];
+    if (c < whole) {
+      __builtin_memcpy(a, w + c * 64, 32);
+      __builtin_memcpy(b, x + c * 64, 32);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const bool in = c * 64 + 16 * q + k < p.K;
+        a[k >> 3][k & 7] = in ? w[c * 64 + k] : (E)0.0f;
+        b[k >> 3][k & 7] = in ? x[c * 64 + k] : (E)0.0f;
+      }
+    }
+    acc = T::mfma(a[0], b[0], acc);
+    acc = T::mfma(a[1], b[1], acc);
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int i = 1; i < kFewWaves; ++i) acc += sums[i][lane];
+  const int64_t at = n0 + 4 * q;  // token r, rows at .. at + 3 of W
+  if (r >= p.T_ || at >= p.N) return;
+  if (p.bias) acc += load4<T>((const E*)p.bias, at, p.N);
+  if (p.z) {
+    const float e[4] = {acc[0], acc[1], acc[2], acc[3]};
+    store4<T>((E*)p.z + r * p.N, at, p.N, e);
+  }
+  f32x4 more = {};
+  if (p.residual) more = load4<T>((const E*)p.residual + r * p.ldr, at, p.N);
+  float e[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) e[k] = act_of(acc[k], p.act) + more[k];
+  store4<T>((E*)p.y + r * p.ldy, at, p.N, e);
+#endif
+}
+
+// ---- the gradients -----------------------------------------------------------
+
+// dz in rows [t][ldo] (zeros from N to ldo) and the parts of db, with the alignment of x's and W's rows in the same
+// launch: 256 columns and every `parts`-th 8 rows a workgroup, 8 values a thread.
+struct DzArgs {
+  const void *dy, *z;
+  void* out;    // null: dy is read in place
+  float* part;  // null: no db; else [parts][N rounded up to 8]
+  int64_t T_, N, ldy, ldo;
+  int act;
+  uint32_t strips, parts;
+};
+template <class T>
+__global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs rows) {
+  typedef typename T::elem E;
+  const uint32_t own = p.strips * p.parts;
+  if (blockIdx.x >= own) {
+    align_rows_of<T>(rows, (int64_t)(blockIdx.x - own) * 256 + threadIdx.x, (int64_t)(gridDim.x - own) * 256);
+    return;
+  }
+  __shared__ float sums[8][256];
+  const uint32_t strip = blockIdx.x % p.strips, part = blockIdx.x / p.strips;
+  const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+  const int64_t col = (int64_t)strip * 256 + lane * 8;
+  float db[8] = {};
+  if (col < p.N) {
+    for (int64_t t = (int64_t)part * 8 + sub; t < p.T_; t += (int64_t)p.parts * 8) {
+      const E* dy = (const E*)p.dy + t * p.ldy + col;
+      typename T::vec8 d = {}, z = {};
+      if (col + 8 <= p.N) {
+        __builtin_memcpy(&d, dy, 16);
+        if (p.z) __builtin_memcpy(&z, (const E*)p.z + t * p.N + col, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+          if (col + j < p.N) {
+            d[j] = dy[j];
+            if (p.z) z[j] = ((const E*)p.z)[t * p.N + col + j];
+          }
+      }
+      typename T::vec8 o;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v = (float)d[j];
+        if (p.z) {
+          float a, da;
+          gate_act_grad((float)z[j], p.act, a, da);
+          v = col + j < p.N ? v * da : 0.0f;
+        }
+        db[j] += v;
+        o[j] = (E)v;
+      }
+      if (p.out) *(typename T::vec8*)((E*)p.out + t * p.ldo + col) = o;
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[sub][lane * 8 + j] = db[j];
+  __syncthreads();
+  const int64_t c = (int64_t)strip * 256 + threadIdx.x;
+  float v = sums[0][threadIdx.x];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) v += sums[j][threadIdx.x];
+  if (c < p.N) p.part[(int64_t)part * ((p.N + 7) & ~(int64_t)7) + c] = v;
+}
+
+// Workgroups of dx, as many as `parts`, then those of dW.
+template <class T, int B, int WJ>
+__device__ __forceinline__ void linear_grad_tiles(const GradArgs& dx, const GradArgs& dw, uint32_t parts,
+                                                  uint8_t* const (&sa)[2], uint8_t* const (&sb)[2]) {
+  const bool first = blockIdx.x < parts;
+  const uint32_t b = first ? blockIdx.x : blockIdx.x - parts;
+  if (first)
+    grad_tile<T, false, 1, B, B, WJ, 2>(dx, sa, sb, b % (dx.ni * dx.nj), b / (dx.ni * dx.nj));
+  else
+    grad_tile<T, true, 1, B, B, WJ, 2>(dw, sa, sb, b % (dw.ni * dw.nj), b / (dw.ni * dw.nj));
+}
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_grad_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
+  HOBFLOPS_STAGES2(256, 256);
+  linear_grad_tiles<T, 256, 4>(dx, dw, parts, sa, sb);
+}
+template <class T>
+__global__ __launch_bounds__(256, 2) void linear_grad_small_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
+  HOBFLOPS_STAGES2(128, 128);
+  linear_grad_tiles<T, 128, 2>(dx, dw, parts, sa, sb);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    p[i] = (typename T::elem)0.0f;
+}
+
+// ---- plans -------------------------------------------------------------------
+
+// The tiles of a product and the parts of its sum, by an estimate of their time in microseconds: rounds of workgroups,
+// each its steps of 64 k and about five more to start and end; the parts of a sum are written and read once
+// more in float32, 4 TB/s, and joined in a launch.
+struct Kind {
+  int side, per_cu;
+  double step;
+};
+constexpr Kind kKinds[] = {{256, 1, 1.42}, {128, 2, 0.8}, {64, 3, 0.45}};
+struct Tiling {
+  int kind, splits;
+};
+constexpr int kMostSplits = 32;
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int kinds) {
+  const int64_t steps = (K + kStepK - 1) / kStepK;
+  Tiling best{0, 1};
+  double least = -1.0;
+  for (int k = 0; k < kinds; ++k) {
+    const int64_t side = kKinds[k].side, slots = kKinds[k].per_cu * kCUs;
+    const int64_t tiles = ((rows + side - 1) / side) * ((cols + side - 1) / side);
+    for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 6); ++n) {
+      const double rounds = (double)((tiles * n + slots - 1) / slots);
+      double us = rounds * ((double)((steps + n - 1) / n) + 5.0) * kKinds[k].step;
+      if (n > 1) us += 4.0 + (double)(n + 1) * rows * cols * 4.0 / 4e6;
+      if (least < 0.0 || us < least) {
+        least = us;
+        best = Tiling{k, n};
+      }
+    }
+  }
+  return best;
+}
+// Rows that the products read in place.
+bool in_place(int64_t cols, int64_t ld, int align) {
+  return align >= 16 && cols % 8 == 0 && ld % 8 == 0 && ld < (int64_t)1 << 21;
+}
+int64_t splits_of(int64_t K, int splits, int64_t* per) {
+  *per = round_up((K + splits - 1) / splits, kStepK);
+  return (K + *per - 1) / *per;
+}
+
+constexpr int64_t kFewTokens = 16;
+
+struct ForwardPlan {
+  int64_t x = -1, w = -1, part = -1, bytes = 0;
+  Tiling tiles{0, 1};
+};
+ForwardPlan plan_forward(const hobflops_linear_desc& d) {
+  ForwardPlan p;
+  if (d.T <= kFewTokens) return p;
+  const int64_t Kp = round_up(d.K, 8);
+  if (!in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * Kp * 2);
+  if (!in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * Kp * 2);
+  p.tiles = plan_tiles(d.N, d.T, d.K, 3);
+  if (p.tiles.splits > 1) p.part = take(&p.bytes, p.tiles.splits * d.T * round_up(d.N, 4) * 4);
+  return p;
+}
+
+struct BackwardPlan {
+  int64_t x = -1, w = -1, dz = -1, db = -1, part_x = -1, part_w = -1, bytes = 0;
+  int64_t Kp, Np;
+  uint32_t parts = 1;  // of db
+  Tiling dx{0, 1}, dw{0, 1};
+};
+// need: the gradients asked for
+BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need) {
+  BackwardPlan p;
+  p.Kp = round_up(d.K, 8);
+  p.Np = round_up(d.N, 8);
+  if (d.T == 0) return p;
+  const bool products = need.dx || need.dw;
+  if (products && (d.act != kNoAct || !in_place(d.N, d.ldy, d.align))) p.dz = take(&p.bytes, d.T * p.Np * 2);
+  if (need.dw && !in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * p.Kp * 2);
+  if (need.dx && !in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * p.Kp * 2);
+  if (need.dx) {
+    p.dx = plan_tiles(d.T, d.K, p.Np, 2);
+    if (p.dx.splits > 1) p.part_x = take(&p.bytes, p.dx.splits * d.T * round_up(d.K, 4) * 4);
+  }
+  if (need.dw) {
+    p.dw = plan_tiles(d.N, d.K, d.T, 2);
+    if (p.dw.splits > 1) p.part_w = take(&p.bytes, p.dw.splits * d.N * round_up(d.K, 4) * 4);
+  }
+  const int64_t strips = (d.N + 255) / 256, most = (d.T + 7) / 8, wanted = (2048 + strips - 1) / strips;
+  p.parts = (uint32_t)(most < wanted ? most : wanted);
+  if (need.db) p.db = take(&p.bytes, (int64_t)p.parts * p.Np * 4);
+  return p;
+}
+
+template <class T>
+hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStream_t s) {
+  LinearArgs p{};
+  p.w = c.w;
+  p.x = c.x;
+  p.bias = c.bias;
+  p.residual = c.residual;
+  p.y = c.y;
+  p.z = c.z;
+  p.ldw = d.ldw;
+  p.ldx = d.ldx;
+  p.ldr = d.ldr;
+  p.ldy = d.ldy;
+  p.T_ = d.T;
+  p.N = d.N;
+  p.K = d.K;
+  p.act = d.act;
+  if (d.T <= kFewTokens) {
+    few_kernel<T><<<(unsigned)((d.N + 15) / 16), kFewWaves * 64, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const ForwardPlan plan = plan_forward(d);
+  uint8_t* ws = (uint8_t*)c.workspace;
+  AlignArgs align{};
+  align.cols = d.K;
+  align.ldd = round_up(d.K, 8);
+  if (plan.x >= 0) {
+    add_rows(align, 0, c.x, d.ldx, d.T, ws + plan.x);
+    p.x = ws + plan.x;
+    p.ldx = align.ldd;
+  }
+  if (plan.w >= 0) {
+    add_rows(align, 1, c.w, d.ldw, d.N, ws + plan.w);
+    p.w = ws + plan.w;
+    p.ldw = align.ldd;
+  }
+  align_rows<T>(align, s);
+  // (rows that were copied have zeros up to the multiple of 8)
+  if (plan.x >= 0 && plan.w >= 0) p.K = align.ldd;
+  const int64_t splits = splits_of(p.K, plan.tiles.splits, &p.per);
+  if (splits > 1) p.part = (float*)(ws + plan.part);
+  const int side = kKinds[plan.tiles.kind].side;
+  p.ni = (uint32_t)((d.N + side - 1) / side);
+  p.nj = (uint32_t)((d.T + side - 1) / side);
+  const unsigned grid = (unsigned)(p.ni * p.nj * splits);
+  if (plan.tiles.kind == 0)
+    linear_kernel<T><<<grid, 512, 0, s>>>(p);
+  else if (plan.tiles.kind == 1)
+    linear_middle_kernel<T><<<grid, 256, 0, s>>>(p);
+  else
+    linear_small_kernel<T><<<grid, 256, 0, s>>>(p);
+  if (p.part)
+    linear_join_kernel<T><<<grid_of(d.T * round_up(d.N, 4) / 4, 4096), 256, 0, s>>>(p, (int)splits);
+  return hipGetLastError();
+}
+
+uint32_t count_tiles(GradArgs& p, const Tiling& t) {
+  const int64_t b = kKinds[t.kind].side;
+  p.ni = (uint32_t)((p.ni_ + b - 1) / b);
+  p.nj = (uint32_t)((p.nj_ + b - 1) / b);
+  return p.ni * p.nj;
+}
+template <class T>
+void grad_products(const GradArgs& dx, uint32_t parts, const GradArgs& dw, uint32_t tiles, int kind, hipStream_t s) {
+  if (parts + tiles == 0) return;
+  if (kind)
+    linear_grad_small_kernel<T><<<parts + tiles, 256, 0, s>>>(dx, dw, parts);
+  else
+    linear_grad_kernel<T><<<parts + tiles, 512, 0, s>>>(dx, dw, parts);
+}
+
+template <class T>
+hipError_t backward(const hobflops_linear_desc& d, const LinearBackward& c, hipStream_t s) {
+  typedef typename T::elem E;
+  if (d.T == 0) {
+    if (c.dw) zeros_kernel<T><<<1024, 256, 0, s>>>((E*)c.dw, d.N * d.K);
+    if (c.db) zeros_kernel<T><<<16, 256, 0, s>>>((E*)c.db, d.N);
+    return hipGetLastError();
+  }
+  const BackwardPlan plan = plan_backward(d, LinearNeed{c.dx != nullptr, c.dw != nullptr, c.db != nullptr});
+  uint8_t* ws = (uint8_t*)c.workspace;
+  DzArgs z{};
+  z.dy = c.dy;
+  z.z = d.act != kNoAct ? c.z : nullptr;
+  z.out = plan.dz >= 0 ? ws + plan.dz : nullptr;
+  z.part = plan.db >= 0 ? (float*)(ws + plan.db) : nullptr;
+  z.T_ = d.T;
+  z.N = d.N;
+  z.ldy = d.ldy;
+  z.ldo = plan.Np;
+  z.act = d.act;
+  z.strips = (uint32_t)((d.N + 255) / 256);
+  z.parts = plan.parts;
+  if (!z.out && !z.part) z.strips = z.parts = 0;
+  AlignArgs align{};
+  align.cols = d.K;
+  align.ldd = plan.Kp;
+  if (plan.x >= 0) add_rows(align, 0, c.x, d.ldx, d.T, ws + plan.x);
+  if (plan.w >= 0) add_rows(align, 1, c.w, d.ldw, d.N, ws + plan.w);
+  const unsigned grid = z.strips * z.parts + grid_of(align.rows[2] * align.ldd / 8, 65536);
+  if (grid) linear_prepare_kernel<T><<<grid, 256, 0, s>>>(z, align);
+  GradArgs p{};  // dx
+  p.b = z.out ? z.out : c.dy;
+  p.ldb = z.out ? plan.Np : d.ldy;
+  p.ni_ = d.K;
+  p.cols = plan.Kp;
+  p.F = d.N;
+  p.Fp = plan.Np;
+  GradArgs w = p;
+  w.a[0] = plan.x >= 0 ? ws + plan.x : c.x;
+  w.lda = plan.x >= 0 ? plan.Kp : d.ldx;
+  w.bcols = plan.Np;
+  w.nj_ = d.N;
+  w.K = d.T;
+  w.out[0] = c.dw;
+  p.a[0] = plan.w >= 0 ? ws + plan.w : c.w;
+  p.lda = plan.w >= 0 ? plan.Kp : d.ldw;
+  p.nj_ = d.T;
+  p.K = plan.Np;
+  p.out[0] = c.dx;
+  const int64_t sx = splits_of(p.K, plan.dx.splits, &p.per), sw = splits_of(w.K, plan.dw.splits, &w.per);
+  if (sx > 1) p.part = (float*)(ws + plan.part_x);
+  if (sw > 1) w.part = (float*)(ws + plan.part_w);
+  const uint32_t parts = c.dx ? count_tiles(p, plan.dx) * (uint32_t)sx : 0;
+  const uint32_t tiles = c.dw ? count_tiles(w, plan.dw) * (uint32_t)sw : 0;
+  if (plan.dx.kind == plan.dw.kind) {
+    grad_products<T>(p, parts, w, tiles, plan.dx.kind, s);
+  } else {
+    grad_products<T>(p, 0, w, tiles, plan.dw.kind, s);
+    grad_products<T>(p, parts, w, 0, plan.dx.kind, s);
+  }
+  if (c.dx && p.part)
+    join_kernel<T><<<grid_of(d.T * round_up(d.K, 4) / 4, 4096), 256, 0, s>>>(p.part, (int)sx, d.T, d.K, (E*)c.dx);
+  if (c.dw && w.part)
+    join_kernel<T><<<grid_of(d.N * round_up(d.K, 4) / 4, 4096), 256, 0, s>>>(w.part, (int)sw, d.N, d.K, (E*)c.dw);
+  if (c.db) launch_column_sums<T>(z.part, plan.parts, plan.Np, c.db, nullptr, d.N, 0, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t linear_forward_workspace(const hobflops_linear_desc& d) { return plan_forward(d).bytes; }
+int64_t linear_backward_workspace(const hobflops_linear_desc& d, const LinearNeed& need) {
+  return plan_backward(d, need).bytes;
+}
+
+hipError_t launch_linear_forward(const hobflops_linear_desc& d, const LinearForward& p, hipStream_t s) {
+  return d.type == HOBFLOPS_TYPE_BF16 ? forward<TypeBF16>(d, p, s) : forward<TypeF16>(d, p, s);
+}
+hipError_t launch_linear_backward(const hobflops_linear_desc& d, const LinearBackward& p, hipStream_t s) {
+  return d.type == HOBFLOPS_TYPE_BF16 ? backward<TypeBF16>(d, p, s) : backward<TypeF16>(d, p, s);
+}
+
+}  // namespace hobflops

@@ -7,6 +7,7 @@ Plane tensors are int32 (the bit patterns of PL32 words).
 """
 import collections
 import ctypes
+import operator
 import os
 import warnings
 
@@ -23,7 +24,8 @@ ALGO_AUTO, ALGO_FUSED, ALGO_SPLIT, ALGO_SPLIT_COMPACT = 0, 1, 2, 3
 OFM_PLANES, OFM_F32, OFM_CODE = 0, 1, 2
 TILE_112X64, TILE_56X64, TILE_32X64, TILE_32X32, TILE_16X32 = 1, 2, 3, 4, 5
 SCALE_POW2, SCALE_BF16, SCALE_F32 = 0, 1, 2
-GATE_SILU, GATE_GELU, GATE_RELU = 0, 1, 2
+GATE_NONE, GATE_SILU, GATE_GELU, GATE_RELU = -1, 0, 1, 2
+NEED_DX, NEED_DW, NEED_DBIAS = 1, 2, 4
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _SCALES = {torch.uint8: SCALE_POW2, torch.bfloat16: SCALE_BF16, torch.float32: SCALE_F32}
 _SCALE_TYPES = {v: k for k, v in _SCALES.items()}
@@ -63,8 +65,39 @@ class GatedDesc(ctypes.Structure):
                 ("align", ctypes.c_int)]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("ldy", ctypes.c_int64), ("ld_add", ctypes.c_int64), ("type", ctypes.c_int),
+                ("wtype", ctypes.c_int), ("eps", ctypes.c_double)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("K", ctypes.c_int64), ("N", ctypes.c_int64),
+                ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldy", ctypes.c_int64),
+                ("ldr", ctypes.c_int64), ("type", ctypes.c_int), ("act", ctypes.c_int),
+                ("align", ctypes.c_int)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("n", ctypes.c_int64)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("grad_type", ctypes.c_int), ("copy_type", ctypes.c_int), ("states", Fmt),
+                ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("lr_at", ctypes.c_void_p), ("step_at", ctypes.c_void_p),
+                ("grad_scale_at", ctypes.c_void_p), ("skip_at", ctypes.c_void_p)]
+
+
 # What gated_forward keeps for gated_backward: (codes, scales) of x, g and u.
 GatedSaved = collections.namedtuple("GatedSaved", "x gate up fmt")
+# What layer_norm keeps for layer_norm_backward: float32 [rows] each.
+NormSaved = collections.namedtuple("NormSaved", "mean rstd")
+# The moments of adamw, flat: float32 each (fmt None), or (codes, scales) each, v by its square root.
+AdamWState = collections.namedtuple("AdamWState", "m v fmt")
 
 
 EXPORTS = ("hobflops_plane_words", "hobflops_pack", "hobflops_pack_batch", "hobflops_unpack",
@@ -75,7 +108,10 @@ EXPORTS = ("hobflops_plane_words", "hobflops_pack", "hobflops_pack_batch", "hobf
            "hobflops_netlist_ops", "hobflops_avgpool", "hobflops_avgpool_supported",
            "hobflops_avgpool_netlist_ops", "hobflops_block_pack", "hobflops_block_unpack",
            "hobflops_gated_workspace", "hobflops_gated_forward", "hobflops_gated_backward",
-           "hobflops_w4_linear", "hobflops_w4_gated", "hobflops_wait_failures", "hobflops_set_wait_limit",
+           "hobflops_w4_linear", "hobflops_w4_gated", "hobflops_layer_norm",
+           "hobflops_layer_norm_workspace", "hobflops_layer_norm_backward", "hobflops_linear",
+           "hobflops_linear_workspace", "hobflops_linear_backward", "hobflops_adamw",
+           "hobflops_adamw_state_len", "hobflops_wait_failures", "hobflops_set_wait_limit",
            "hobflops_get_wait_limit", "hobflops_status_string")
 
 
@@ -112,6 +148,16 @@ def lib():
         L.hobflops_w4_linear.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, ci, vp, i64, vp]
         L.hobflops_w4_gated.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, vp, vp, ci, ci, ci, vp,
                                         i64, vp]
+        nd, ld = ctypes.POINTER(NormDesc), ctypes.POINTER(LinearDesc)
+        L.hobflops_layer_norm.argtypes = [nd] + [vp] * 7
+        L.hobflops_layer_norm_workspace.argtypes = [nd, ctypes.POINTER(i64)]
+        L.hobflops_layer_norm_backward.argtypes = [nd] + [vp] * 10 + [i64, vp]
+        L.hobflops_linear.argtypes = [ld] + [vp] * 7 + [i64, vp]
+        L.hobflops_linear_workspace.argtypes = [ld, ci, ctypes.POINTER(i64)]
+        L.hobflops_linear_backward.argtypes = [ld] + [vp] * 8 + [i64, vp]
+        # (arrays of AdamwTensor: any ctypes array of its words)
+        L.hobflops_adamw.argtypes = [ctypes.POINTER(AdamwDesc), vp, ci, vp, vp, vp, vp, i64, vp]
+        L.hobflops_adamw_state_len.argtypes = [vp, ci, ctypes.POINTER(i64)]
         L.hobflops_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ci]
         L.hobflops_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.hobflops_get_wait_limit.argtypes = []
@@ -518,10 +564,11 @@ def _align(*ptrs):
 
 def _no_gradient(name, *tensors):
     """Says that autograd records nothing of a call whose inputs it follows."""
-    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         warnings.warn(f"{name}: its result carries no gradient to its inputs; wrap it in a "
-                      "torch.autograd.Function (gated_backward has the gated block's gradients), or "
-                      "call it under torch.no_grad()", stacklevel=3)
+                      "torch.autograd.Function (gated_backward, layer_norm_backward and "
+                      "linear_backward have the gradients), or call it under torch.no_grad()",
+                      stacklevel=3)
 
 
 def _workspace(d, backward, device):
@@ -615,3 +662,252 @@ def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, o
     _no_gradient("w4_gated", x)
     _call(x.device, lib().hobflops_w4_gated, *head, act, *tail)
     return y
+
+
+# ---- around the gated block in a training step: layer norm, a linear layer, AdamW ----
+
+
+def _vector(t, n, dtypes, device, name):
+    """The pointer of a dense vector of n values, None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name}: a tensor on {device} is needed")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: {' or '.join(str(d) for d in dtypes)} is needed, not {t.dtype}")
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: a dense vector of {n} values is needed")
+    return t.data_ptr()
+
+
+def _like(t, shape, like, name):
+    """(pointer, elements between rows) of a matrix of this shape with `like`'s type and device."""
+    ptr, r, c, ld = _rows(t, name)
+    if (r, c) != tuple(shape):
+        raise ValueError(f"{name}: {tuple(shape)} is needed, not {(r, c)}")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError(f"{name}: {like.dtype} on {like.device} is needed")
+    return ptr, ld
+
+
+def _bytes_of(query, device, *args):
+    """A workspace of the size that a query gives: (tensor, pointer, bytes)."""
+    n = ctypes.c_int64()
+    _check(query(*args, ctypes.byref(n)))
+    if n.value == 0:
+        return None, None, 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n.value
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
+    """y = (x - mean) rstd weight + bias over the rows of x [rows, cols] (float32, bfloat16 or
+    float16, dense rows any distance apart); weight and bias [cols] of x's type or float32 (one type).
+    With save: (y, saved), what layer_norm_backward needs beside x. out may be x. Autograd
+    records nothing of it."""
+    px, rows, cols, ldx = _rows(x, "layer_norm x")
+    kind, dev = _type(x, "layer_norm x"), x.device
+    pw = _vector(weight, cols, (x.dtype, torch.float32), dev, "layer_norm weight")
+    pb = _vector(bias, cols, (x.dtype, torch.float32), dev, "layer_norm bias")
+    one = weight if weight is not None else bias
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("layer_norm: weight and bias must have one type")
+    _no_gradient("layer_norm", x, weight, bias)
+    y, py, ldy = _out_rows(out, (rows, cols), x.dtype, dev, "layer_norm out")
+    d = NormDesc(rows, cols, ldx, ldy, cols, kind, _TYPES[one.dtype] if one is not None else kind, eps)
+    saved, pm, pr = None, None, None
+    if save:
+        saved = NormSaved(torch.empty(rows, dtype=torch.float32, device=dev),
+                          torch.empty(rows, dtype=torch.float32, device=dev))
+        pm, pr = saved.mean.data_ptr(), saved.rstd.data_ptr()
+    _call(dev, lib().hobflops_layer_norm, ctypes.byref(d), px, pw, pb, py, pm, pr)
+    return (y, saved) if save else y
+
+
+def layer_norm_backward(dy, x, saved, weight=None, add=None, dw=True, db=True):
+    """The gradients (dx, dw, db) of layer_norm from dy [rows, cols], its x and what it saved. add: a
+    gradient [rows, cols] that reaches x past the norm (a residual path), joined to dx. dw and db have
+    the type of weight (without weight: of x); False: not computed, None."""
+    px, rows, cols, ldx = _rows(x, "layer_norm_backward x")
+    kind, dev = _type(x, "layer_norm_backward x"), x.device
+    pg, ldg = _like(dy, (rows, cols), x, "layer_norm_backward dy")
+    pa, lda = (None, cols) if add is None else _like(add, (rows, cols), x, "layer_norm_backward add")
+    pw = _vector(weight, cols, (x.dtype, torch.float32), dev, "layer_norm_backward weight")
+    pm, pr = (_vector(t, rows, (torch.float32,), dev, "layer_norm_backward saved") for t in saved)
+    wdtype = x.dtype if weight is None else weight.dtype
+    d = NormDesc(rows, cols, ldx, ldg, lda, kind, _TYPES[wdtype], 0.0)
+    dx = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    gw, gb = (torch.empty(cols, dtype=wdtype, device=dev) if need else None for need in (dw, db))
+    ws, pws, n = (None, None, 0)
+    if dw or db:
+        ws, pws, n = _bytes_of(lib().hobflops_layer_norm_workspace, dev, ctypes.byref(d))
+    _call(dev, lib().hobflops_layer_norm_backward, ctypes.byref(d), pg, px, pw, pm, pr, pa, dx.data_ptr(),
+          gw.data_ptr() if dw else None, gb.data_ptr() if db else None, pws, n)
+    return dx, gw, gb
+
+
+def linear(x, w, bias=None, act=None, residual=None, save=False, out=None):
+    """y = act(x w^T + bias) + residual: x [T, K], w [N, K], bias [N], residual [T, N], bfloat16 or
+    float16 -> y [T, N]. act: GATE_SILU, GATE_GELU, GATE_RELU or None. With save: (y, z), z [T, N] what act
+    was applied to, for linear_backward (None without act). out may be the residual. Autograd records
+    nothing of it."""
+    px, T, K, ldx = _rows(x, "linear x")
+    pw, N, Kw, ldw = _rows(w, "linear w")
+    kind, dev = _type(x, "linear x"), x.device
+    if Kw != K:
+        raise ValueError("linear: x and w differ in K")
+    if w.dtype != x.dtype or w.device != dev:
+        raise TypeError("linear: x and w must have one type and device")
+    pb = _vector(bias, N, (x.dtype,), dev, "linear bias")
+    pr, ldr = (None, N) if residual is None else _like(residual, (T, N), x, "linear residual")
+    _no_gradient("linear", x, w, bias, residual)
+    y, py, ldy = _out_rows(out, (T, N), x.dtype, dev, "linear out")
+    a = GATE_NONE if act is None else act
+    d = LinearDesc(T, K, N, ldx, ldw, ldy, ldr, kind, a, _align(px, pw))
+    z = torch.empty((T, N), dtype=x.dtype, device=dev) if save and a != GATE_NONE else None
+    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, ctypes.byref(d), 0)
+    _call(dev, lib().hobflops_linear, ctypes.byref(d), px, pw, pb, pr, py,
+          None if z is None else z.data_ptr(), pws, n)
+    return (y, z) if save else y
+
+
+def linear_backward(dy, x, w, z=None, act=None, dx=True, dw=True, db=True):
+    """The gradients (dx, dw, db) of linear from dy [T, N], its x and w, and with an activation the z that
+    it saved; the residual's gradient is dy itself. False: not computed, None."""
+    pg, T, N, ldg = _rows(dy, "linear_backward dy")
+    px, Tx, K, ldx = _rows(x, "linear_backward x")
+    pw, Nw, Kw, ldw = _rows(w, "linear_backward w")
+    kind, dev, dtype = _type(dy, "linear_backward dy"), dy.device, dy.dtype
+    if (Tx, Nw, Kw) != (T, N, K):
+        raise ValueError("linear_backward: dy, x and w do not fit together")
+    if x.dtype != dtype or w.dtype != dtype or x.device != dev or w.device != dev:
+        raise TypeError("linear_backward: dy, x and w must have one type and device")
+    a = GATE_NONE if act is None else act
+    pz = None
+    if a != GATE_NONE:
+        if z is None:
+            raise ValueError("linear_backward: an activation's gradient needs z")
+        pz = _dense(z, (T, N), dtype, dev, "linear_backward z")
+    d = LinearDesc(T, K, N, ldx, ldw, ldg, N, kind, a, _align(pg, px, pw))
+    need = (NEED_DX if dx else 0) | (NEED_DW if dw else 0) | (NEED_DBIAS if db else 0)
+    if not need:
+        return None, None, None
+    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, ctypes.byref(d), need)
+    gx, gw, gb = (torch.empty(shape, dtype=dtype, device=dev) if asked else None
+                  for shape, asked in (((T, K), dx), ((N, K), dw), (N, db)))
+    ptrs = [None if t is None else t.data_ptr() for t in (gx, gw, gb)]
+    _call(dev, lib().hobflops_linear_backward, ctypes.byref(d), pg, px, pw, pz, *ptrs, pws, n)
+    return gx, gw, gb
+
+
+def adamw_places(params):
+    """Where each tensor's part of the flat states of adamw begins, and their length: parts begin at
+    multiples of 32."""
+    at, total = [], 0
+    for p in params:
+        at.append(total)
+        total += (p.numel() + 31) // 32 * 32
+    return at, total
+
+
+def adamw_state(params, fmt=None):
+    """Zero moments for adamw of these tensors: float32, or blocks of an 8-bit format."""
+    total, dev = adamw_places(params)[1], params[0].device
+    if fmt is None:
+        return AdamWState(*(torch.zeros(total, dtype=torch.float32, device=dev) for _ in "mv"), None)
+    m, v = (tuple(torch.zeros(n, dtype=torch.uint8, device=dev) for n in (total, total // 32))
+            for _ in "mv")
+    return AdamWState(m, v, fmt)
+
+
+_numel, _contiguous, _data_ptr, _get_device = (torch.Tensor.numel, torch.Tensor.is_contiguous,
+                                               torch.Tensor.data_ptr, torch.Tensor.get_device)
+_dtype, _shape = operator.attrgetter("dtype"), operator.attrgetter("shape")
+
+
+def _tensors(ts, dtypes, device, name):
+    """Pointers of dense tensors of one of these types on a device, and the type."""
+    if set(map(_get_device, ts)) != {device.index}:
+        raise TypeError(f"adamw {name}: tensors on {device} are needed")
+    types = set(map(_dtype, ts))
+    if len(types) != 1 or not types <= set(dtypes):
+        raise TypeError(f"adamw {name}: one type of {', '.join(map(str, dtypes))} is needed")
+    if not all(map(_contiguous, ts)):
+        raise ValueError(f"adamw {name}: contiguous tensors are needed")
+    return list(map(_data_ptr, ts)), types.pop()
+
+
+def _scalar(value, dtype, device, name):
+    """(number, pointer) of a number, or of a tensor of one value on the device."""
+    if not isinstance(value, torch.Tensor):
+        return value, None
+    if value.dtype != dtype or value.numel() != 1 or value.device != device:
+        raise TypeError(f"adamw {name}: a number, or a {dtype} tensor of one value on {device}")
+    return 1, value.data_ptr()
+
+
+def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+          copies=None, grad_scale=1.0, skip=None, seed=0):
+    """One AdamW step, in place, over all of params (float32) with grads (float32, bfloat16 or float16, one
+    type; None: that tensor stays as it is) and state (adamw_state). step: its number, from 1 on.
+    copies: bfloat16 or float16 tensors that receive the new weights too (None entries: none). grad_scale: a factor of
+    the gradients. seed: of the rounding of 8-bit states (the random numbers depend on it, the step and a
+    value's place). lr, step (int64) and grad_scale (else float32) may be GPU tensors of one value; skip, a
+    float32 one: where it is not 0 nothing changes."""
+    if len(params) != len(grads) or (copies is not None and len(copies) != len(params)):
+        raise ValueError("adamw: params, grads and copies must be as many")
+    if not params:
+        return
+    dev = params[0].device
+    if dev.type != "cuda":
+        raise TypeError("hobflops operates on GPU tensors only")
+    pp, _ = _tensors(params, (torch.float32,), dev, "params")
+    sizes = list(map(_numel, params))
+    if list(map(_shape, params)) == [getattr(g, "shape", None) for g in grads]:
+        pg, gtype = _tensors(grads, tuple(_TYPES), dev, "grads")
+    else:
+        here = [i for i, g in enumerate(grads) if g is not None]
+        if any(grads[i].shape != params[i].shape for i in here):
+            raise ValueError("adamw: a gradient has another shape than its tensor")
+        if not here:
+            return
+        ptrs, gtype = _tensors([grads[i] for i in here], tuple(_TYPES), dev, "grads")
+        pg = [0] * len(params)
+        for i, p in zip(here, ptrs):
+            pg[i] = p
+    pc, ctype = [0] * len(params), torch.bfloat16
+    if copies is not None:
+        here = [i for i, c in enumerate(copies) if c is not None]
+        if any(copies[i].shape != params[i].shape for i in here):
+            raise ValueError("adamw: a copy has another shape than its tensor")
+        if here:
+            ptrs, ctype = _tensors([copies[i] for i in here], (torch.bfloat16, torch.float16), dev, "copies")
+            for i, p in zip(here, ptrs):
+                pc[i] = p
+    f = Fmt(0, 0) if state.fmt is None else fmt(state.fmt)
+    total = sum(-(-n // 32) for n in sizes) * 32
+    if state.fmt is None:
+        (pm, ps), (pv, pt) = ((_dense(t, (total,), torch.float32, dev, "adamw state"), None)
+                              for t in (state.m, state.v))
+    else:
+        (pm, ps), (pv, pt) = ((_dense(codes, (total,), torch.uint8, dev, "adamw state codes"),
+                               _dense(scales, (total // 32,), torch.uint8, dev, "adamw state scales"))
+                              for codes, scales in (state.m, state.v))
+    step, step_at = _scalar(step, torch.int64, dev, "step")
+    lr, lr_at = _scalar(lr, torch.float32, dev, "lr")
+    grad_scale, scale_at = _scalar(grad_scale, torch.float32, dev, "grad_scale")
+    skip_at = None
+    if skip is not None:
+        if not isinstance(skip, torch.Tensor):
+            raise TypeError("adamw skip: a float32 GPU tensor of one value is needed")
+        skip_at = _scalar(skip, torch.float32, dev, "skip")[1]
+    d = AdamwDesc(_TYPES[gtype], _TYPES[ctype], f, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
+                  step, seed, lr_at, step_at, scale_at, skip_at)
+    n = len(params)
+    words = [0] * (4 * n)
+    words[0::4], words[1::4], words[2::4], words[3::4] = pp, pg, pc, sizes
+    table = (ctypes.c_int64 * (4 * n))(*words)
+    _call(dev, lib().hobflops_adamw, ctypes.byref(d), table, n, pm, ps, pv, pt, total)
+    # what autograd has kept of these tensors is not theirs any more
+    torch.autograd.graph.increment_version(params if copies is None else
+                                           [*params, *(c for c in copies if c is not None)])
