@@ -798,7 +798,7 @@ int hobflops_layer_norm_workspace(const hobflops_norm_desc* d, int64_t* bytes) {
   if (!bytes) return HOBFLOPS_EINVAL;
   const int st = norm_check(d);
   if (st != HOBFLOPS_OK) return st;
-  *bytes = norm_backward_workspace(d->rows, d->cols);
+  *bytes = norm_backward_workspace(d->rows, d->cols, d->type);
   return HOBFLOPS_OK;
 }
 
@@ -812,7 +812,7 @@ int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, co
   if (d->rows > 0) {
     if (!dy || !x || !mean || !rstd || !dx) return HOBFLOPS_EINVAL;
     if ((dweight || dbias) &&
-        (!workspace || workspace_bytes < norm_backward_workspace(d->rows, d->cols)))
+        (!workspace || workspace_bytes < norm_backward_workspace(d->rows, d->cols, d->type)))
       return HOBFLOPS_EINVAL;
   }
   const int b = type_bytes(d->type), wb = type_bytes(d->wtype);

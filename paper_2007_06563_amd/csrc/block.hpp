@@ -73,7 +73,7 @@ struct LayerNorm {  // a forward or a backward call; dx rows are dense
   float *mean, *rstd;
   void* workspace;
 };
-int64_t norm_backward_workspace(int64_t rows, int64_t cols);
+int64_t norm_backward_workspace(int64_t rows, int64_t cols, int type);
 hipError_t launch_norm_forward(const LayerNorm& p, hipStream_t stream);
 hipError_t launch_norm_backward(const LayerNorm& p, hipStream_t stream);
 

@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "block.hpp"
 #include "columns.hpp"
 #include "lanes.hpp"
@@ -28,35 +30,84 @@ struct NormArgs {
   float eps;
 };
 
-// Eight values of a row; beyond its end zeros.
+// A thread's values at a time: 16 bytes.
 template <class T>
-__device__ __forceinline__ void load8(const typename T::elem* row, int64_t col, int64_t cols,
-                                      typename T::elem (&e)[8]) {
-  if (col + 8 <= cols) {  // 16 bytes at a time whatever the alignment
+constexpr int kVec = 16 / (int)sizeof(typename T::elem);
+
+// V values of a row; beyond its end zeros.
+template <class T, int V>
+__device__ __forceinline__ void load_raw(const typename T::elem* row, int64_t col, int64_t cols,
+                                         typename T::elem (&e)[V]) {
+  if (col + V <= cols) {  // 16 bytes at a time whatever the alignment
     __builtin_memcpy(e, row + col, sizeof e);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = col + j < cols ? row[col + j] : (typename T::elem)0.0f;
+    for (int j = 0; j < V; ++j) e[j] = col + j < cols ? row[col + j] : (typename T::elem)0.0f;
   }
 }
-template <class T>
-__device__ __forceinline__ void load8f(const void* row, int64_t col, int64_t cols, float (&v)[8]) {
-  typename T::elem e[8];
-  load8<T>((const typename T::elem*)row, col, cols, e);
+template <class T, int V>
+__device__ __forceinline__ void load_values(const void* row, int64_t col, int64_t cols, float (&v)[V]) {
+  typename T::elem e[V];
+  load_raw<T, V>((const typename T::elem*)row, col, cols, e);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (float)e[j];
+  for (int j = 0; j < V; ++j) v[j] = (float)e[j];
 }
-template <class T>
-__device__ __forceinline__ void store8(typename T::elem* row, int64_t col, int64_t cols, const float (&v)[8]) {
-  if (col + 8 <= cols) {
-    typename T::elem e[8];
+template <class T, int V>
+__device__ __forceinline__ void store_values(typename T::elem* row, int64_t col, int64_t cols, const float (&v)[V]) {
+  if (col + V <= cols) {
+    typename T::elem e[V];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = (typename T::elem)v[j];
+    for (int j = 0; j < V; ++j) e[j] = (typename T::elem)v[j];
     __builtin_memcpy(row + col, e, sizeof e);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < V; ++j)
       if (col + j < cols) row[col + j] = (typename T::elem)v[j];
+  }
+}
+// 16 bytes of a row as they are, beyond its end zeros, and their values.
+template <class T>
+__device__ __forceinline__ u32x4v load_words(const void* row, int64_t col, int64_t cols) {
+  constexpr int V = kVec<T>;
+  const typename T::elem* src = (const typename T::elem*)row + col;
+  u32x4v w = {0, 0, 0, 0};
+  if (col + V <= cols) {
+    __builtin_memcpy(&w, src, 16);
+  } else if constexpr (V == 4) {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (col + j < cols) w[j] = ((const uint32_t*)src)[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (col + j < cols) w[j >> 1] |= (uint32_t)((const uint16_t*)src)[j] << (16 * (j & 1));
+  }
+  return w;
+}
+template <class T>
+__device__ __forceinline__ float value_of(const u32x4v& w, int j) {
+  if constexpr (kVec<T> == 4) {
+    return __uint_as_float(w[j]);
+  } else if constexpr (std::is_same_v<T, TypeBF16>) {
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
+  } else {
+    const uint16_t h = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    return (float)__builtin_bit_cast(_Float16, h);
+  }
+}
+
+// A vector of all columns, or without one a constant.
+template <class T, int V, int NC>
+__device__ __forceinline__ void load_columns(const void* p, const int64_t (&col)[NC], int64_t cols, float without,
+                                             float (&v)[NC][V]) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    if (p) {
+      load_values<T, V>(p, col[c], cols, v[c]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[c][j] = without;
+    }
   }
 }
 
@@ -101,23 +152,23 @@ struct Stats {
   float mean, off, rstd;  // the mean is mean + off
 };
 
-// A row's values x[NV][8] become their differences from the mean (0 beyond the end).
-template <int NW, int NV>
-__device__ __forceinline__ Stats stats_of(float (&x)[NV][8], const int64_t (&col)[NV], int64_t cols, float eps,
+// A row's values become their differences from the mean (0 beyond the end).
+template <int NW, int NC, int V>
+__device__ __forceinline__ Stats stats_of(float (&x)[NC][V], const int64_t (&col)[NC], int64_t cols, float eps,
                                           float2* lds) {
   const float n = (float)cols;
   float2 s{0.0f, 0.0f};
 #pragma unroll
-  for (int c = 0; c < NV; ++c)
+  for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s.x += x[c][j];
+    for (int j = 0; j < V; ++j) s.x += x[c][j];
   Stats r;
   r.mean = row_sums<NW>(s, lds, 0).x / n;
   s.x = 0.0f;
 #pragma unroll
-  for (int c = 0; c < NV; ++c)
+  for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < V; ++j) {
       x[c][j] = col[c] + j < cols ? x[c][j] - r.mean : 0.0f;
       s.x += x[c][j];
       s.y += x[c][j] * x[c][j];
@@ -131,50 +182,55 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NV][8], const int64_t (&col
   return r;
 }
 
-template <class T, class W, int NW, int NV>
+// A wave, or the NW waves of a workgroup, has a row, a lane NC times 16 bytes of it; the next row is under way
+// while a row's sums meet.
+template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs p) {
   typedef typename T::elem E;
-  constexpr int kRows = NW == 1 ? 4 : 1;  // of a workgroup at a time
+  constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;  // kRows: of a workgroup at a time
   __shared__ float2 lds[2 * NW];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
-  int64_t col[NV];
-  float w[NV][8], b[NV][8];
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
+  if (row >= p.rows) return;
+  int64_t col[NC];
 #pragma unroll
-  for (int c = 0; c < NV; ++c) {
-    col[c] = ((int64_t)c * NW * 64 + lane) * 8;
-    if (p.w)
-      load8f<W>(p.w, col[c], p.cols, w[c]);
-    else
-      for (int j = 0; j < 8; ++j) w[c][j] = 1.0f;
-    if (p.b)
-      load8f<W>(p.b, col[c], p.cols, b[c]);
-    else
-      for (int j = 0; j < 8; ++j) b[c][j] = 0.0f;
-  }
-  for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0); row < p.rows;
-       row += (int64_t)gridDim.x * kRows) {
+  for (int c = 0; c < NC; ++c) col[c] = ((int64_t)c * NW * 64 + lane) * V;
+  u32x4v next[NC];
+  const auto load = [&](int64_t row) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) next[c] = load_words<T>((const E*)p.x + row * p.ldx, col[c], p.cols);
+  };
+  load(row);
+  float w[NC][V], b[NC][V];
+  load_columns<W>(p.w, col, p.cols, 1.0f, w);
+  load_columns<W>(p.b, col, p.cols, 0.0f, b);
+  for (; row < p.rows; row += stride) {
     const E* src = (const E*)p.x + row * p.ldx;
-    float x[NV][8];
+    float x[NC][V];
 #pragma unroll
-    for (int c = 0; c < NV; ++c) load8f<T>(src, col[c], p.cols, x[c]);
-    Stats s = stats_of<NW, NV>(x, col, p.cols, p.eps, lds);
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[c][j] = value_of<T>(next[c], j);
+    if (row + stride < p.rows) load(row + stride);
+    Stats s = stats_of<NW>(x, col, p.cols, p.eps, lds);
     if (!(s.rstd > 0.0f)) {
       // squares beyond float32: the row scaled by a power of two (what is not finite stays NaN)
       float most = 0.0f;
 #pragma unroll
-      for (int c = 0; c < NV; ++c) {
-        load8f<T>(src, col[c], p.cols, x[c]);
+      for (int c = 0; c < NC; ++c) {
+        load_values<T, V>(src, col[c], p.cols, x[c]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[c][j]));
+        for (int j = 0; j < V; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[c][j]));
       }
       most = row_max<NW>(most, lds);
       const int e = (int)(__float_as_uint(most) >> 23) - 127;
       const float down = pow2f(-(e < 126 ? e : 126));
 #pragma unroll
-      for (int c = 0; c < NV; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[c][j] *= down;
-      s = stats_of<NW, NV>(x, col, p.cols, p.eps * down * down, lds);
+        for (int j = 0; j < V; ++j) x[c][j] *= down;
+      s = stats_of<NW>(x, col, p.cols, p.eps * down * down, lds);
       if (p.mean && lane == 0) {
         p.mean[row] = (s.mean + s.off) / down;
         p.rstd[row] = s.rstd * down;
@@ -185,98 +241,131 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
     }
     E* dst = (E*)p.y + row * p.ldy;
 #pragma unroll
-    for (int c = 0; c < NV; ++c) {
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c][j] + b[c][j];
-      store8<T>(dst, col[c], p.cols, x[c]);
+      for (int j = 0; j < V; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c][j] + b[c][j];
+      store_values<T, V>(dst, col[c], p.cols, x[c]);
     }
   }
 }
 
-template <class T, class W, int NW, int NV>
+// As norm_kernel; a lane also keeps its columns' parts of dw and db.
+template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
-  constexpr int kRows = NW == 1 ? 4 : 1;
+  constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;
+  constexpr bool kAhead = NW < 16;  // (16 waves have no registers for the next row; one's loads cover another's sums)
   __shared__ float2 lds[2 * NW];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
-  int64_t col[NV];
-  float w[NV][8], dw[NV][8] = {}, db[NV][8] = {};
-#pragma unroll
-  for (int c = 0; c < NV; ++c) {
-    col[c] = ((int64_t)c * NW * 64 + lane) * 8;
-    if (p.w)
-      load8f<W>(p.w, col[c], p.cols, w[c]);
-    else
-      for (int j = 0; j < 8; ++j) w[c][j] = 1.0f;
-  }
-  const float n = (float)p.cols;
-  const int64_t first = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
   const int64_t stride = (int64_t)gridDim.x * kRows;
-  E xe[NV][8], ge[NV][8];
+  const int64_t first = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
+  int64_t col[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) col[c] = ((int64_t)c * NW * 64 + lane) * V;
+  const float n = (float)p.cols;
+  u32x4v xn[NC], gn[NC], an[NC] = {};  // the next row
   float mean = 0.0f, rstd = 0.0f;
   const auto load = [&](int64_t row) {
     mean = p.mean[row];
     rstd = p.rstd[row];
 #pragma unroll
-    for (int c = 0; c < NV; ++c) {
-      load8<T>((const E*)p.x + row * p.ldx, col[c], p.cols, xe[c]);
-      load8<T>((const E*)p.dy + row * p.ldy, col[c], p.cols, ge[c]);
+    for (int c = 0; c < NC; ++c) {
+      xn[c] = load_words<T>((const E*)p.x + row * p.ldx, col[c], p.cols);
+      gn[c] = load_words<T>((const E*)p.dy + row * p.ldy, col[c], p.cols);
     }
-  };
-  if (first < p.rows) load(first);
-  int place = 0;
-  for (int64_t row = first; row < p.rows; row += stride) {
-    float xh[NV][8], a[NV][8], more[NV][8];
-    // half of the difference, which stays within range, and twice rstd
-    const float half = 0.5f * mean, twice = 2.0f * rstd, r = rstd;
-    float2 s{0.0f, 0.0f};
-#pragma unroll
-    for (int c = 0; c < NV; ++c)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float g = (float)ge[c][j];  // (0 beyond the end)
-        xh[c][j] = __builtin_fmaf(0.5f, (float)xe[c][j], -half) * twice;
-        a[c][j] = g * w[c][j];
-        dw[c][j] += g * xh[c][j];
-        db[c][j] += g;
-        s.x += a[c][j];
-        s.y += a[c][j] * xh[c][j];
-      }
     if (p.add) {
 #pragma unroll
-      for (int c = 0; c < NV; ++c) load8f<T>((const E*)p.add + row * p.ld_add, col[c], p.cols, more[c]);
+      for (int c = 0; c < NC; ++c) an[c] = load_words<T>((const E*)p.add + row * p.ld_add, col[c], p.cols);
     }
-    // the next row is on its way while this one's sums meet
-    if (row + stride < p.rows) load(row + stride);
+  };
+  if (kAhead && first < p.rows) load(first);
+  float w[NC][V], dw[NC][V] = {}, db[NC][V] = {};
+  load_columns<W>(p.w, col, p.cols, 1.0f, w);
+  int place = 0;
+  for (int64_t row = first; row < p.rows; row += stride) {
+    if (!kAhead) load(row);
+    u32x4v xe[NC], ge[NC], ae[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      xe[c] = xn[c];
+      ge[c] = gn[c];
+      ae[c] = an[c];
+    }
+    // half of the difference, which stays within range, and twice rstd
+    const float half = 0.5f * mean, twice = 2.0f * rstd, r = rstd;
+    if (kAhead && row + stride < p.rows) load(row + stride);
+    float2 s{0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float g = value_of<T>(ge[c], j);  // (0 beyond the end)
+        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice, a = g * w[c][j];
+        dw[c][j] += g * xh;
+        db[c][j] += g;
+        s.x += a;
+        s.y += a * xh;
+      }
     s = row_sums<NW>(s, lds, place);
     place ^= 1;
     s.x /= n;
     s.y /= n;
+    // (xh and a are formed again: kept through the sums they would take twice the registers)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm("" : "+v"(xe[c]), "+v"(ge[c]), "+v"(ae[c]));
     E* dst = (E*)p.dx + row * p.cols;
 #pragma unroll
-    for (int c = 0; c < NV; ++c) {
+    for (int c = 0; c < NC; ++c) {
+      float v[V];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        a[c][j] = r * (a[c][j] - s.x - xh[c][j] * s.y);
-        if (p.add) a[c][j] += more[c][j];
+      for (int j = 0; j < V; ++j) {
+        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
+        v[j] = r * (value_of<T>(ge[c], j) * w[c][j] - s.x - xh * s.y);
+        if (p.add) v[j] += value_of<T>(ae[c], j);
       }
-      store8<T>(dst, col[c], p.cols, a[c]);
+      store_values<T, V>(dst, col[c], p.cols, v);
     }
   }
-  if (p.part) {
-    const int64_t wide = (p.cols + 7) & ~(int64_t)7;
-    float* to = p.part + first * 2 * wide;
+  if (!p.part) return;
+  if constexpr (NW == 1) {
+    // the four waves' parts as one, wave after wave
+    __shared__ float sums[2][NC][V][64];
+    for (int i = 1; i < kRows; ++i) {
+      if ((int)threadIdx.x >> 6 == i) {
 #pragma unroll
-    for (int c = 0; c < NV; ++c)
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            sums[0][c][j][lane] = dw[c][j];
+            sums[1][c][j][lane] = db[c][j];
+          }
+      }
+      __syncthreads();
+      if (threadIdx.x < 64) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            dw[c][j] += sums[0][c][j][lane];
+            db[c][j] += sums[1][c][j][lane];
+          }
+      }
+      __syncthreads();
+    }
+  }
+  if (NW > 1 || threadIdx.x < 64) {
+    const int64_t wide = (p.cols + 7) & ~(int64_t)7;
+    float* to = p.part + (int64_t)blockIdx.x * 2 * wide;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
       if (col[c] < p.cols) {
-        __builtin_memcpy(to + col[c], dw[c], 32);
-        __builtin_memcpy(to + wide + col[c], db[c], 32);
+        __builtin_memcpy(to + col[c], dw[c], 4 * V);
+        __builtin_memcpy(to + wide + col[c], db[c], 4 * V);
       }
   }
 }
 
-// Rows of more than kMostCols values: a workgroup walks the row, three times over (from L2 after the first).
-constexpr int64_t kMostCols = 16384;
+// Rows of more than 32 KB: a workgroup walks the row, three times over (from L2 after the first).
 constexpr int kWide = 16;  // waves
 
 template <class T, class Each>
@@ -284,7 +373,7 @@ __device__ __forceinline__ float2 walk(const typename T::elem* row, int64_t cols
   float2 s{0.0f, 0.0f};
   for (int64_t col = (int64_t)threadIdx.x * 8; col < cols; col += kWide * 64 * 8) {
     float v[8];
-    load8f<T>(row, col, cols, v);
+    load_values<T, 8>(row, col, cols, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (col + j < cols) each(s, v[j]);
@@ -315,7 +404,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
       float most = 0.0f;
       for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
         float v[8];
-        load8f<T>(src, col, p.cols, v);
+        load_values<T, 8>(src, col, p.cols, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(v[j]));
       }
@@ -329,13 +418,13 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
     }
     for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
       float v[8], w[8], b[8];
-      load8f<T>(src, col, p.cols, v);
-      if (p.w) load8f<W>(p.w, col, p.cols, w);
-      if (p.b) load8f<W>(p.b, col, p.cols, b);
+      load_values<T, 8>(src, col, p.cols, v);
+      if (p.w) load_values<W, 8>(p.w, col, p.cols, w);
+      if (p.b) load_values<W, 8>(p.b, col, p.cols, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         v[j] = (v[j] * down - mean - off) * rstd * (p.w ? w[j] : 1.0f) + (p.b ? b[j] : 0.0f);
-      store8<T>((E*)p.y + row * p.ldy, col, p.cols, v);
+      store_values<T, 8>((E*)p.y + row * p.ldy, col, p.cols, v);
     }
   }
 }
@@ -352,9 +441,9 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
     float2 s{0.0f, 0.0f};
     for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
       float x[8], g[8], w[8];
-      load8f<T>(src, col, p.cols, x);
-      load8f<T>(dy, col, p.cols, g);
-      if (p.w) load8f<W>(p.w, col, p.cols, w);
+      load_values<T, 8>(src, col, p.cols, x);
+      load_values<T, 8>(dy, col, p.cols, g);
+      if (p.w) load_values<W, 8>(p.w, col, p.cols, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float a = p.w ? g[j] * w[j] : g[j];
@@ -368,16 +457,16 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
     s.y /= n;
     for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
       float x[8], g[8], w[8], more[8];
-      load8f<T>(src, col, p.cols, x);
-      load8f<T>(dy, col, p.cols, g);
-      if (p.w) load8f<W>(p.w, col, p.cols, w);
-      if (p.add) load8f<T>((const E*)p.add + row * p.ld_add, col, p.cols, more);
+      load_values<T, 8>(src, col, p.cols, x);
+      load_values<T, 8>(dy, col, p.cols, g);
+      if (p.w) load_values<W, 8>(p.w, col, p.cols, w);
+      if (p.add) load_values<T, 8>((const E*)p.add + row * p.ld_add, col, p.cols, more);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float a = p.w ? g[j] * w[j] : g[j];
         x[j] = r * (a - s.x - (__builtin_fmaf(0.5f, x[j], -half) * twice) * s.y) + (p.add ? more[j] : 0.0f);
       }
-      store8<T>((E*)p.dx + row * p.cols, col, p.cols, x);
+      store_values<T, 8>((E*)p.dx + row * p.cols, col, p.cols, x);
     }
   }
 }
@@ -391,8 +480,8 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
   float dw[8] = {}, db[8] = {};
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
     float x[8], g[8];
-    load8f<T>((const E*)p.x + row * p.ldx, col, p.cols, x);
-    load8f<T>((const E*)p.dy + row * p.ldy, col, p.cols, g);
+    load_values<T, 8>((const E*)p.x + row * p.ldx, col, p.cols, x);
+    load_values<T, 8>((const E*)p.dy + row * p.ldy, col, p.cols, g);
     const float half = 0.5f * p.mean[row], twice = 2.0f * p.rstd[row];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -406,82 +495,100 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
   __builtin_memcpy(to + wide + col, db, 32);
 }
 
-// Workgroups of a pass, and with them the parts of a sum over rows.
-int64_t forward_groups(int64_t rows, int64_t cols) {
-  const int64_t groups = cols <= 1024 ? (rows + 3) / 4 : rows;
-  return groups < 2048 ? groups : 2048;
+// The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane at most. (Four a lane, 4097 x 2731 float32:
+// backward 40 us, two waves on a SIMD; two a lane 30.)
+struct Shape {
+  int waves;
+  int64_t chunks;  // at most
+};
+constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {4, 256}, {4, 512}, {8, 1024}, {16, 2048}};
+constexpr int kWalk = 6;  // none of them
+int shape_of(int64_t cols, int type) {
+  const int64_t chunks = (cols + (type == HOBFLOPS_TYPE_F32 ? 3 : 7)) / (type == HOBFLOPS_TYPE_F32 ? 4 : 8);
+  int i = 0;
+  while (i < kWalk && chunks > kShapes[i].chunks) ++i;
+  return i;
 }
-int64_t grad_groups(int64_t rows, int64_t cols) {
-  const int64_t groups = cols <= 1024 ? (rows + 3) / 4 : rows;
-  const int64_t most = cols <= 4096 ? 1024 : cols <= 8192 ? 512 : cols <= kMostCols ? 256 : 128;
+// Backward, eight waves of 16-bit values, which are twice as many a lane, would be one workgroup on a CU, or two whose
+// registers spill (8192 x 8192 bfloat16: 226 us); sixteen waves with half of a lane's values take 96.
+bool wide_grad(int shape, int type) { return shape == 4 && type != HOBFLOPS_TYPE_F32; }
+// Workgroups of a pass: about as many as are on the chip at a time (backward: three waves on a SIMD, four of
+// those with 8 or 16 in a workgroup).
+int64_t groups_of(int64_t rows, int64_t cols, int type, bool grad) {
+  const int i = shape_of(cols, type);
+  if (i == kWalk) return rows < 512 ? rows : 512;
+  const int64_t groups = kShapes[i].waves == 1 ? (rows + 3) / 4 : rows;
+  const int64_t most = !grad                                ? (kShapes[i].waves == 16 ? 512 : 2048)
+                       : kShapes[i].waves <= 4              ? 768
+                       : kShapes[i].waves == 8 && !wide_grad(i, type) ? 512
+                                                            : 256;
   return groups < most ? groups : most;
 }
-int64_t parts_of(int64_t rows, int64_t cols) { return grad_groups(rows, cols) * (cols <= 1024 ? 4 : 1); }
-
-template <class T, class W>
-void forward(const NormArgs& p, hipStream_t s) {
-  const unsigned grid = (unsigned)forward_groups(p.rows, p.cols);
-  if (p.cols <= 512)
-    norm_kernel<T, W, 1, 1><<<grid, 256, 0, s>>>(p);
-  else if (p.cols <= 1024)
-    norm_kernel<T, W, 1, 2><<<grid, 256, 0, s>>>(p);
-  else if (p.cols <= 2048)
-    norm_kernel<T, W, 4, 1><<<grid, 256, 0, s>>>(p);
-  else if (p.cols <= 4096)
-    norm_kernel<T, W, 4, 2><<<grid, 256, 0, s>>>(p);
-  else if (p.cols <= 8192)
-    norm_kernel<T, W, 8, 2><<<grid, 512, 0, s>>>(p);
-  else if (p.cols <= kMostCols)
-    norm_kernel<T, W, 16, 2><<<grid, 1024, 0, s>>>(p);
-  else
-    norm_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
-}
-
-template <class T, class W>
-void backward(const NormArgs& p, void* dw, void* db, hipStream_t s) {
-  if (p.rows > 0) {
-    const unsigned grid = (unsigned)grad_groups(p.rows, p.cols);
-    if (p.cols <= 512) {
-      norm_grad_kernel<T, W, 1, 1><<<grid, 256, 0, s>>>(p);
-    } else if (p.cols <= 1024) {
-      norm_grad_kernel<T, W, 1, 2><<<grid, 256, 0, s>>>(p);
-    } else if (p.cols <= 2048) {
-      norm_grad_kernel<T, W, 4, 1><<<grid, 256, 0, s>>>(p);
-    } else if (p.cols <= 4096) {
-      norm_grad_kernel<T, W, 4, 2><<<grid, 256, 0, s>>>(p);
-    } else if (p.cols <= 8192) {
-      norm_grad_kernel<T, W, 8, 2><<<grid, 512, 0, s>>>(p);
-    } else if (p.cols <= kMostCols) {
-      norm_grad_kernel<T, W, 16, 2><<<grid, 1024, 0, s>>>(p);
-    } else {
-      const unsigned walkers = (unsigned)(p.rows < 2048 ? p.rows : 2048);
-      norm_grad_wide_kernel<T, W><<<walkers, kWide * 64, 0, s>>>(p);
-      if (p.part)
-        norm_columns_kernel<T><<<dim3((unsigned)((p.cols + 2047) / 2048), grid), 256, 0, s>>>(p);
-    }
-  }
-  if (dw || db) {
-    const int64_t wide = (p.cols + 7) & ~(int64_t)7;
-    const int64_t parts = parts_of(p.rows, p.cols);
-    launch_column_sums<W>(p.part, parts, 2 * wide, dw, db, p.cols, wide, s);
-  }
-}
-
-}  // namespace
-
-int64_t norm_backward_workspace(int64_t rows, int64_t cols) {
-  return parts_of(rows, cols) * 2 * ((cols + 7) & ~(int64_t)7) * 4;
+// The parts of the sums over rows: one a workgroup.
+constexpr int64_t kWideParts = 128;
+int64_t parts_of(int64_t rows, int64_t cols, int type) {
+  if (shape_of(cols, type) == kWalk) return rows < kWideParts ? rows : kWideParts;
+  return groups_of(rows, cols, type, true);
 }
 
 template <class T>
-static void norm_of(const LayerNorm& c, const NormArgs& p, bool back, hipStream_t s) {
-  if (c.wtype == HOBFLOPS_TYPE_F32)
-    back ? backward<T, TypeF32>(p, c.dw, c.db, s) : forward<T, TypeF32>(p, s);
-  else
-    back ? backward<T, T>(p, c.dw, c.db, s) : forward<T, T>(p, s);
+constexpr int kType = kVec<T> == 4 ? HOBFLOPS_TYPE_F32 : HOBFLOPS_TYPE_BF16;  // (either 16-bit type)
+
+template <class T, class W, int NW, int NC>
+void launch_grad(const NormArgs& p, hipStream_t s) {
+  norm_grad_kernel<T, W, NW, NC>
+      <<<(unsigned)groups_of(p.rows, p.cols, kType<T>, true), NW == 1 ? 256 : NW * 64, 0, s>>>(p);
+}
+template <class T, class W, int NW, int NC>
+void launch(const NormArgs& p, bool grad, hipStream_t s) {
+  if constexpr (NW != 8 || kVec<T> == 4) {
+    if (grad) return launch_grad<T, W, NW, NC>(p, s);
+  }
+  norm_kernel<T, W, NW, NC>
+      <<<(unsigned)groups_of(p.rows, p.cols, kType<T>, false), NW == 1 ? 256 : NW * 64, 0, s>>>(p);
+}
+template <class T, class W>
+void launch_rows(const NormArgs& p, bool grad, hipStream_t s) {
+  if (p.rows == 0) return;
+  switch (shape_of(p.cols, kType<T>)) {
+    case 0: return launch<T, W, 1, 1>(p, grad, s);
+    case 1: return launch<T, W, 1, 2>(p, grad, s);
+    case 2: return launch<T, W, 4, 1>(p, grad, s);
+    case 3: return launch<T, W, 4, 2>(p, grad, s);
+    case 4:
+      if constexpr (kVec<T> == 8) {
+        if (grad) return launch_grad<T, W, 16, 1>(p, s);
+      }
+      return launch<T, W, 8, 2>(p, grad, s);
+    case 5: return launch<T, W, 16, 2>(p, grad, s);
+  }
+  const unsigned grid = (unsigned)groups_of(p.rows, p.cols, kType<T>, grad);
+  if (grad) {
+    norm_grad_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
+    if (p.part)
+      norm_columns_kernel<T><<<dim3((unsigned)((p.cols + 2047) / 2048), (unsigned)parts_of(p.rows, p.cols, kType<T>)), 256,
+                               0, s>>>(p);
+  } else {
+    norm_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
+  }
 }
 
-static hipError_t norm_run(const LayerNorm& c, bool back, hipStream_t s) {
+template <class T, class W>
+void run_types(const LayerNorm& c, const NormArgs& p, bool grad, hipStream_t s) {
+  launch_rows<T, W>(p, grad, s);
+  if (!grad || !(c.dw || c.db)) return;
+  const int64_t wide = (p.cols + 7) & ~(int64_t)7;
+  launch_column_sums<W>(p.part, parts_of(p.rows, p.cols, kType<T>), 2 * wide, c.dw, c.db, p.cols, wide, s);
+}
+template <class T>
+void run_type(const LayerNorm& c, const NormArgs& p, bool grad, hipStream_t s) {
+  if (c.wtype == HOBFLOPS_TYPE_F32)
+    run_types<T, TypeF32>(c, p, grad, s);
+  else
+    run_types<T, T>(c, p, grad, s);
+}
+
+hipError_t run(const LayerNorm& c, bool grad, hipStream_t s) {
   NormArgs p{};
   p.x = c.x;
   p.w = c.w;
@@ -499,13 +606,18 @@ static hipError_t norm_run(const LayerNorm& c, bool back, hipStream_t s) {
   p.ldy = c.ldy;
   p.ld_add = c.ld_add;
   p.eps = (float)c.eps;
-  if (c.type == HOBFLOPS_TYPE_F32) norm_of<TypeF32>(c, p, back, s);
-  if (c.type == HOBFLOPS_TYPE_BF16) norm_of<TypeBF16>(c, p, back, s);
-  if (c.type == HOBFLOPS_TYPE_F16) norm_of<TypeF16>(c, p, back, s);
+  if (c.type == HOBFLOPS_TYPE_F32) run_type<TypeF32>(c, p, grad, s);
+  if (c.type == HOBFLOPS_TYPE_BF16) run_type<TypeBF16>(c, p, grad, s);
+  if (c.type == HOBFLOPS_TYPE_F16) run_type<TypeF16>(c, p, grad, s);
   return hipGetLastError();
 }
 
-hipError_t launch_norm_forward(const LayerNorm& c, hipStream_t s) { return norm_run(c, false, s); }
-hipError_t launch_norm_backward(const LayerNorm& c, hipStream_t s) { return norm_run(c, true, s); }
+}  // namespace
+
+int64_t norm_backward_workspace(int64_t rows, int64_t cols, int type) {
+  return parts_of(rows, cols, type) * 2 * ((cols + 7) & ~(int64_t)7) * 4;
+}
+hipError_t launch_norm_forward(const LayerNorm& c, hipStream_t s) { return run(c, false, s); }
+hipError_t launch_norm_backward(const LayerNorm& c, hipStream_t s) { return run(c, true, s); }
 
 }  // namespace hobflops
