@@ -423,7 +423,7 @@ int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* 
  *   dx = rstd (a - mean(a) - xh mean(a xh)) + add, dweight = sum over rows of dy xh,
  *   dbias = sum over rows of dy
  * add (rows ld_add apart; NULL: none): a gradient that reaches x past the norm, joined before the one rounding. dx is
- * dense, and may be add (dense, then), but not x or dy. dweight and dbias of wtype, either may be NULL. Sums run in a
+ * dense and overlaps none of the call's inputs. dweight and dbias of wtype, either may be NULL. Sums run in a
  * fixed order. The workspace is needed where one of these two is asked for. */
 int hobflops_layer_norm_workspace(const hobflops_norm_desc* d, int64_t* bytes);
 int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, const void* x,

@@ -25,7 +25,7 @@ namespace {
 struct NormArgs {
   const void *x, *w, *b, *dy, *add;
   void *y, *dx;
-  float *mean, *rstd, *part;  // part: [parts][2][cols rounded up to 8]
+  float *mean, *rstd, *part;  // part: [parts][2][cols]
   int64_t rows, cols, ldx, ldy, ld_add;  // ldy: of y or of dy
   float eps;
 };
@@ -65,24 +65,36 @@ __device__ __forceinline__ void store_values(typename T::elem* row, int64_t col,
       if (col + j < cols) row[col + j] = (typename T::elem)v[j];
   }
 }
-// 16 bytes of a row as they are, beyond its end zeros, and their values.
+// The 16 bytes of a row that a lane has: of those that would pass the row's end the last ones of the row, so that every
+// load and store is a whole one. The first `lead` of their values are another lane's as well: both compute and store
+// them alike, and this one leaves them out of the row's sums. (A row has at least as many values; of NC times 16 bytes a
+// lane only the last half may pass the end, by the choice of NC.)
 template <class T>
-__device__ __forceinline__ u32x4v load_words(const void* row, int64_t col, int64_t cols) {
-  constexpr int V = kVec<T>;
-  const typename T::elem* src = (const typename T::elem*)row + col;
-  u32x4v w = {0, 0, 0, 0};
-  if (col + V <= cols) {
-    __builtin_memcpy(&w, src, 16);
-  } else if constexpr (V == 4) {
-#pragma unroll
-    for (int j = 0; j < 3; ++j)
-      if (col + j < cols) w[j] = ((const uint32_t*)src)[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (col + j < cols) w[j >> 1] |= (uint32_t)((const uint16_t*)src)[j] << (16 * (j & 1));
+struct Chunk {
+  int at, lead;
+  bool there;  // not all of them another lane's
+  __device__ __forceinline__ void start(int col, int cols) {
+    constexpr int V = kVec<T>;
+    at = col + V <= cols ? col : cols - V;
+    lead = col - at;
+    there = lead < V;
   }
-  return w;
+  __device__ __forceinline__ u32x4v load(const void* row) const {
+    u32x4v w;
+    __builtin_memcpy(&w, (const typename T::elem*)row + at, 16);
+    return w;
+  }
+  __device__ __forceinline__ void store(void* row, const float (&v)[kVec<T>]) const {
+    typename T::elem e[kVec<T>];
+#pragma unroll
+    for (int j = 0; j < kVec<T>; ++j) e[j] = (typename T::elem)v[j];
+    if (there) __builtin_memcpy((typename T::elem*)row + at, e, 16);
+  }
+};
+// Values of a chunk as they count for sums.
+template <int NC>
+__device__ __forceinline__ float counted(float v, int c, int j, int lead) {
+  return c < NC / 2 || j >= lead ? v : 0.0f;
 }
 template <class T>
 __device__ __forceinline__ float value_of(const u32x4v& w, int j) {
@@ -96,18 +108,16 @@ __device__ __forceinline__ float value_of(const u32x4v& w, int j) {
   }
 }
 
-// A vector of all columns, or without one a constant.
-template <class T, int V, int NC>
-__device__ __forceinline__ void load_columns(const void* p, const int64_t (&col)[NC], int64_t cols, float without,
-                                             float (&v)[NC][V]) {
+// A lane's values of a vector of all columns, or without one a constant.
+template <class T, class W, int NC>
+__device__ __forceinline__ void load_columns(const void* p, const Chunk<T> (&chunk)[NC], float without,
+                                             float (&v)[NC][kVec<T>]) {
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    if (p) {
-      load_values<T, V>(p, col[c], cols, v[c]);
-    } else {
+    typename W::elem e[kVec<T>];
+    if (p) __builtin_memcpy(e, (const typename W::elem*)p + chunk[c].at, sizeof e);
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[c][j] = without;
-    }
+    for (int j = 0; j < kVec<T>; ++j) v[c][j] = p ? (float)e[j] : without;
   }
 }
 
@@ -152,16 +162,17 @@ struct Stats {
   float mean, off, rstd;  // the mean is mean + off
 };
 
-// A row's values become their differences from the mean (0 beyond the end).
-template <int NW, int NC, int V>
-__device__ __forceinline__ Stats stats_of(float (&x)[NC][V], const int64_t (&col)[NC], int64_t cols, float eps,
-                                          float2* lds) {
+// A row's values become their differences from the mean.
+template <class T, int NW, int NC>
+__device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T> (&chunk)[NC], int64_t cols,
+                                          float eps, float2* lds) {
+  constexpr int V = kVec<T>;
   const float n = (float)cols;
   float2 s{0.0f, 0.0f};
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int j = 0; j < V; ++j) s.x += x[c][j];
+    for (int j = 0; j < V; ++j) s.x += counted<NC>(x[c][j], c, j, chunk[c].lead);
   Stats r;
   r.mean = row_sums<NW>(s, lds, 0).x / n;
   s.x = 0.0f;
@@ -169,9 +180,10 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][V], const int64_t (&col
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      x[c][j] = col[c] + j < cols ? x[c][j] - r.mean : 0.0f;
-      s.x += x[c][j];
-      s.y += x[c][j] * x[c][j];
+      x[c][j] -= r.mean;
+      const float d = counted<NC>(x[c][j], c, j, chunk[c].lead);
+      s.x += d;
+      s.y += d * d;
     }
   s = row_sums<NW>(s, lds, 1);
   r.off = s.x / n;
@@ -193,35 +205,37 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
   if (row >= p.rows) return;
-  int64_t col[NC];
+  Chunk<T> chunk[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) col[c] = ((int64_t)c * NW * 64 + lane) * V;
+  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * 64 + lane) * V, (int)p.cols);
   u32x4v next[NC];
   const auto load = [&](int64_t row) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) next[c] = load_words<T>((const E*)p.x + row * p.ldx, col[c], p.cols);
+    for (int c = 0; c < NC; ++c) next[c] = chunk[c].load((const E*)p.x + row * p.ldx);
   };
   load(row);
   float w[NC][V], b[NC][V];
-  load_columns<W>(p.w, col, p.cols, 1.0f, w);
-  load_columns<W>(p.b, col, p.cols, 0.0f, b);
+  load_columns<T, W>(p.w, chunk, 1.0f, w);
+  load_columns<T, W>(p.b, chunk, 0.0f, b);
   for (; row < p.rows; row += stride) {
-    const E* src = (const E*)p.x + row * p.ldx;
     float x[NC][V];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int j = 0; j < V; ++j) x[c][j] = value_of<T>(next[c], j);
-    if (row + stride < p.rows) load(row + stride);
-    Stats s = stats_of<NW>(x, col, p.cols, p.eps, lds);
+    load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
+    Stats s = stats_of<T, NW>(x, chunk, p.cols, p.eps, lds);
     if (!(s.rstd > 0.0f)) {
       // squares beyond float32: the row scaled by a power of two (what is not finite stays NaN)
       float most = 0.0f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        load_values<T, V>(src, col[c], p.cols, x[c]);
+        const u32x4v v = chunk[c].load((const E*)p.x + row * p.ldx);
 #pragma unroll
-        for (int j = 0; j < V; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[c][j]));
+        for (int j = 0; j < V; ++j) {
+          x[c][j] = value_of<T>(v, j);
+          most = __builtin_fmaxf(most, __builtin_fabsf(x[c][j]));
+        }
       }
       most = row_max<NW>(most, lds);
       const int e = (int)(__float_as_uint(most) >> 23) - 127;
@@ -230,7 +244,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int j = 0; j < V; ++j) x[c][j] *= down;
-      s = stats_of<NW>(x, col, p.cols, p.eps * down * down, lds);
+      s = stats_of<T, NW>(x, chunk, p.cols, p.eps * down * down, lds);
       if (p.mean && lane == 0) {
         p.mean[row] = (s.mean + s.off) / down;
         p.rstd[row] = s.rstd * down;
@@ -239,12 +253,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
       p.mean[row] = s.mean + s.off;
       p.rstd[row] = s.rstd;
     }
-    E* dst = (E*)p.y + row * p.ldy;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
       for (int j = 0; j < V; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c][j] + b[c][j];
-      store_values<T, V>(dst, col[c], p.cols, x[c]);
+      chunk[c].store((E*)p.y + row * p.ldy, x[c]);
     }
   }
 }
@@ -254,14 +267,13 @@ template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
   constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;
-  constexpr bool kAhead = NW < 16;  // (16 waves have no registers for the next row; one's loads cover another's sums)
   __shared__ float2 lds[2 * NW];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   const int64_t first = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
-  int64_t col[NC];
+  Chunk<T> chunk[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) col[c] = ((int64_t)c * NW * 64 + lane) * V;
+  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * 64 + lane) * V, (int)p.cols);
   const float n = (float)p.cols;
   u32x4v xn[NC], gn[NC], an[NC] = {};  // the next row
   float mean = 0.0f, rstd = 0.0f;
@@ -270,20 +282,19 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     rstd = p.rstd[row];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      xn[c] = load_words<T>((const E*)p.x + row * p.ldx, col[c], p.cols);
-      gn[c] = load_words<T>((const E*)p.dy + row * p.ldy, col[c], p.cols);
+      xn[c] = chunk[c].load((const E*)p.x + row * p.ldx);
+      gn[c] = chunk[c].load((const E*)p.dy + row * p.ldy);
     }
     if (p.add) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) an[c] = load_words<T>((const E*)p.add + row * p.ld_add, col[c], p.cols);
+      for (int c = 0; c < NC; ++c) an[c] = chunk[c].load((const E*)p.add + row * p.ld_add);
     }
   };
-  if (kAhead && first < p.rows) load(first);
+  if (first < p.rows) load(first);
   float w[NC][V], dw[NC][V] = {}, db[NC][V] = {};
-  load_columns<W>(p.w, col, p.cols, 1.0f, w);
+  load_columns<T, W>(p.w, chunk, 1.0f, w);
   int place = 0;
   for (int64_t row = first; row < p.rows; row += stride) {
-    if (!kAhead) load(row);
     u32x4v xe[NC], ge[NC], ae[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -293,18 +304,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     }
     // half of the difference, which stays within range, and twice rstd
     const float half = 0.5f * mean, twice = 2.0f * rstd, r = rstd;
-    if (kAhead && row + stride < p.rows) load(row + stride);
+    load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
     float2 s{0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float g = value_of<T>(ge[c], j);  // (0 beyond the end)
-        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice, a = g * w[c][j];
-        dw[c][j] += g * xh;
-        db[c][j] += g;
+        const float g = value_of<T>(ge[c], j);
+        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
+        const float a = counted<NC>(g * w[c][j], c, j, chunk[c].lead);
         s.x += a;
-        s.y += a * xh;
+        s.y += a * counted<NC>(xh, c, j, chunk[c].lead);
       }
     s = row_sums<NW>(s, lds, place);
     place ^= 1;
@@ -313,17 +323,19 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     // (xh and a are formed again: kept through the sums they would take twice the registers)
 #pragma unroll
     for (int c = 0; c < NC; ++c) asm("" : "+v"(xe[c]), "+v"(ge[c]), "+v"(ae[c]));
-    E* dst = (E*)p.dx + row * p.cols;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float v[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
+        const float g = value_of<T>(ge[c], j);
         const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
-        v[j] = r * (value_of<T>(ge[c], j) * w[c][j] - s.x - xh * s.y);
+        dw[c][j] += g * xh;
+        db[c][j] += g;
+        v[j] = r * (g * w[c][j] - s.x - xh * s.y);
         if (p.add) v[j] += value_of<T>(ae[c], j);
       }
-      store_values<T, V>(dst, col[c], p.cols, v);
+      chunk[c].store((E*)p.dx + row * p.cols, v);
     }
   }
   if (!p.part) return;
@@ -354,18 +366,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     }
   }
   if (NW > 1 || threadIdx.x < 64) {
-    const int64_t wide = (p.cols + 7) & ~(int64_t)7;
-    float* to = p.part + (int64_t)blockIdx.x * 2 * wide;
+    float* to = p.part + (int64_t)blockIdx.x * 2 * p.cols;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (col[c] < p.cols) {
-        __builtin_memcpy(to + col[c], dw[c], 4 * V);
-        __builtin_memcpy(to + wide + col[c], db[c], 4 * V);
+      if (chunk[c].there) {
+        __builtin_memcpy(to + chunk[c].at, dw[c], 4 * V);
+        __builtin_memcpy(to + p.cols + chunk[c].at, db[c], 4 * V);
       }
   }
 }
 
-// Rows of more than 32 KB: a workgroup walks the row, three times over (from L2 after the first).
+// Rows of more than 32 KB, or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the first).
 constexpr int kWide = 16;  // waves
 
 template <class T, class Each>
@@ -489,10 +500,13 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
       db[j] += g[j];
     }
   }
-  const int64_t wide = (p.cols + 7) & ~(int64_t)7;
-  float* to = p.part + (int64_t)blockIdx.y * 2 * wide;
-  __builtin_memcpy(to + col, dw, 32);
-  __builtin_memcpy(to + wide + col, db, 32);
+  float* to = p.part + (int64_t)blockIdx.y * 2 * p.cols + col;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (col + j < p.cols) {
+      to[j] = dw[j];
+      to[p.cols + j] = db[j];
+    }
 }
 
 // The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane at most. (Four a lane, 4097 x 2731 float32:
@@ -502,9 +516,10 @@ struct Shape {
   int64_t chunks;  // at most
 };
 constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {4, 256}, {4, 512}, {8, 1024}, {16, 2048}};
-constexpr int kWalk = 6;  // none of them
+constexpr int kWalk = 6;  // none of them: the rows are walked
 int shape_of(int64_t cols, int type) {
   const int64_t chunks = (cols + (type == HOBFLOPS_TYPE_F32 ? 3 : 7)) / (type == HOBFLOPS_TYPE_F32 ? 4 : 8);
+  if (cols < (type == HOBFLOPS_TYPE_F32 ? 4 : 8)) return kWalk;  // (no whole 16 bytes)
   int i = 0;
   while (i < kWalk && chunks > kShapes[i].chunks) ++i;
   return i;
@@ -577,8 +592,7 @@ template <class T, class W>
 void run_types(const LayerNorm& c, const NormArgs& p, bool grad, hipStream_t s) {
   launch_rows<T, W>(p, grad, s);
   if (!grad || !(c.dw || c.db)) return;
-  const int64_t wide = (p.cols + 7) & ~(int64_t)7;
-  launch_column_sums<W>(p.part, parts_of(p.rows, p.cols, kType<T>), 2 * wide, c.dw, c.db, p.cols, wide, s);
+  launch_column_sums<W>(p.part, parts_of(p.rows, p.cols, kType<T>), 2 * p.cols, c.dw, c.db, p.cols, p.cols, s);
 }
 template <class T>
 void run_type(const LayerNorm& c, const NormArgs& p, bool grad, hipStream_t s) {
@@ -615,7 +629,7 @@ hipError_t run(const LayerNorm& c, bool grad, hipStream_t s) {
 }  // namespace
 
 int64_t norm_backward_workspace(int64_t rows, int64_t cols, int type) {
-  return parts_of(rows, cols, type) * 2 * ((cols + 7) & ~(int64_t)7) * 4;
+  return parts_of(rows, cols, type) * 2 * cols * 4;
 }
 hipError_t launch_norm_forward(const LayerNorm& c, hipStream_t s) { return run(c, false, s); }
 hipError_t launch_norm_backward(const LayerNorm& c, hipStream_t s) { return run(c, true, s); }
