@@ -2,7 +2,7 @@
 //   z = x W^T + b,  dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum over rows of dz.
 // Products run on the 16x16x32 matrix instruction with float32 sums, to which bias, activation and residual are
 // applied before the one rounding of y. Few tokens read the weights once, straight to registers
-// (few_kernel); more go through LDS in tiles (gemm.hpp). Where tiles are too few for the chip, a sum is
+// (direct_kernel); more go through LDS in tiles (gemm.hpp). Where tiles are too few for the chip, a sum is
 // split and its parts are joined in their order in a second launch, which then has the epilogue.
 //
 // Roundings to 16 bits: y, dx, dW and db once each; z, kept for the backward pass, and dz as operand of
@@ -22,7 +22,49 @@ namespace {
 
 constexpr int kNoAct = HOBFLOPS_GATE_NONE;
 
-__device__ __forceinline__ float act_of(float z, int act) { return act == kNoAct ? z : gate_act(z, act); }
+// The activations for results of 16 bits: relative errors of some 2^-20, tails included, in about half of the
+// instructions of gate_act (a tile's epilogue runs them with nothing beside: of 4096 x 4096 -> 11264, 369 us
+// with a gelu of erfc).
+// The normal distribution beyond |z|, over its density's exponential: exp(z^2 / 2) Phi(-|z|) as a polynomial of
+// 1 / (1 + 0.35 |z|), fitted to a relative 3.2e-7 for |z| <= 14.5 (beyond it the product is below float32's range).
+__device__ __forceinline__ float tail_ratio(float a) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.0f));
+  float r = __builtin_fmaf(0.0489021204f, t, -0.201967299f);
+  r = __builtin_fmaf(r, t, 0.240405872f);
+  r = __builtin_fmaf(r, t, -0.0168311354f);
+  r = __builtin_fmaf(r, t, 0.155871853f);
+  r = __builtin_fmaf(r, t, 0.133378804f);
+  r = __builtin_fmaf(r, t, 0.140267059f);
+  return __builtin_fmaf(r, t, -2.71316530e-5f);
+}
+struct Gate {
+  float p, e;  // the gate, and (gelu) exp(-z^2 / 2)
+};
+__device__ __forceinline__ Gate gelu_gate(float z) {
+  const float a = __builtin_fabsf(z), e = exp2f(z * z * -0.721347520f), q = e * tail_ratio(a);
+  return Gate{z < 0.0f ? q : 1.0f - q, e};
+}
+// sigmoid(z) and sigmoid(-z)
+__device__ __forceinline__ Sigmoid silu_gate(float z) {
+  const float e = exp2f(__builtin_fabsf(z) * -1.44269504f), r = __builtin_amdgcn_rcpf(1.0f + e), far = e * r;
+  return z < 0.0f ? Sigmoid{far, r} : Sigmoid{r, far};
+}
+__device__ __forceinline__ float act_of(float z, int act) {
+  if (act == HOBFLOPS_GATE_SILU) return z * silu_gate(z).s;
+  if (act == HOBFLOPS_GATE_GELU) return z * gelu_gate(z).p;
+  return act == kNoAct || z > 0.0f || z != z ? z : 0.0f;
+}
+__device__ __forceinline__ float act_grad_of(float z, int act) {
+  if (act == HOBFLOPS_GATE_SILU) {
+    const Sigmoid v = silu_gate(z);
+    return v.s * __builtin_fmaf(z, v.c, 1.0f);
+  }
+  if (act == HOBFLOPS_GATE_GELU) {
+    const Gate v = gelu_gate(z);
+    return __builtin_fmaf(z, v.e * 0.398942280f, v.p);
+  }
+  return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+}
 
 struct LinearArgs {
   const void *w, *x, *bias, *residual;
@@ -125,7 +167,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
         for (int k = 0; k < 8; ++k) {
           const float e = v[k >> 2][k & 3] + bias[k];
           z[k] = (E)e;
-          v[k >> 2][k & 3] = gate_act(e, p.act);
+          v[k >> 2][k & 3] = act_of(e, p.act);
         }
         if (p.z && t < p.T_) store8((E*)p.z + t * p.N, z);
         at[0] = v[0];
@@ -207,17 +249,10 @@ __global__ __launch_bounds__(512, 2) void linear_kernel(LinearArgs p) {
 }
 // 128 x 128 sums, two workgroups on a CU.
 template <class T>
-__global__ __launch_bounds__(256, 2) void linear_middle_kernel(LinearArgs p) {
+__global__ __launch_bounds__(256, 2) void linear_small_kernel(LinearArgs p) {
   HOBFLOPS_STAGES2(128, 128);
   linear_tile<T, 128, 128, 2, 2, 2>(p, sa, sb);
 }
-// 64 x 64 sums, three workgroups on a CU.
-template <class T>
-__global__ __launch_bounds__(256, 3) void linear_small_kernel(LinearArgs p) {
-  HOBFLOPS_STAGES3(64, 64);
-  linear_tile<T, 64, 64, 2, 2, 3>(p, sa, sb);
-}
-
 // The parts of a sum in their order, then the epilogue: 4 values a thread.
 template <class T>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int splits) {
@@ -241,73 +276,156 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int spli
   }
 }
 
-// Up to 16 tokens: a workgroup has 16 rows of W, its waves every kFewWaves-th 64 k of them, the lane 16 k of one
-// row each time (32 bytes), so that the four lanes of a row read a whole line. The same k of x is the other operand: which
-// k a lane has does not matter as long as both operands agree. The waves' sums meet in LDS.
-constexpr int kFewWaves = 8;
-template <class T>
-__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(LinearArgs p) {
+// Few tokens or small layers, rows of any alignment: a workgroup has 16 NI rows of W and 16 NJ tokens, its waves
+// every kDirectWaves-th 64 k of them, each by itself: U times 64 k are under way to its registers (eight lanes read a
+// row's line of 128 bytes), go through its own part of LDS into the matrix instruction's order, and no wave
+// waits for another before the end, where the waves' sums meet, are added in the waves' order and take the
+// epilogue. (Loading the matrix instruction's order from memory, where neighbouring lanes have different rows, reads
+// 45 bytes a nanosecond on a CU at most.)
+constexpr int kDirectWaves = 8;
+#ifdef __HIP_DEVICE_COMPILE__
+// The loads of N times 16 rows and 64 k: 8 rows each.
+template <class T, int N>
+struct DirectRows {
+  const typename T::elem* row[2 * N];  // the lane's, at its k
+  int k[2];                            // of loads 0, 2, .. and 1, 3, ..
+  __device__ __forceinline__ void start(const void* p, int64_t ld, int64_t rows, int64_t row0, int lane) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) k[i] = 8 * ((lane & 7) ^ ((4 * i + (lane >> 4)) & 7));
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) {
+      // rows beyond the end: the last one again, whose sums nobody stores
+      const int64_t r = row0 + 8 * i + (lane >> 3);
+      row[i] = (const typename T::elem*)p + (r < rows ? r : rows - 1) * ld + k[i & 1];
+    }
+  }
+  __device__ __forceinline__ void load(u32x4v (&v)[2 * N], int64_t k0) const {
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) __builtin_memcpy(&v[i], row[i] + k0, 16);
+  }
+  // The last, fewer than 64 values of a row, from k0 to K, and zeros.
+  __device__ __forceinline__ void load_end(u32x4v (&v)[2 * N], int64_t k0, int64_t K) const {
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) {
+      const int over = (int)(k0 + k[i & 1] + 8 - K);  // values of the lane's 8 beyond the end
+      if (K >= 8) {
+        // the 8 values that end there
+        __builtin_memcpy(&v[i], row[i] + k0 - (over > 0 ? over : 0), 16);
+        if (over > 0) v[i] = shifted_down(v[i], over < 8 ? (uint32_t)over * 16 : 128);
+      } else {
+        v[i] = u32x4v{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+          if (j < 8 - over) v[i][j >> 1] |= (uint32_t)((const uint16_t*)(row[i] + k0))[j] << (16 * (j & 1));
+      }
+    }
+  }
+};
+#endif
+
+template <class T, int NI, int NJ, int U>
+__global__ __launch_bounds__(kDirectWaves * 64) void direct_kernel(LinearArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__
   typedef typename T::elem E;
   typedef typename T::vec8 Vec;
-  __shared__ f32x4 sums[kFewWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane & 15, q = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
-  // rows and tokens beyond the end: the last one again, whose sums nobody stores
-  const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1, t = r < p.T_ ? r : p.T_ - 1;
-  const E *w = (const E*)p.w + n * p.ldw + 16 * q, *x = (const E*)p.x + t * p.ldx + 16 * q;
-  const int64_t whole = p.K / 64;
-  f32x4 acc = {};
-  constexpr int U = 4;
-  int64_t c = wave;
-  for (; c + (U - 1) * kFewWaves < whole; c += U * kFewWaves) {
-    Vec a[U][2], b[U][2];
+  constexpr int kStage = (NI + NJ) * 2048, kSums = NI * NJ * 1024;
+  __shared__ __align__(1024) uint8_t lds[kDirectWaves * (kStage > kSums ? kStage : kSums)];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t ti, tj;
+  tile_of(blockIdx.x, p.ni, p.nj, ti, tj);
+  const int64_t f0 = (int64_t)ti * NI * 16, t0 = (int64_t)tj * NJ * 16;
+  DirectRows<T, NI> la;
+  DirectRows<T, NJ> lb;
+  la.start(p.w, p.ldw, p.N, f0, lane);
+  lb.start(p.x, p.ldx, p.T_, t0, lane);
+  ReadRows<T, NI, 0> ra;
+  ReadRows<T, NJ, 0> rb;
+  ra.start(0, lane);
+  rb.start(0, lane);
+  uint8_t *const sa = lds + wave * kStage, *const sb = sa + NI * 2048;
+  u32x4v a[U][2 * NI], b[U][2 * NJ];
+  f32x4 acc[NI][NJ] = {};
+  const auto write = [&](int u) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      __builtin_memcpy(a[u], w + (c + u * kFewWaves) * 64, 32);
-      __builtin_memcpy(b[u], x + (c + u * kFewWaves) * 64, 32);
+    for (int i = 0; i < 2 * NI; ++i) *(u32x4v*)(sa + i * 1024 + lane * 16) = a[u][i];
+#pragma unroll
+    for (int i = 0; i < 2 * NJ; ++i) *(u32x4v*)(sb + i * 1024 + lane * 16) = b[u][i];
+    wave_sync();
+  };
+  const auto multiply = [&] {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      Vec fa[NI], fb[NJ];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fa[i] = ra.get(sa, i, ks);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fb[j] = rb.get(sb, j, ks);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
     }
+    wave_sync();
+  };
+  // the wave's whole 64 k
+  const int64_t whole = p.K / 64, mine = (whole - wave + kDirectWaves - 1) / kDirectWaves;
+  if (mine > 0) {
+    // (beyond the last the last one again, which nobody multiplies)
+    const auto load = [&](int u, int64_t n) {
+      const int64_t k = ((n < mine ? n : mine - 1) * kDirectWaves + wave) * 64;
+      la.load(a[u], k);
+      lb.load(b[u], k);
+    };
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      acc = T::mfma(a[u][0], b[u][0], acc);
-      acc = T::mfma(a[u][1], b[u][1], acc);
-    }
-  }
-  for (; c * 64 < p.K; c += kFewWaves) {
-    Vec a[2], b[2];
-    if (c < whole) {
-      __builtin_memcpy(a, w + c * 64, 32);
-      __builtin_memcpy(b, x + c * 64, 32);
-    } else {
+    for (int u = 0; u < U; ++u) load(u, u);
+    int64_t n = 0;
+    for (; n + U <= mine; n += U) {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        const bool in = c * 64 + 16 * q + k < p.K;
-        a[k >> 3][k & 7] = in ? w[c * 64 + k] : (E)0.0f;
-        b[k >> 3][k & 7] = in ? x[c * 64 + k] : (E)0.0f;
+      for (int u = 0; u < U; ++u) {
+        write(u);
+        load(u, n + U + u);
+        multiply();
       }
     }
-    acc = T::mfma(a[0], b[0], acc);
-    acc = T::mfma(a[1], b[1], acc);
+#pragma unroll
+    for (int u = 0; u + 1 < U; ++u)
+      if (n + u < mine) {
+        write(u);
+        multiply();
+      }
   }
-  sums[wave][lane] = acc;
+  if (p.K % 64 != 0 && wave == (int)(whole % kDirectWaves)) {
+    la.load_end(a[0], whole * 64, p.K);
+    lb.load_end(b[0], whole * 64, p.K);
+    write(0);
+    multiply();
+  }
   __syncthreads();
-  if (wave) return;
+  f32x4* const sums = (f32x4*)lds;  // [wave][NI * NJ][64]
 #pragma unroll
-  for (int i = 1; i < kFewWaves; ++i) acc += sums[i][lane];
-  const int64_t at = n0 + 4 * q;  // token r, rows at .. at + 3 of W
-  if (r >= p.T_ || at >= p.N) return;
-  if (p.bias) acc += load4<T>((const E*)p.bias, at, p.N);
-  if (p.z) {
-    const float e[4] = {acc[0], acc[1], acc[2], acc[3]};
-    store4<T>((E*)p.z + r * p.N, at, p.N, e);
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sums[((wave * NI + i) * NJ + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int n = wave; n < NI * NJ; n += kDirectWaves) {
+    // a lane has token t and four rows of W
+    const int64_t at = f0 + 16 * (n / NJ) + 4 * (lane >> 4), t = t0 + 16 * (n % NJ) + (lane & 15);
+    f32x4 v = sums[n * 64 + lane];
+#pragma unroll
+    for (int i = 1; i < kDirectWaves; ++i) v += sums[(i * NI * NJ + n) * 64 + lane];
+    if (t >= p.T_ || at >= p.N) continue;
+    if (p.bias) v += load4<T>((const E*)p.bias, at, p.N);
+    if (p.z) {
+      const float e[4] = {v[0], v[1], v[2], v[3]};
+      store4<T>((E*)p.z + t * p.N, at, p.N, e);
+    }
+    f32x4 more = {};
+    if (p.residual) more = load4<T>((const E*)p.residual + t * p.ldr, at, p.N);
+    float e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = act_of(v[k], p.act) + more[k];
+    store4<T>((E*)p.y + t * p.ldy, at, p.N, e);
   }
-  f32x4 more = {};
-  if (p.residual) more = load4<T>((const E*)p.residual + r * p.ldr, at, p.N);
-  float e[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) e[k] = act_of(acc[k], p.act) + more[k];
-  store4<T>((E*)p.y + r * p.ldy, at, p.N, e);
 #endif
 }
 
@@ -356,9 +474,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs
       for (int j = 0; j < 8; ++j) {
         float v = (float)d[j];
         if (p.z) {
-          float a, da;
-          gate_act_grad((float)z[j], p.act, a, da);
-          v = col + j < p.N ? v * da : 0.0f;
+          v = col + j < p.N ? v * act_grad_of((float)z[j], p.act) : 0.0f;
         }
         db[j] += v;
         o[j] = (E)v;
@@ -407,33 +523,52 @@ __global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t
 
 // ---- plans -------------------------------------------------------------------
 
-// The tiles of a product and the parts of its sum, by an estimate of their time in microseconds: rounds of workgroups,
-// each its steps of 64 k and about five more to start and end; the parts of a sum are written and read once
-// more in float32, 4 TB/s, and joined in a launch.
+// The tiles of a product through LDS and the parts of its sum, by an estimate of their time in microseconds: rounds of
+// workgroups, each its steps of 64 k and about five more to start and end; the parts of a sum are written and read
+// once more in float32, 4 TB/s, and joined in a launch.
 struct Kind {
   int side, per_cu;
   double step;
 };
-constexpr Kind kKinds[] = {{256, 1, 1.42}, {128, 2, 0.8}, {64, 3, 0.45}};
+constexpr Kind kKinds[] = {{256, 1, 1.42}, {128, 2, 0.8}};
 struct Tiling {
   int kind, splits;
+  double us;
 };
 constexpr int kMostSplits = 32;
-Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int kinds) {
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K) {
   const int64_t steps = (K + kStepK - 1) / kStepK;
-  Tiling best{0, 1};
-  double least = -1.0;
-  for (int k = 0; k < kinds; ++k) {
+  Tiling best{0, 1, -1.0};
+  for (int k = 0; k < 2; ++k) {
     const int64_t side = kKinds[k].side, slots = kKinds[k].per_cu * kCUs;
     const int64_t tiles = ((rows + side - 1) / side) * ((cols + side - 1) / side);
     for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 6); ++n) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
       double us = rounds * ((double)((steps + n - 1) / n) + 5.0) * kKinds[k].step;
       if (n > 1) us += 4.0 + (double)(n + 1) * rows * cols * 4.0 / 4e6;
-      if (least < 0.0 || us < least) {
-        least = us;
-        best = Tiling{k, n};
-      }
+      if (best.us < 0.0 || us < best.us) best = Tiling{k, n, us};
+    }
+  }
+  return best;
+}
+// The tile of direct_kernel in 16 rows of W and 16 tokens, by an estimate: rounds of workgroups, two on a CU of the
+// small ones, each of which reads its rows at 100 bytes a nanosecond.
+struct Direct {
+  int ni, nj;
+};
+constexpr Direct kDirect[] = {{1, 1}, {1, 2}, {1, 4}, {2, 2}, {2, 4}, {4, 4}};
+int plan_direct(int64_t N, int64_t T, int64_t K, double* us) {
+  int best = 0;
+  *us = -1.0;
+  for (int i = 0; i < 6; ++i) {
+    const Direct d = kDirect[i];
+    if (d.nj > 1 && T <= 8 * d.nj) continue;  // more than half of the tokens would be nobody's
+    const int64_t groups = ((N + 16 * d.ni - 1) / (16 * d.ni)) * ((T + 16 * d.nj - 1) / (16 * d.nj));
+    const double rounds = (double)((groups + kCUs - 1) / kCUs);
+    const double t = rounds * ((double)(16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0) + 3.0;
+    if (*us < 0.0 || t < *us) {
+      *us = t;
+      best = i;
     }
   }
   return best;
@@ -447,19 +582,26 @@ int64_t splits_of(int64_t K, int splits, int64_t* per) {
   return (K + *per - 1) / *per;
 }
 
-constexpr int64_t kFewTokens = 16;
-
 struct ForwardPlan {
   int64_t x = -1, w = -1, part = -1, bytes = 0;
-  Tiling tiles{0, 1};
+  Tiling tiles{0, 1, 0.0};
+  int direct = -1;  // of kDirect
 };
 ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
-  if (d.T <= kFewTokens) return p;
   const int64_t Kp = round_up(d.K, 8);
+  p.tiles = plan_tiles(d.N, d.T, d.K);
+  double us = p.tiles.us, direct = 0.0;
+  // (rows that are not in place are copied in a launch of their own first)
+  if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
+    us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
+  const int i = plan_direct(d.N, d.T, d.K, &direct);
+  if (direct < us) {
+    p.direct = i;
+    return p;
+  }
   if (!in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * Kp * 2);
   if (!in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * Kp * 2);
-  p.tiles = plan_tiles(d.N, d.T, d.K, 3);
   if (p.tiles.splits > 1) p.part = take(&p.bytes, p.tiles.splits * d.T * round_up(d.N, 4) * 4);
   return p;
 }
@@ -468,7 +610,7 @@ struct BackwardPlan {
   int64_t x = -1, w = -1, dz = -1, db = -1, part_x = -1, part_w = -1, bytes = 0;
   int64_t Kp, Np;
   uint32_t parts = 1;  // of db
-  Tiling dx{0, 1}, dw{0, 1};
+  Tiling dx{0, 1, 0.0}, dw{0, 1, 0.0};
 };
 // need: the gradients asked for
 BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need) {
@@ -481,17 +623,24 @@ BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need
   if (need.dw && !in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * p.Kp * 2);
   if (need.dx && !in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * p.Kp * 2);
   if (need.dx) {
-    p.dx = plan_tiles(d.T, d.K, p.Np, 2);
+    p.dx = plan_tiles(d.T, d.K, p.Np);
     if (p.dx.splits > 1) p.part_x = take(&p.bytes, p.dx.splits * d.T * round_up(d.K, 4) * 4);
   }
   if (need.dw) {
-    p.dw = plan_tiles(d.N, d.K, d.T, 2);
+    p.dw = plan_tiles(d.N, d.K, d.T);
     if (p.dw.splits > 1) p.part_w = take(&p.bytes, p.dw.splits * d.N * round_up(d.K, 4) * 4);
   }
   const int64_t strips = (d.N + 255) / 256, most = (d.T + 7) / 8, wanted = (2048 + strips - 1) / strips;
   p.parts = (uint32_t)(most < wanted ? most : wanted);
   if (need.db) p.db = take(&p.bytes, (int64_t)p.parts * p.Np * 4);
   return p;
+}
+
+template <class T, int NI, int NJ, int U>
+void launch_direct(LinearArgs& p, hipStream_t s) {
+  p.ni = (uint32_t)((p.N + 16 * NI - 1) / (16 * NI));
+  p.nj = (uint32_t)((p.T_ + 16 * NJ - 1) / (16 * NJ));
+  direct_kernel<T, NI, NJ, U><<<p.ni * p.nj, kDirectWaves * 64, 0, s>>>(p);
 }
 
 template <class T>
@@ -511,11 +660,18 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   p.N = d.N;
   p.K = d.K;
   p.act = d.act;
-  if (d.T <= kFewTokens) {
-    few_kernel<T><<<(unsigned)((d.N + 15) / 16), kFewWaves * 64, 0, s>>>(p);
+  const ForwardPlan plan = plan_forward(d);
+  if (plan.direct >= 0) {
+    switch (plan.direct) {
+      case 0: launch_direct<T, 1, 1, 4>(p, s); break;
+      case 1: launch_direct<T, 1, 2, 4>(p, s); break;
+      case 2: launch_direct<T, 1, 4, 2>(p, s); break;
+      case 3: launch_direct<T, 2, 2, 3>(p, s); break;
+      case 4: launch_direct<T, 2, 4, 2>(p, s); break;
+      default: launch_direct<T, 4, 4, 1>(p, s);
+    }
     return hipGetLastError();
   }
-  const ForwardPlan plan = plan_forward(d);
   uint8_t* ws = (uint8_t*)c.workspace;
   AlignArgs align{};
   align.cols = d.K;
@@ -541,8 +697,6 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   const unsigned grid = (unsigned)(p.ni * p.nj * splits);
   if (plan.tiles.kind == 0)
     linear_kernel<T><<<grid, 512, 0, s>>>(p);
-  else if (plan.tiles.kind == 1)
-    linear_middle_kernel<T><<<grid, 256, 0, s>>>(p);
   else
     linear_small_kernel<T><<<grid, 256, 0, s>>>(p);
   if (p.part)

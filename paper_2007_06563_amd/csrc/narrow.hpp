@@ -44,6 +44,19 @@ __device__ __forceinline__ typename T::elem round_product(float a, float b) {
   return (typename T::elem)v;
 }
 
+// 16 bytes moved down by `bits` (128 or more: nothing is left of them), zeros from above.
+__device__ __forceinline__ u32x4v shifted_down(const u32x4v& w, uint32_t bits) {
+  uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+  lo = bits >= 64 ? hi : lo;
+  hi = bits >= 64 ? 0 : hi;
+  const uint32_t n = bits & 63;
+  lo = lo >> n | (hi << 1) << (63 - n);
+  hi >>= n;
+  lo = bits >= 128 ? 0 : lo;
+  hi = bits >= 128 ? 0 : hi;
+  return u32x4v{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // The scale exponent k of a group whose largest finite magnitude has the
 // float32 bits a: the smallest k >= kMinScale for which the largest magnitude
 // times 2^-k does not round beyond the format's largest value. In (4, 3) that
