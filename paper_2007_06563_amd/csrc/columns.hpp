@@ -8,35 +8,41 @@
 
 namespace hobflops {
 
-// part: [parts][stride]; out[0][c] the sum of column c, out[1][c] that of column second + c, c < cols
-// (either may be null). A workgroup has 64 columns; its waves take every sixteenth part each, and
-// their sums meet in LDS.
+// The sums of up to 64 columns (as many as there are, `cols` or more) of part [parts][stride] by a workgroup of NW
+// waves: each takes every NW-th part, their sums meet in LDS.
+template <class T, int NW>
+__device__ __forceinline__ void column_sum(const float* part, int64_t parts, int64_t stride, int64_t cols,
+                                           typename T::elem* out) {
+  __shared__ float sums[NW][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* p = part + (lane < cols ? lane : 0);
+  float v = 0.0f;
+  int64_t i = wave;
+  for (; i + 7 * NW < parts; i += 8 * NW) {
+    float e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = p[(i + NW * j) * stride];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v += e[j];
+  }
+  for (; i < parts; i += NW) v += p[i * stride];
+  sums[wave][lane] = v;
+  __syncthreads();
+  if (wave || lane >= cols) return;
+#pragma unroll
+  for (int j = 1; j < NW; ++j) v += sums[j][lane];
+  out[lane] = (typename T::elem)v;
+}
+
+// part: [parts][stride]; out0[c] the sum of column c, out1[c] that of column second + c, c < cols
+// (either may be null).
 template <class T>
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float* part, int64_t parts, int64_t stride,
                                                            int64_t cols, int64_t second,
                                                            typename T::elem* out0, typename T::elem* out1) {
-  __shared__ float sums[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t c = (int64_t)blockIdx.x * 64;
   typename T::elem* out = blockIdx.y ? out1 : out0;
-  if (!out) return;
-  const float* p = part + (blockIdx.y ? second : 0) + (c < cols ? c : 0);
-  float v = 0.0f;
-  int64_t i = wave;
-  for (; i + 7 * 16 < parts; i += 8 * 16) {
-    float e[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = p[(i + 16 * j) * stride];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v += e[j];
-  }
-  for (; i < parts; i += 16) v += p[i * stride];
-  sums[wave][lane] = v;
-  __syncthreads();
-  if (wave || c >= cols) return;
-#pragma unroll
-  for (int j = 1; j < 16; ++j) v += sums[j][lane];
-  out[c] = (typename T::elem)v;
+  if (out) column_sum<T, 16>(part + (blockIdx.y ? second : 0) + c, parts, stride, cols - c, out + c);
 }
 
 template <class T>

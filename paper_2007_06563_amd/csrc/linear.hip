@@ -515,6 +515,40 @@ __global__ __launch_bounds__(256, 2) void linear_grad_small_kernel(GradArgs dx, 
   linear_grad_tiles<T, 128, 2>(dx, dw, parts, sa, sb);
 }
 
+// What is left after the products, in one launch: the parts of dx and of dW joined in their order, 4 values a thread, and
+// the parts of db, a column a thread's. (A launch each took a short step 3 us more.)
+struct JoinArgs {
+  const float* part;
+  void* out;
+  int64_t rows, cols;
+  int splits;
+  uint32_t groups;
+};
+template <class T>
+__device__ __forceinline__ void join_of(const JoinArgs& p, int64_t i, int64_t stride) {
+  const int64_t ldp = (p.cols + 3) & ~(int64_t)3, n = p.rows * ldp;
+  for (i *= 4; i < n; i += stride * 4) {
+    f32x4 v = *(const f32x4*)(p.part + i);
+    for (int s = 1; s < p.splits; ++s) v += *(const f32x4*)(p.part + s * n + i);
+    const int64_t row = i / ldp, col = i - row * ldp;
+    const float e[4] = {v[0], v[1], v[2], v[3]};
+    store4<T>((typename T::elem*)p.out + row * p.cols, col, p.cols, e);
+  }
+}
+template <class T>
+__global__ __launch_bounds__(256) void linear_finish_kernel(JoinArgs dx, JoinArgs dw, const float* db_part, int64_t parts,
+                                                            int64_t stride, int64_t cols, typename T::elem* db) {
+  const uint32_t b = blockIdx.x;
+  if (b < dx.groups) {
+    join_of<T>(dx, (int64_t)b * 256 + threadIdx.x, (int64_t)dx.groups * 256);
+  } else if (b < dx.groups + dw.groups) {
+    join_of<T>(dw, (int64_t)(b - dx.groups) * 256 + threadIdx.x, (int64_t)dw.groups * 256);
+  } else {
+    const int64_t c = (int64_t)(b - dx.groups - dw.groups) * 64;
+    column_sum<T, 4>(db_part + c, parts, stride, cols - c, db + c);
+  }
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
@@ -551,8 +585,11 @@ Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K) {
   }
   return best;
 }
-// The tile of direct_kernel in 16 rows of W and 16 tokens, by an estimate: rounds of workgroups, two on a CU of the
-// small ones, each of which reads its rows at 100 bytes a nanosecond.
+// The tile of direct_kernel in 16 rows of W and 16 tokens, by an estimate: rounds of workgroups, one on each CU, which
+// read their rows at 100 bytes a nanosecond, and start and end, the longer the larger the tile. Measured, us, in the order
+// of kDirect, and in tiles through LDS: 16 x 4096 -> 4096 8.5, 9.3, 10.7, 9.6, 12.0, 18.1, LDS 15.3; 64 x 4096 -> 4096
+// 19.0, 15.5, 12.1, 10.7, 13.5, 18.4, LDS 17.3; 333 x 2730 -> 1000 24.5, 20.6, 19.2, 16.8, 13.0, 18.6, LDS 24.2;
+// 1024 x 1024 -> 1024 33, 29, 19, 16, 13, 9.4, LDS 14.0; 2048 x 512 -> 1408 77, 66, 25, 38, 22, 18, LDS 10.0.
 struct Direct {
   int ni, nj;
 };
@@ -565,7 +602,7 @@ int plan_direct(int64_t N, int64_t T, int64_t K, double* us) {
     if (d.nj > 1 && T <= 8 * d.nj) continue;  // more than half of the tokens would be nobody's
     const int64_t groups = ((N + 16 * d.ni - 1) / (16 * d.ni)) * ((T + 16 * d.nj - 1) / (16 * d.nj));
     const double rounds = (double)((groups + kCUs - 1) / kCUs);
-    const double t = rounds * ((double)(16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0) + 3.0;
+    const double t = rounds * ((double)(16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0 + 0.18 * d.ni * d.nj) + 3.0;
     if (*us < 0.0 || t < *us) {
       *us = t;
       best = i;
@@ -591,7 +628,7 @@ ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
   const int64_t Kp = round_up(d.K, 8);
   p.tiles = plan_tiles(d.N, d.T, d.K);
-  double us = p.tiles.us, direct = 0.0;
+  double us = p.tiles.us + (p.tiles.splits > 1 ? 4.0 : 0.0), direct = 0.0;  // (the second launch's start)
   // (rows that are not in place are copied in a launch of their own first)
   if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
     us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
@@ -779,11 +816,12 @@ hipError_t backward(const hobflops_linear_desc& d, const LinearBackward& c, hipS
     grad_products<T>(p, 0, w, tiles, plan.dw.kind, s);
     grad_products<T>(p, parts, w, 0, plan.dx.kind, s);
   }
-  if (c.dx && p.part)
-    join_kernel<T><<<grid_of(d.T * round_up(d.K, 4) / 4, 4096), 256, 0, s>>>(p.part, (int)sx, d.T, d.K, (E*)c.dx);
-  if (c.dw && w.part)
-    join_kernel<T><<<grid_of(d.N * round_up(d.K, 4) / 4, 4096), 256, 0, s>>>(w.part, (int)sw, d.N, d.K, (E*)c.dw);
-  if (c.db) launch_column_sums<T>(z.part, plan.parts, plan.Np, c.db, nullptr, d.N, 0, s);
+  JoinArgs jx{}, jw{};
+  if (c.dx && p.part) jx = JoinArgs{p.part, c.dx, d.T, d.K, (int)sx, grid_of(d.T * round_up(d.K, 4) / 4, 4096)};
+  if (c.dw && w.part) jw = JoinArgs{w.part, c.dw, d.N, d.K, (int)sw, grid_of(d.N * round_up(d.K, 4) / 4, 4096)};
+  const unsigned last = jx.groups + jw.groups + (c.db ? (unsigned)((d.N + 63) / 64) : 0);
+  if (last)
+    linear_finish_kernel<T><<<last, 256, 0, s>>>(jx, jw, z.part, plan.parts, plan.Np, d.N, (E*)c.db);
   return hipGetLastError();
 }
 
