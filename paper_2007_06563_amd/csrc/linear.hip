@@ -38,19 +38,28 @@ __device__ __forceinline__ float tail_ratio(float a) {
   return __builtin_fmaf(r, t, -2.71316530e-5f);
 }
 struct Gate {
-  float p, e;  // the gate, and (gelu) exp(-z^2 / 2)
+  float p, e;  // the gate, and exp(-z^2 / 2)
 };
+// (The exponential instruction gives 0 below 2^-126: that is beyond |z| = 13.2, where z Phi(z) is below 2^-126 as well.)
 __device__ __forceinline__ Gate gelu_gate(float z) {
-  const float a = __builtin_fabsf(z), e = exp2f(z * z * -0.721347520f), q = e * tail_ratio(a);
+  const float e = __builtin_amdgcn_exp2f(z * z * -0.721347520f), q = e * tail_ratio(__builtin_fabsf(z));
   return Gate{z < 0.0f ? q : 1.0f - q, e};
+}
+// exp(-|z|) 2^64, which the exponential instruction has down to |z| = 131, where z exp(z) is below bfloat16's range;
+// within 2^-17.
+__device__ __forceinline__ float far_exp(float z) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fabsf(z), -1.44269504f, 64.0f));
 }
 // sigmoid(z) and sigmoid(-z)
 __device__ __forceinline__ Sigmoid silu_gate(float z) {
-  const float e = exp2f(__builtin_fabsf(z) * -1.44269504f), r = __builtin_amdgcn_rcpf(1.0f + e), far = e * r;
+  const float e = far_exp(z) * 0x1p-64f, r = __builtin_amdgcn_rcpf(1.0f + e), far = e * r;
   return z < 0.0f ? Sigmoid{far, r} : Sigmoid{r, far};
 }
 __device__ __forceinline__ float act_of(float z, int act) {
-  if (act == HOBFLOPS_GATE_SILU) return z * silu_gate(z).s;
+  if (act == HOBFLOPS_GATE_SILU) {
+    const float e = far_exp(z), v = z * __builtin_amdgcn_rcpf(__builtin_fmaf(e, 0x1p-64f, 1.0f));
+    return z < 0.0f ? v * e * 0x1p-64f : v;
+  }
   if (act == HOBFLOPS_GATE_GELU) return z * gelu_gate(z).p;
   return act == kNoAct || z > 0.0f || z != z ? z : 0.0f;
 }
