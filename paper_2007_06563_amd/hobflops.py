@@ -5,6 +5,7 @@ torch's current stream; torch supplies device memory and streams. There is no
 CPU fallback: a missing library or a host tensor raises.
 Plane tensors are int32 (the bit patterns of PL32 words).
 """
+import array
 import collections
 import ctypes
 import operator
@@ -564,11 +565,17 @@ def _align(*ptrs):
 
 def _no_gradient(name, *tensors):
     """Says that autograd records nothing of a call whose inputs it follows."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        warnings.warn(f"{name}: its result carries no gradient to its inputs; wrap it in a "
-                      "torch.autograd.Function (gated_backward, layer_norm_backward and "
-                      "linear_backward have the gradients), or call it under torch.no_grad()",
-                      stacklevel=3)
+    if not torch.is_grad_enabled():
+        return
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            break
+    else:
+        return
+    warnings.warn(f"{name}: its result carries no gradient to its inputs; wrap it in a "
+                  "torch.autograd.Function (gated_backward, layer_norm_backward and "
+                  "linear_backward have the gradients), or call it under torch.no_grad()",
+                  stacklevel=3)
 
 
 def _workspace(d, backward, device):
@@ -823,6 +830,7 @@ def adamw_state(params, fmt=None):
 _numel, _contiguous, _data_ptr, _get_device = (torch.Tensor.numel, torch.Tensor.is_contiguous,
                                                torch.Tensor.data_ptr, torch.Tensor.get_device)
 _dtype, _shape = operator.attrgetter("dtype"), operator.attrgetter("shape")
+_NO_FMT = Fmt(0, 0)
 
 
 def _tensors(ts, dtypes, device, name):
@@ -830,11 +838,28 @@ def _tensors(ts, dtypes, device, name):
     if set(map(_get_device, ts)) != {device.index}:
         raise TypeError(f"adamw {name}: tensors on {device} are needed")
     types = set(map(_dtype, ts))
-    if len(types) != 1 or not types <= set(dtypes):
+    dtype = types.pop()
+    if types or dtype not in dtypes:
         raise TypeError(f"adamw {name}: one type of {', '.join(map(str, dtypes))} is needed")
-    if not all(map(_contiguous, ts)):
+    if False in map(_contiguous, ts):
         raise ValueError(f"adamw {name}: contiguous tensors are needed")
-    return list(map(_data_ptr, ts)), types.pop()
+    return list(map(_data_ptr, ts)), dtype
+
+
+def _some_tensors(ts, shapes, dtypes, device, name):
+    """Pointers of tensors of these shapes, 0 for None, and the type (of none: None)."""
+    if any(t is None for t in ts):
+        here = [i for i, t in enumerate(ts) if t is not None]
+        if not here:
+            return [0] * len(ts), None
+        ptrs, dtype = _some_tensors([ts[i] for i in here], [shapes[i] for i in here], dtypes, device, name)
+        out = [0] * len(ts)
+        for i, p in zip(here, ptrs):
+            out[i] = p
+        return out, dtype
+    if list(map(_shape, ts)) != shapes:
+        raise ValueError(f"adamw {name}: another shape than its tensor's")
+    return _tensors(ts, dtypes, device, name)
 
 
 def _scalar(value, dtype, device, name):
@@ -861,31 +886,18 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
     dev = params[0].device
     if dev.type != "cuda":
         raise TypeError("hobflops operates on GPU tensors only")
-    pp, _ = _tensors(params, (torch.float32,), dev, "params")
-    sizes = list(map(_numel, params))
-    if list(map(_shape, params)) == [getattr(g, "shape", None) for g in grads]:
-        pg, gtype = _tensors(grads, tuple(_TYPES), dev, "grads")
-    else:
-        here = [i for i, g in enumerate(grads) if g is not None]
-        if any(grads[i].shape != params[i].shape for i in here):
-            raise ValueError("adamw: a gradient has another shape than its tensor")
-        if not here:
-            return
-        ptrs, gtype = _tensors([grads[i] for i in here], tuple(_TYPES), dev, "grads")
-        pg = [0] * len(params)
-        for i, p in zip(here, ptrs):
-            pg[i] = p
-    pc, ctype = [0] * len(params), torch.bfloat16
+    n, shapes = len(params), list(map(_shape, params))
+    words = [0] * (4 * n)   # of n AdamwTensor
+    words[0::4], _ = _tensors(params, (torch.float32,), dev, "params")
+    words[1::4], gtype = _some_tensors(grads, shapes, tuple(_TYPES), dev, "grads")
+    if gtype is None:
+        return
+    ctype = None
     if copies is not None:
-        here = [i for i, c in enumerate(copies) if c is not None]
-        if any(copies[i].shape != params[i].shape for i in here):
-            raise ValueError("adamw: a copy has another shape than its tensor")
-        if here:
-            ptrs, ctype = _tensors([copies[i] for i in here], (torch.bfloat16, torch.float16), dev, "copies")
-            for i, p in zip(here, ptrs):
-                pc[i] = p
-    f = Fmt(0, 0) if state.fmt is None else fmt(state.fmt)
-    total = sum(-(-n // 32) for n in sizes) * 32
+        words[2::4], ctype = _some_tensors(copies, shapes, (torch.bfloat16, torch.float16), dev, "copies")
+    words[3::4] = sizes = list(map(_numel, params))
+    f = _NO_FMT if state.fmt is None else fmt(state.fmt)
+    total = sum([(n + 31) & -32 for n in sizes])
     if state.fmt is None:
         (pm, ps), (pv, pt) = ((_dense(t, (total,), torch.float32, dev, "adamw state"), None)
                               for t in (state.m, state.v))
@@ -901,13 +913,11 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
         if not isinstance(skip, torch.Tensor):
             raise TypeError("adamw skip: a float32 GPU tensor of one value is needed")
         skip_at = _scalar(skip, torch.float32, dev, "skip")[1]
-    d = AdamwDesc(_TYPES[gtype], _TYPES[ctype], f, lr, betas[0], betas[1], eps, weight_decay, grad_scale,
-                  step, seed, lr_at, step_at, scale_at, skip_at)
-    n = len(params)
-    words = [0] * (4 * n)
-    words[0::4], words[1::4], words[2::4], words[3::4] = pp, pg, pc, sizes
-    table = (ctypes.c_int64 * (4 * n))(*words)
-    _call(dev, lib().hobflops_adamw, ctypes.byref(d), table, n, pm, ps, pv, pt, total)
+    d = AdamwDesc(_TYPES[gtype], _TYPES[ctype or torch.bfloat16], f, lr, betas[0], betas[1], eps, weight_decay,
+                  grad_scale, step, seed, lr_at, step_at, scale_at, skip_at)
+    table = array.array("q", words)
+    _call(dev, lib().hobflops_adamw, ctypes.byref(d), table.buffer_info()[0], n, pm, ps, pv, pt, total)
     # what autograd has kept of these tensors is not theirs any more
-    torch.autograd.graph.increment_version(params if copies is None else
-                                           [*params, *(c for c in copies if c is not None)])
+    torch.autograd.graph.increment_version(params)
+    if ctype is not None:
+        torch.autograd.graph.increment_version([c for c in copies if c is not None])
