@@ -10,6 +10,7 @@ import collections
 import ctypes
 import operator
 import os
+import struct
 import warnings
 
 import torch
@@ -93,6 +94,11 @@ class AdamwDesc(ctypes.Structure):
                 ("grad_scale_at", ctypes.c_void_p), ("skip_at", ctypes.c_void_p)]
 
 
+# The bytes of a NormDesc and of a LinearDesc, made in a quarter of a ctypes.Structure's time.
+_norm_desc = struct.Struct("qqqqqiid").pack
+_linear_desc = struct.Struct("qqqqqqqiiixxxx").pack
+
+
 # What gated_forward keeps for gated_backward: (codes, scales) of x, g and u.
 GatedSaved = collections.namedtuple("GatedSaved", "x gate up fmt")
 # What layer_norm keeps for layer_norm_backward: float32 [rows] each.
@@ -149,14 +155,13 @@ def lib():
         L.hobflops_w4_linear.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, ci, vp, i64, vp]
         L.hobflops_w4_gated.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, vp, vp, ci, ci, ci, vp,
                                         i64, vp]
-        nd, ld = ctypes.POINTER(NormDesc), ctypes.POINTER(LinearDesc)
-        L.hobflops_layer_norm.argtypes = [nd] + [vp] * 7
-        L.hobflops_layer_norm_workspace.argtypes = [nd, ctypes.POINTER(i64)]
-        L.hobflops_layer_norm_backward.argtypes = [nd] + [vp] * 10 + [i64, vp]
-        L.hobflops_linear.argtypes = [ld] + [vp] * 7 + [i64, vp]
-        L.hobflops_linear_workspace.argtypes = [ld, ci, ctypes.POINTER(i64)]
-        L.hobflops_linear_backward.argtypes = [ld] + [vp] * 8 + [i64, vp]
-        # (arrays of AdamwTensor: any ctypes array of its words)
+        # (descriptors and arrays of AdamwTensor: a ctypes.Structure's address or their bytes)
+        L.hobflops_layer_norm.argtypes = [vp] * 8
+        L.hobflops_layer_norm_workspace.argtypes = [vp, ctypes.POINTER(i64)]
+        L.hobflops_layer_norm_backward.argtypes = [vp] * 11 + [i64, vp]
+        L.hobflops_linear.argtypes = [vp] * 8 + [i64, vp]
+        L.hobflops_linear_workspace.argtypes = [vp, ci, ctypes.POINTER(i64)]
+        L.hobflops_linear_backward.argtypes = [vp] * 9 + [i64, vp]
         L.hobflops_adamw.argtypes = [ctypes.POINTER(AdamwDesc), vp, ci, vp, vp, vp, vp, i64, vp]
         L.hobflops_adamw_state_len.argtypes = [vp, ci, ctypes.POINTER(i64)]
         L.hobflops_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ci]
@@ -682,7 +687,7 @@ def _vector(t, n, dtypes, device, name):
         raise TypeError(f"{name}: a tensor on {device} is needed")
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: {' or '.join(str(d) for d in dtypes)} is needed, not {t.dtype}")
-    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: a dense vector of {n} values is needed")
     return t.data_ptr()
 
@@ -720,14 +725,18 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise TypeError("layer_norm: weight and bias must have one type")
     _no_gradient("layer_norm", x, weight, bias)
-    y, py, ldy = _out_rows(out, (rows, cols), x.dtype, dev, "layer_norm out")
-    d = NormDesc(rows, cols, ldx, ldy, cols, kind, _TYPES[one.dtype] if one is not None else kind, eps)
+    if out is None:
+        y = x.new_empty((rows, cols))
+        py, ldy = y.data_ptr(), cols
+    else:
+        y, py, ldy = _out_rows(out, (rows, cols), x.dtype, dev, "layer_norm out")
+    d = _norm_desc(rows, cols, ldx, ldy, cols, kind, kind if one is None else _TYPES[one.dtype], eps)
     saved, pm, pr = None, None, None
     if save:
         saved = NormSaved(torch.empty(rows, dtype=torch.float32, device=dev),
                           torch.empty(rows, dtype=torch.float32, device=dev))
         pm, pr = saved.mean.data_ptr(), saved.rstd.data_ptr()
-    _call(dev, lib().hobflops_layer_norm, ctypes.byref(d), px, pw, pb, py, pm, pr)
+    _call(dev, lib().hobflops_layer_norm, d, px, pw, pb, py, pm, pr)
     return (y, saved) if save else y
 
 
@@ -742,13 +751,13 @@ def layer_norm_backward(dy, x, saved, weight=None, add=None, dw=True, db=True):
     pw = _vector(weight, cols, (x.dtype, torch.float32), dev, "layer_norm_backward weight")
     pm, pr = (_vector(t, rows, (torch.float32,), dev, "layer_norm_backward saved") for t in saved)
     wdtype = x.dtype if weight is None else weight.dtype
-    d = NormDesc(rows, cols, ldx, ldg, lda, kind, _TYPES[wdtype], 0.0)
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    d = _norm_desc(rows, cols, ldx, ldg, lda, kind, _TYPES[wdtype], 0.0)
+    dx = x.new_empty((rows, cols))
     gw, gb = (torch.empty(cols, dtype=wdtype, device=dev) if need else None for need in (dw, db))
     ws, pws, n = (None, None, 0)
     if dw or db:
-        ws, pws, n = _bytes_of(lib().hobflops_layer_norm_workspace, dev, ctypes.byref(d))
-    _call(dev, lib().hobflops_layer_norm_backward, ctypes.byref(d), pg, px, pw, pm, pr, pa, dx.data_ptr(),
+        ws, pws, n = _bytes_of(lib().hobflops_layer_norm_workspace, dev, d)
+    _call(dev, lib().hobflops_layer_norm_backward, d, pg, px, pw, pm, pr, pa, dx.data_ptr(),
           gw.data_ptr() if dw else None, gb.data_ptr() if db else None, pws, n)
     return dx, gw, gb
 
@@ -768,12 +777,16 @@ def linear(x, w, bias=None, act=None, residual=None, save=False, out=None):
     pb = _vector(bias, N, (x.dtype,), dev, "linear bias")
     pr, ldr = (None, N) if residual is None else _like(residual, (T, N), x, "linear residual")
     _no_gradient("linear", x, w, bias, residual)
-    y, py, ldy = _out_rows(out, (T, N), x.dtype, dev, "linear out")
+    if out is None:
+        y = x.new_empty((T, N))
+        py, ldy = y.data_ptr(), N
+    else:
+        y, py, ldy = _out_rows(out, (T, N), x.dtype, dev, "linear out")
     a = GATE_NONE if act is None else act
-    d = LinearDesc(T, K, N, ldx, ldw, ldy, ldr, kind, a, _align(px, pw))
-    z = torch.empty((T, N), dtype=x.dtype, device=dev) if save and a != GATE_NONE else None
-    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, ctypes.byref(d), 0)
-    _call(dev, lib().hobflops_linear, ctypes.byref(d), px, pw, pb, pr, py,
+    d = _linear_desc(T, K, N, ldx, ldw, ldy, ldr, kind, a, _align(px, pw))
+    z = x.new_empty((T, N)) if save and a != GATE_NONE else None
+    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, d, 0)
+    _call(dev, lib().hobflops_linear, d, px, pw, pb, pr, py,
           None if z is None else z.data_ptr(), pws, n)
     return (y, z) if save else y
 
@@ -795,15 +808,15 @@ def linear_backward(dy, x, w, z=None, act=None, dx=True, dw=True, db=True):
         if z is None:
             raise ValueError("linear_backward: an activation's gradient needs z")
         pz = _dense(z, (T, N), dtype, dev, "linear_backward z")
-    d = LinearDesc(T, K, N, ldx, ldw, ldg, N, kind, a, _align(pg, px, pw))
+    d = _linear_desc(T, K, N, ldx, ldw, ldg, N, kind, a, _align(pg, px, pw))
     need = (NEED_DX if dx else 0) | (NEED_DW if dw else 0) | (NEED_DBIAS if db else 0)
     if not need:
         return None, None, None
-    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, ctypes.byref(d), need)
-    gx, gw, gb = (torch.empty(shape, dtype=dtype, device=dev) if asked else None
+    ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, d, need)
+    gx, gw, gb = (dy.new_empty(shape) if asked else None
                   for shape, asked in (((T, K), dx), ((N, K), dw), (N, db)))
     ptrs = [None if t is None else t.data_ptr() for t in (gx, gw, gb)]
-    _call(dev, lib().hobflops_linear_backward, ctypes.byref(d), pg, px, pw, pz, *ptrs, pws, n)
+    _call(dev, lib().hobflops_linear_backward, d, pg, px, pw, pz, *ptrs, pws, n)
     return gx, gw, gb
 
 
@@ -848,16 +861,20 @@ def _tensors(ts, dtypes, device, name):
 
 def _some_tensors(ts, shapes, dtypes, device, name):
     """Pointers of tensors of these shapes, 0 for None, and the type (of none: None)."""
-    if any(t is None for t in ts):
+    try:
+        same = list(map(_shape, ts)) == shapes
+    except AttributeError:   # None is among them
         here = [i for i, t in enumerate(ts) if t is not None]
-        if not here:
+        if not here or len(here) == len(ts):
+            if here:
+                raise
             return [0] * len(ts), None
         ptrs, dtype = _some_tensors([ts[i] for i in here], [shapes[i] for i in here], dtypes, device, name)
         out = [0] * len(ts)
         for i, p in zip(here, ptrs):
             out[i] = p
         return out, dtype
-    if list(map(_shape, ts)) != shapes:
+    if not same:
         raise ValueError(f"adamw {name}: another shape than its tensor's")
     return _tensors(ts, dtypes, device, name)
 

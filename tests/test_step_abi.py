@@ -95,7 +95,7 @@ def test_linear_pointers(hf):
         assert L.hobflops_linear(d, *args, BIG, None) == -3, i
     assert L.hobflops_linear(_linear_desc(hf, ldr=95), *[FAKE] * 7, BIG, None) == -1
     assert L.hobflops_linear(_linear_desc(hf, T=0), *[None] * 7, 0, None) == 0
-    loose = _linear_desc(hf, align=2)
+    loose = _linear_desc(hf, T=4096, K=4096, N=4096, ldx=4096, ldw=4096, ldy=4096, ldr=4096, align=2)
     assert L.hobflops_linear_workspace(loose, 0, ctypes.byref(n)) == 0 and n.value > 0
     assert L.hobflops_linear(loose, *[FAKE] * 7, n.value - 1, None) == -1
     assert L.hobflops_linear(loose, *[FAKE] * 6, None, BIG, None) == -1
