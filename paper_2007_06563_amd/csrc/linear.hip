@@ -112,12 +112,37 @@ __device__ __forceinline__ void wave_sync() {
 // tokens at a time, so that a lane has 8 neighbouring values of y and a token's lanes whole lines of y, z and the
 // residual. The activation is applied in a loop of its own, whose code is there once for 16 tokens (unrolled
 // over the whole tile it would not fit the instruction cache); the next 16 tokens' residual is under way meanwhile.
+template <int NI>
+constexpr int kPassesOf = NI / 2;  // of 16 tokens: 64 lanes with 8 values each
+// The residual of 16 tokens from t0 on.
+template <class T, int NI>
+__device__ __forceinline__ void load_residual(const LinearArgs& p, int64_t f0, int64_t t0, int lane,
+                                              typename T::vec8 (&r)[kPassesOf<NI>]) {
+  typedef typename T::elem E;
+  if (!p.residual || p.part) return;
+  const int64_t f = f0 + 8 * (lane % (2 * NI));
+#pragma unroll
+  for (int n = 0; n < kPassesOf<NI>; ++n) {
+    const int64_t t = t0 + n * (32 / NI) + lane / (2 * NI);
+    const E* row = (const E*)p.residual + t * p.ldr;
+    if (t >= p.T_) continue;
+    if (f + 8 <= p.N) {
+      __builtin_memcpy(&r[n], row + f, 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 7; ++k)
+        if (f + k < p.N) r[n][k] = row[f + k];
+    }
+  }
+}
+
+// more0: the residual of the first 16 tokens, loaded before the sums.
 template <class T, int NI, int NJ>
 __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&acc)[NI][NJ], int64_t f0, int64_t t0,
-                                           uint8_t* lds, int lane) {
+                                           uint8_t* lds, int lane, const typename T::vec8 (&more0)[kPassesOf<NI>]) {
   typedef typename T::elem E;
   typedef typename T::vec8 Vec;
-  constexpr int kRow = NI * 64 + 16, kLanes = NI * 2, kAtOnce = 64 / kLanes, kPasses = 16 / kAtOnce;
+  constexpr int kRow = NI * 64 + 16, kLanes = NI * 2, kAtOnce = 64 / kLanes, kPasses = kPassesOf<NI>;
   const int64_t f = f0 + 8 * (lane % kLanes);
   const int first = lane / kLanes;
   const bool whole = f + 8 <= p.N;
@@ -149,21 +174,14 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
     for (int k = 0; k < 8; ++k) bias[k] = (float)b[k];
   }
   Vec more[2][kPasses] = {};
-  const auto residual = [&](int j, Vec(&r)[kPasses]) {
-    if (!p.residual) return;
 #pragma unroll
-    for (int n = 0; n < kPasses; ++n) {
-      const int64_t t = t0 + 16 * j + n * kAtOnce + first;
-      if (t < p.T_) r[n] = load8((const E*)p.residual + t * p.ldr);
-    }
-  };
-  residual(0, more[0]);
+  for (int n = 0; n < kPasses; ++n) more[0][n] = more0[n];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
 #pragma unroll
     for (int i = 0; i < NI; ++i)
       *(f32x4*)(lds + (lane & 15) * kRow + 64 * i + 16 * (lane >> 4)) = acc[i][j];
-    if (j + 1 < NJ) residual(j + 1, more[(j + 1) & 1]);
+    if (j + 1 < NJ) load_residual<T, NI>(p, f0, t0 + 16 * (j + 1), lane, more[(j + 1) & 1]);
     wave_sync();
     if (p.act != kNoAct) {
 #pragma unroll 1
@@ -223,6 +241,9 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const 
   ReadRows<T, NJ, 0> rb;
   ra.start(wi * NI * 16, lane);
   rb.start(wj * NJ * 16, lane);
+  const int64_t f0 = i0 + wi * NI * 16, t0 = j0 + wj * NJ * 16;
+  typename T::vec8 more[kPassesOf<NI>] = {};
+  load_residual<T, NI>(p, f0, t0, lane, more);
   f32x4 acc[NI][NJ] = {};
   const auto load = [&](int s) {
     la.load(sa[s], wave);
@@ -230,7 +251,6 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const 
   };
   sum_tiles<T, NI, NJ, (BI + BJ) / 8 / NW, S>(acc, sa, sb, ra, rb, load,
                                               (int)((k1 - k0 + kStepK - 1) / kStepK));
-  const int64_t f0 = i0 + wi * NI * 16, t0 = j0 + wj * NJ * 16;
   if (p.part) {
     const int64_t ldp = (p.N + 3) & ~(int64_t)3;
 #pragma unroll
@@ -246,7 +266,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const 
   // (two waves, or one, an array)
   constexpr int kEach = NW / 4;
   uint8_t* const stage = wave / kEach == 0 ? sa[0] : wave / kEach == 1 ? sa[1] : wave / kEach == 2 ? sb[0] : sb[1];
-  store_tile<T, NI, NJ>(p, acc, f0, t0, stage + (wave % kEach) * kTileBytes<NI>, lane);
+  store_tile<T, NI, NJ>(p, acc, f0, t0, stage + (wave % kEach) * kTileBytes<NI>, lane, more);
 #endif
 }
 
@@ -585,10 +605,10 @@ Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K) {
   for (int k = 0; k < 2; ++k) {
     const int64_t side = kKinds[k].side, slots = kKinds[k].per_cu * kCUs;
     const int64_t tiles = ((rows + side - 1) / side) * ((cols + side - 1) / side);
-    for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 6); ++n) {
+    for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); ++n) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
       double us = rounds * ((double)((steps + n - 1) / n) + 5.0) * kKinds[k].step;
-      if (n > 1) us += 4.0 + (double)(n + 1) * rows * cols * 4.0 / 4e6;
+      if (n > 1) us += 4.0 + (double)(2 * n) * rows * cols * 4.0 / 4e6;
       if (best.us < 0.0 || us < best.us) best = Tiling{k, n, us};
     }
   }
