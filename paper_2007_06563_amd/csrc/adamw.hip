@@ -67,9 +67,6 @@ __device__ __forceinline__ uint32_t bits_of(uint32_t key, int64_t place) {
   return stirred((uint32_t)place * 0x9E3779B9u + (key ^ (uint32_t)(place >> 32) * 0x6A09E667u));
 }
 
-// 16 bytes at any address, past the caches' reuse: every value is read and written once a step.
-typedef u32x4v Words __attribute__((aligned(2)));
-
 template <class G>
 __device__ __forceinline__ void load_values(const typename G::elem* src, int64_t left, float (&v)[8]) {
   if (left >= kPer) {
@@ -77,7 +74,7 @@ __device__ __forceinline__ void load_values(const typename G::elem* src, int64_t
     constexpr int n = sizeof e / 16;
     u32x4v w[n];
 #pragma unroll
-    for (int i = 0; i < n; ++i) w[i] = __builtin_nontemporal_load((const Words*)src + i);
+    for (int i = 0; i < n; ++i) w[i] = __builtin_nontemporal_load((const Words16*)src + i);
     __builtin_memcpy(e, w, sizeof e);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)e[j];
@@ -96,7 +93,7 @@ __device__ __forceinline__ void store_values(typename G::elem* dst, int64_t left
     u32x4v w[n];
     __builtin_memcpy(w, e, sizeof e);
 #pragma unroll
-    for (int i = 0; i < n; ++i) __builtin_nontemporal_store(w[i], (Words*)dst + i);
+    for (int i = 0; i < n; ++i) stream16((u32x4v*)dst + i, w[i]);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)

@@ -193,7 +193,10 @@ __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
       typename T::elem e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = round(v[j]);
-      __builtin_memcpy(dst, e, sizeof e);
+      u32x4v w[sizeof e / 16];
+      __builtin_memcpy(w, e, sizeof e);
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof e / 16); ++i) stream16((u32x4v*)dst + i, w[i]);
     } else {
       for (int j = 0; j < 8 && col + j < p.cols; ++j) dst[j] = round(v[j]);
     }

@@ -160,7 +160,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
   };
   const auto store8 = [&](E* row, const Vec& v) {
     if (whole) {
-      __builtin_memcpy(row + f, &v, 16);
+      stream16(row + f, __builtin_bit_cast(u32x4v, v));
     } else {
 #pragma unroll
       for (int k = 0; k < 7; ++k)

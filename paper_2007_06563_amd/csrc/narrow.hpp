@@ -44,6 +44,10 @@ __device__ __forceinline__ typename T::elem round_product(float a, float b) {
   return (typename T::elem)v;
 }
 
+// 16 bytes to any address of a 16-bit type, past the caches' reuse: for results of many megabytes.
+typedef u32x4v Words16 __attribute__((aligned(2)));
+__device__ __forceinline__ void stream16(void* p, const u32x4v& w) { __builtin_nontemporal_store(w, (Words16*)p); }
+
 // 16 bytes moved down by `bits` (128 or more: nothing is left of them), zeros from above.
 __device__ __forceinline__ u32x4v shifted_down(const u32x4v& w, uint32_t bits) {
   uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];

@@ -88,7 +88,9 @@ struct Chunk {
     typename T::elem e[kVec<T>];
 #pragma unroll
     for (int j = 0; j < kVec<T>; ++j) e[j] = (typename T::elem)v[j];
-    if (there) __builtin_memcpy((typename T::elem*)row + at, e, 16);
+    u32x4v w;
+    __builtin_memcpy(&w, e, 16);
+    if (there) stream16((typename T::elem*)row + at, w);
   }
 };
 // Values of a chunk as they count for sums.
