@@ -402,7 +402,7 @@ int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, 
 
 /* ---- Around the gated block in a training step: layer norm, a linear layer, AdamW ----
  *
- * Layer norm of the rows of x [rows][cols] (rows ldx apart), rows >= 0, cols >= 1:
+ * Layer norm of the rows of x [rows][cols] (rows ldx apart), rows >= 0, 1 <= cols <= 2^24:
  *   mean, var: of a row's values (var their mean squared distance from the mean),
  *   rstd = 1 / sqrt(var + eps), y = (x - mean) rstd weight + bias
  * x and y (rows ldy apart) of `type`, weight and bias [cols] of `wtype`: `type` or float32; NULL: 1 and 0.
@@ -435,8 +435,9 @@ int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, co
  *   z = x w^T + bias, y = act(z) + residual
  * x [T][K] (rows ldx apart), w [N][K] (ldw), bias [N], residual [T][N] (ldr) and y [T][N] (ldy) of type
  * bfloat16 or float16; bias and residual may be NULL. act: HOBFLOPS_GATE_*, or HOBFLOPS_GATE_NONE: z itself.
- * Sums, z and the activation in float32, one rounding at the end. y may be the residual (same rows). z, if
- * not NULL, receives z [T][N], dense, rounded to the type: what the backward pass needs of an activation.
+ * Sums, z and the activation in float32, one rounding at the end. y may be the residual (same rows), and
+ * otherwise overlaps no input. z, if not NULL, receives z [T][N], dense, rounded to the type: what the backward pass
+ * needs of an activation.
  * With align 16 and K, ldx and ldw multiples of 8 the kernels read x and w in place; else a call of more than a few
  * tokens copies what it must into the workspace first. */
 enum { HOBFLOPS_GATE_NONE = -1 };

@@ -238,7 +238,7 @@ int align_ok(int align) { return align == 2 || align == 4 || align == 8 || align
 
 int norm_check(const hobflops_norm_desc* d) {
   if (!d) return HOBFLOPS_EINVAL;
-  if (d->cols < 1 || !extent_ok(d->rows, d->cols, d->ldx) || !extent_ok(d->rows, d->cols, d->ldy) ||
+  if (d->cols < 1 || d->cols > (int64_t)1 << 24 || !extent_ok(d->rows, d->cols, d->ldx) || !extent_ok(d->rows, d->cols, d->ldy) ||
       !type_ok(d->type) || !type_ok(d->wtype) || !(d->eps >= 0.0) || !isfinite(d->eps))
     return HOBFLOPS_EINVAL;
   return d->wtype == d->type || d->wtype == HOBFLOPS_TYPE_F32 ? HOBFLOPS_OK : HOBFLOPS_EUNSUPPORTED;

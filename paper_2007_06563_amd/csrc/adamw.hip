@@ -307,12 +307,12 @@ hipError_t launch_adamw(const hobflops_adamw_desc& d, const hobflops_adamw_tenso
   };
   for (int i = 0; i < count; ++i) {
     const hobflops_adamw_tensor& c = tensors[i];
-    // a part of a tensor a launch, so that a launch has fewer than 2^31 workgroups
-    const int64_t part = (int64_t)1 << 40;
+    // a part of a tensor a launch, so that a launch has fewer than 2^32 threads
+    const int64_t part = (int64_t)1 << 34;
     for (int64_t o = 0; c.g && o < c.n; o += part) {
       const int64_t n = c.n - o < part ? c.n - o : part;
       const uint64_t groups = (uint64_t)((n + chunk - 1) / chunk);
-      if (a.count == kTensors || grid + groups >= (uint64_t)1 << 31) flush();
+      if (a.count == kTensors || grid + groups >= (uint64_t)1 << 24) flush();
       Tensor& e = a.t[a.count++];
       const int gb = d.grad_type == HOBFLOPS_TYPE_F32 ? 4 : 2;
       e.p = c.p + o;

@@ -173,6 +173,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
 #pragma unroll
     for (int k = 0; k < 8; ++k) bias[k] = (float)b[k];
   }
+  const bool apart = p.act != kNoAct || p.z;  // bias, z and the activation in a loop before the residual's
   Vec more[2][kPasses] = {};
 #pragma unroll
   for (int n = 0; n < kPasses; ++n) more[0][n] = more0[n];
@@ -183,7 +184,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
       *(f32x4*)(lds + (lane & 15) * kRow + 64 * i + 16 * (lane >> 4)) = acc[i][j];
     if (j + 1 < NJ) load_residual<T, NI>(p, f0, t0 + 16 * (j + 1), lane, more[(j + 1) & 1]);
     wave_sync();
-    if (p.act != kNoAct) {
+    if (apart) {
 #pragma unroll 1
       for (int n = 0; n < kPasses; ++n) {
         f32x4* at = (f32x4*)(mine + n * kAtOnce * kRow);
@@ -209,7 +210,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
       Vec y;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float e = v[k >> 2][k & 3] + (p.act == kNoAct ? bias[k] : 0.0f);
+        const float e = v[k >> 2][k & 3] + (apart ? 0.0f : bias[k]);
         y[k] = (E)(e + (float)more[j & 1][n][k]);
       }
       if (t < p.T_) store8((E*)p.y + t * p.ldy, y);
@@ -282,6 +283,7 @@ __global__ __launch_bounds__(256, 2) void linear_small_kernel(LinearArgs p) {
   HOBFLOPS_STAGES2(128, 128);
   linear_tile<T, 128, 128, 2, 2, 2>(p, sa, sb);
 }
+
 // The parts of a sum in their order, then the epilogue: 4 values a thread.
 template <class T>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int splits) {

@@ -141,6 +141,24 @@ def test_the_residual_may_be_the_output(T, K, N, act):
     assert torch.equal(r, want)
 
 
+@pytest.mark.parametrize("T,K,N", [(1, 64, 40), (40, 264, 100), (300, 520, 4096), (20, 8192, 64), (2100, 136, 2600)])
+def test_z_without_an_activation(T, K, N):
+    """The C call takes a z then, too: y before the residual."""
+    import ctypes
+    hf = need_gpu()
+    x, _ = _make(T, K, "bf16", 30)
+    w, _ = _make(N, K, "bf16", 31, K ** -0.5)
+    b, r = _make(1, N, "bf16", 32)[0][0].contiguous(), _make(T, N, "bf16", 33)[0]
+    y, z = torch.empty_like(r), torch.empty_like(r)
+    d = hf.LinearDesc(T, K, N, K, K, N, N, 1, hf.GATE_NONE, 16)
+    n = ctypes.c_int64()
+    assert hf.lib().hobflops_linear_workspace(ctypes.byref(d), 0, ctypes.byref(n)) == 0
+    ws = torch.empty(n.value + 16, dtype=torch.uint8, device="cuda")
+    assert hf.lib().hobflops_linear(ctypes.byref(d), *[t.data_ptr() for t in (x, w, b, r, y, z, ws)], n.value,
+                                    torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(z, hf.linear(x, w, b)) and torch.equal(y, hf.linear(x, w, b, residual=r))
+
+
 @pytest.mark.parametrize("T,K,N", [(1, 96, 40), (5, 1000, 33), (40, 264, 100), (300, 520, 520), (20, 8192, 64),
                                    (2100, 136, 2600)])
 @pytest.mark.parametrize("act", [None, 0, 1, 2])

@@ -25,7 +25,7 @@ def _norm_desc(hf, **kw):
     (dict(rows=-1), -1), (dict(cols=0), -1), (dict(ldx=63), -1), (dict(ldy=63), -1), (dict(type=3), -1),
     (dict(wtype=3), -1), (dict(wtype=2), -2), (dict(type=0, wtype=1), -2), (dict(eps=-1e-9), -1),
     (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1), (dict(rows=1 << 40), -1),
-    (dict(cols=1 << 31, ldx=1 << 31, ldy=1 << 31), -1)])
+    (dict(cols=(1 << 24) + 1, ldx=1 << 25, ldy=1 << 25), -1)])
 def test_norm_refusals(hf, bad, status):
     L, n = hf.lib(), ctypes.c_int64()
     d = _norm_desc(hf, **bad)
