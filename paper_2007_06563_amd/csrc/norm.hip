@@ -264,11 +264,13 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
   }
 }
 
-// As norm_kernel; a lane also keeps its columns' parts of dw and db.
+// As norm_kernel; a lane also keeps its columns' parts of dw and db. Sixteen waves with four times 16 bytes a lane have
+// registers for neither the next row nor the weights, which come from L2 for each row.
 template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
   constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;
+  constexpr bool kAhead = NW * NC < 64;
   __shared__ float2 lds[2 * NW];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t stride = (int64_t)gridDim.x * kRows;
@@ -292,11 +294,21 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
       for (int c = 0; c < NC; ++c) an[c] = chunk[c].load((const E*)p.add + row * p.ld_add);
     }
   };
-  if (first < p.rows) load(first);
-  float w[NC][V], dw[NC][V] = {}, db[NC][V] = {};
-  load_columns<T, W>(p.w, chunk, 1.0f, w);
+  if (kAhead && first < p.rows) load(first);
+  float w[kAhead ? NC : 1][V], dw[NC][V] = {}, db[NC][V] = {};
+  if constexpr (kAhead) load_columns<T, W>(p.w, chunk, 1.0f, w);
+  const auto weights = [&](int c) -> const float(&)[V] {
+    if constexpr (kAhead) {
+      return w[c];
+    } else {
+      const Chunk<T> one[1] = {chunk[c]};
+      load_columns<T, W>(p.w, one, 1.0f, w);
+      return w[0];
+    }
+  };
   int place = 0;
   for (int64_t row = first; row < p.rows; row += stride) {
+    if (!kAhead) load(row);
     u32x4v xe[NC], ge[NC], ae[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -306,18 +318,20 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     }
     // half of the difference, which stays within range, and twice rstd
     const float half = 0.5f * mean, twice = 2.0f * rstd, r = rstd;
-    load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
+    if (kAhead) load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
     float2 s{0.0f, 0.0f};
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NC; ++c) {
+      const float(&wc)[V] = weights(c);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float g = value_of<T>(ge[c], j);
         const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
-        const float a = counted<NC>(g * w[c][j], c, j, chunk[c].lead);
+        const float a = counted<NC>(g * wc[j], c, j, chunk[c].lead);
         s.x += a;
         s.y += a * counted<NC>(xh, c, j, chunk[c].lead);
       }
+    }
     s = row_sums<NW>(s, lds, place);
     place ^= 1;
     s.x /= n;
@@ -327,6 +341,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     for (int c = 0; c < NC; ++c) asm("" : "+v"(xe[c]), "+v"(ge[c]), "+v"(ae[c]));
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      const float(&wc)[V] = weights(c);
       float v[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -334,7 +349,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
         const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
         dw[c][j] += g * xh;
         db[c][j] += g;
-        v[j] = r * (g * w[c][j] - s.x - xh * s.y);
+        v[j] = r * (g * wc[j] - s.x - xh * s.y);
         if (p.add) v[j] += value_of<T>(ae[c], j);
       }
       chunk[c].store((E*)p.dx + row * p.cols, v);
@@ -378,7 +393,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
   }
 }
 
-// Rows of more than 32 KB, or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the first).
+// Rows of more than 32 KB (float32: 64), or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the first).
 constexpr int kWide = 16;  // waves
 
 template <class T, class Each>
@@ -511,20 +526,20 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
     }
 }
 
-// The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane at most. (Four a lane, 4097 x 2731 float32:
-// backward 40 us, two waves on a SIMD; two a lane 30.)
+// The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane (of float32 rows beyond 8192 four), the
+// more waves the longer it is. (Four a lane, 4097 x 2731 float32: backward 40 us, two waves on a SIMD; two a lane 28.)
 struct Shape {
   int waves;
   int64_t chunks;  // at most
 };
-constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {4, 256}, {4, 512}, {8, 1024}, {16, 2048}};
-constexpr int kWalk = 6;  // none of them: the rows are walked
+constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {4, 256}, {4, 512}, {8, 1024}, {16, 2048}, {16, 4096}};
+constexpr int kWalk = 7;  // none of them: the rows are walked
 int shape_of(int64_t cols, int type) {
   const int64_t chunks = (cols + (type == HOBFLOPS_TYPE_F32 ? 3 : 7)) / (type == HOBFLOPS_TYPE_F32 ? 4 : 8);
   if (cols < (type == HOBFLOPS_TYPE_F32 ? 4 : 8)) return kWalk;  // (no whole 16 bytes)
   int i = 0;
   while (i < kWalk && chunks > kShapes[i].chunks) ++i;
-  return i;
+  return i == 6 && type != HOBFLOPS_TYPE_F32 ? kWalk : i;  // (32 values of 16 bits a lane: too many registers)
 }
 // Backward, eight waves of 16-bit values, which are twice as many a lane, would be one workgroup on a CU, or two whose
 // registers spill (8192 x 8192 bfloat16: 226 us); sixteen waves with half of a lane's values take 96.
@@ -578,6 +593,9 @@ void launch_rows(const NormArgs& p, bool grad, hipStream_t s) {
       }
       return launch<T, W, 8, 2>(p, grad, s);
     case 5: return launch<T, W, 16, 2>(p, grad, s);
+    case 6:
+      if constexpr (kVec<T> == 4) return launch<T, W, 16, 4>(p, grad, s);
+      break;
   }
   const unsigned grid = (unsigned)groups_of(p.rows, p.cols, kType<T>, grad);
   if (grad) {

@@ -97,7 +97,7 @@ def _case(hf, rows, cols, dtype, wdtype, ld=None, off=0, scale=1.0, mean=0.0, ep
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 2), (5, 7), (3, 8), (4, 33), (9, 64), (2, 511), (6, 512),
                                        (7, 513), (1, 1000), (13, 1024), (3, 1025), (5, 2048), (2, 2049),
                                        (4, 4096), (1, 4096), (3, 4097), (2, 8192), (3, 8193), (2, 16384),
-                                       (3, 16385), (2, 40001), (300, 96), (130, 1030)])
+                                       (3, 16385), (2, 40001), (300, 96), (130, 1030), (2, 12291)])
 @pytest.mark.parametrize("dtype,wdtype", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f32"), ("bf16", "f32"),
                                           ("f16", "f16")])
 def test_forward_and_backward(rows, cols, dtype, wdtype):
@@ -106,7 +106,7 @@ def test_forward_and_backward(rows, cols, dtype, wdtype):
     _case(hf, rows, cols, dtype, wdtype, add=rows % 2 == 0, affine=cols % 7 != 0)
 
 
-@pytest.mark.parametrize("cols", [40, 1000, 2056, 2731, 5000, 9000, 17000])
+@pytest.mark.parametrize("cols", [40, 1000, 2056, 2731, 5000, 9000, 16381, 17000])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_apart_and_misaligned(cols, dtype):
     hf = need_gpu()
