@@ -2,7 +2,7 @@
 //   g' = scale g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
 //   p = p (1 - lr decay) - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // HBM-bound: every tensor is read and written once, in one launch for up to 64 of them (their
-// addresses are kernel arguments). A thread takes 8 values at a time.
+// addresses are kernel arguments). A thread takes 4 values at a time.
 //
 // All operations are float32 ones, each rounded (no multiply-add takes two of them together), so
 // that the results are those of the formula written with elementary operations, bit for bit.
@@ -26,7 +26,7 @@ namespace hobflops {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 8;        // values a thread
+constexpr int kPer = 4;        // values a thread at a time: 16 bytes of float32, whole lines a wave
 constexpr int kTensors = 64;   // a launch: 3 KB of arguments
 
 struct Tensor {
@@ -51,7 +51,7 @@ struct Args {
 
 // Rounds of a workgroup, kThreads * kPer values each.
 template <bool kStream>
-constexpr int kRounds = kStream ? 4 : 1;
+constexpr int kRounds = kStream ? 8 : 1;
 
 // 32 bits stirred: two rounds of a fold and an odd factor (digits of the square roots of 3 and 2).
 __host__ __device__ __forceinline__ uint32_t stirred(uint32_t x) {
@@ -71,65 +71,61 @@ __device__ __forceinline__ uint32_t bits_of(uint32_t key, int64_t place) {
   return stirred((uint32_t)place * 0x9E3779B9u + (key ^ (uint32_t)(place >> 32) * 0x6A09E667u));
 }
 
+// A thread's values, `left` of them; zeros beyond.
 template <class G, bool kStream>
-__device__ __forceinline__ void load_values(const typename G::elem* src, int64_t left, float (&v)[8]) {
+__device__ __forceinline__ void load_values(const typename G::elem* src, int64_t left, float (&v)[kPer]) {
+  typedef typename G::elem E;
   if (left >= kPer) {
-    typename G::elem e[8];
-    constexpr int n = sizeof e / 16;
-    u32x4v w[n];
+    typedef uint32_t Words __attribute__((ext_vector_type(kPer * sizeof(E) / 4), aligned(sizeof(E))));
+    const Words w = kStream ? __builtin_nontemporal_load((const Words*)src) : *(const Words*)src;
+    E e[kPer];
+    __builtin_memcpy(e, &w, sizeof e);
 #pragma unroll
-    for (int i = 0; i < n; ++i) w[i] = kStream ? __builtin_nontemporal_load((const Words16*)src + i) : ((const Words16*)src)[i];
-    __builtin_memcpy(e, w, sizeof e);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)e[j];
+    for (int j = 0; j < kPer; ++j) v[j] = (float)e[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < left ? (float)src[j] : 0.0f;
+    for (int j = 0; j < kPer; ++j) v[j] = j < left ? (float)src[j] : 0.0f;
   }
 }
 template <class G, bool kStream>
-__device__ __forceinline__ void store_values(typename G::elem* dst, int64_t left, const float (&v)[8]) {
+__device__ __forceinline__ void store_values(typename G::elem* dst, int64_t left, const float (&v)[kPer]) {
+  typedef typename G::elem E;
   if (left >= kPer) {
-    typename G::elem e[8];
+    E e[kPer];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = (typename G::elem)v[j];
-    constexpr int n = sizeof e / 16;
-    u32x4v w[n];
-    __builtin_memcpy(w, e, sizeof e);
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      if (kStream)
-        stream16((u32x4v*)dst + i, w[i]);
-      else
-        ((Words16*)dst)[i] = w[i];
-    }
+    for (int j = 0; j < kPer; ++j) e[j] = (E)v[j];
+    typedef uint32_t Words __attribute__((ext_vector_type(kPer * sizeof(E) / 4), aligned(sizeof(E))));
+    Words w;
+    __builtin_memcpy(&w, e, sizeof e);
+    if (kStream)
+      __builtin_nontemporal_store(w, (Words*)dst);
+    else
+      *(Words*)dst = w;
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) dst[j] = (typename G::elem)v[j];
+    for (int j = 0; j < kPer; ++j)
+      if (j < left) dst[j] = (E)v[j];
   }
 }
 
 template <int kFmt>
-__device__ __forceinline__ void decode8(const uint8_t* codes, uint8_t scale, float (&v)[8]) {
-  uint32_t w[2];
-  __builtin_memcpy(w, codes, 8);
+__device__ __forceinline__ void decode_values(const uint8_t* codes, uint8_t scale, float (&v)[kPer]) {
+  uint32_t w;
+  __builtin_memcpy(&w, codes, 4);
   const float s = pow2_scale_of(scale);
+  const f32x4 d = decode4<kFmt>(w);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const f32x4 d = decode4<kFmt>(w[h]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[4 * h + j] = d[j] * s;
-  }
+  for (int j = 0; j < kPer; ++j) v[j] = d[j] * s;
 }
 
-// The smallest scale exponent, at least kMinScale, under which the largest of the four threads' values is no
+// The smallest scale exponent, at least kMinScale, under which the largest of eight threads' values is no
 // larger than the format's largest, 1.75 * 2^8 or 1.75 * 2^15.
 template <int kFmt>
-__device__ __forceinline__ int group_scale(const float (&v)[8]) {
+__device__ __forceinline__ int group_scale(const float (&v)[kPer]) {
   uint32_t a = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) a = max(a, finite_abs(v[j]));
+  for (int j = 0; j < kPer; ++j) a = max(a, finite_abs(v[j]));
+  a = max(a, row_xor<1>(a));
   a = max(a, row_xor<2>(a));
   a = max(a, row_xor<3>(a));
   const int k = (int)(a >> 23) - 127 - (kFmt == kE4M3 ? 8 : 15) + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
@@ -147,9 +143,9 @@ __device__ __forceinline__ float in_steps(float n, float& step) {
 }
 
 template <int kFmt>
-__device__ __forceinline__ void store_codes(uint8_t* codes, const float (&q)[8]) {
-  const uint32_t w[2] = {encode4<kFmt>(q[0], q[1], q[2], q[3]), encode4<kFmt>(q[4], q[5], q[6], q[7])};
-  __builtin_memcpy(codes, w, 8);
+__device__ __forceinline__ void store_codes(uint8_t* codes, const float (&q)[kPer]) {
+  const uint32_t w = encode4<kFmt>(q[0], q[1], q[2], q[3]);
+  __builtin_memcpy(codes, &w, 4);
 }
 
 // The factors that depend on the step, where it or the rate stands on the device.
@@ -168,8 +164,8 @@ __device__ __forceinline__ void factors_of(const Args& a, float& keep, float& ra
   if (a.step_at) key = step_key(t, a.seed);
 }
 
-// kStream: so many values that they do not stay in the last cache from step to step: past the caches, and four rounds a
-// workgroup. (2.16 M values, 60 MB, in this way 20.9 us, otherwise 13.3; 138 M values 790, otherwise 805.)
+// kStream: so many values that they do not stay in the last cache from step to step: past the caches, and eight rounds a
+// workgroup. (2.16 M values, 60 MB, in this way 21 us, otherwise 13; 138 M values 2 % less in this way.)
 template <int kFmt, class G, bool kStream>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
 #pragma clang fp contract(off)
@@ -185,24 +181,24 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
   const float scale = a.scale_at ? *a.scale_at : a.scale;
   int64_t i = (int64_t)(blockIdx.x - first) * kRounds<kStream> * (kThreads * kPer) + threadIdx.x * kPer;
   for (int round = 0; round < kRounds<kStream>; ++round, i += kThreads * kPer) {
-    // (four threads of a group of 32 leave together)
+    // (eight threads of a group of 32 leave together)
     if (i >= ((t.n + 31) & ~(int64_t)31)) return;
     const int64_t left = t.n - i, at = t.at + i;
-    float p[8], g[8], m[8], v[8];
+    float p[kPer], g[kPer], m[kPer], v[kPer];
     load_values<TypeF32, kStream>(t.p + i, left, p);
     load_values<G, kStream>((const typename G::elem*)t.g + i, left, g);
     if constexpr (kFmt < 0) {
       load_values<TypeF32, kStream>((const float*)a.m + at, left, m);
       load_values<TypeF32, kStream>((const float*)a.v + at, left, v);
     } else {
-      decode8<kFmt>((const uint8_t*)a.m + at, a.m_scales[at >> 5], m);
-      decode8<kFmt>((const uint8_t*)a.v + at, a.v_scales[at >> 5], v);
+      decode_values<kFmt>((const uint8_t*)a.m + at, a.m_scales[at >> 5], m);
+      decode_values<kFmt>((const uint8_t*)a.v + at, a.v_scales[at >> 5], v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = v[j] * v[j];
+      for (int j = 0; j < kPer; ++j) v[j] = v[j] * v[j];
     }
-    float r[8];
+    float r[kPer];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kPer; ++j) {
       const float d = g[j] * scale;
       m[j] = m[j] * a.b1 + d * a.c1;
       v[j] = v[j] * a.b2 + d * d * a.c2;
@@ -222,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
     } else {
       if (left < kPer) {  // behind the tensor's end, up to its last group's: zeros
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kPer; ++j)
           if (j >= left) m[j] = r[j] = v[j] = 0.0f;
       }
       const int km = group_scale<kFmt>(m), kr = group_scale<kFmt>(r);
@@ -233,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
       const float sm = pow2f(-km), sr = pow2f(-kr);
       constexpr float kLeast = kFmt == kE4M3 ? 0x1p-9f : 0x1p-16f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < kPer; ++j) {
         const uint32_t bits = bits_of(key, at + j);
         float step;
         const float n = in_steps<kFmt>(__builtin_fabsf(m[j]) * sm, step), whole = floorf(n);
