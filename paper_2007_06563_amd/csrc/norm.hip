@@ -164,6 +164,15 @@ struct Stats {
   float mean, off, rstd;  // the mean is mean + off
 };
 
+// From the mean of the differences' squares. What is left of equal values far from 0 is rounding, 2^-24 of the
+// differences' mean; a variance of no less than 2^-44 of its square keeps that from growing.
+__device__ __forceinline__ float variance(float squares, float off) {
+  const float var = squares - off * off, least = off * off * 0x1p-44f;
+  return var < least ? least : var;
+}
+// The same of a row that was scaled by `down`: equal values whose eps is 0 there have the rstd that eps gives.
+__device__ __forceinline__ bool equal_values(float rstd, float eps) { return rstd == INFINITY && eps > 0.0f; }
+
 // A row's values become their differences from the mean.
 template <class T, int NW, int NC>
 __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T> (&chunk)[NC], int64_t cols,
@@ -189,8 +198,7 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
     }
   s = row_sums<NW>(s, lds, 1);
   r.off = s.x / n;
-  float var = s.y / n - r.off * r.off;
-  var = var < 0.0f ? 0.0f : var;
+  const float var = variance(s.y / n, r.off);
   r.rstd = 1.0f / sqrtf(var + eps);
   // (NaN, or 0 for an infinite variance: for the caller)
   return r;
@@ -247,9 +255,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
 #pragma unroll
         for (int j = 0; j < V; ++j) x[c][j] *= down;
       s = stats_of<T, NW>(x, chunk, p.cols, p.eps * down * down, lds);
+      const bool equal = equal_values(s.rstd, p.eps);
+      if (equal) s.rstd = 0.0f;
       if (p.mean && lane == 0) {
         p.mean[row] = (s.mean + s.off) / down;
-        p.rstd[row] = s.rstd * down;
+        p.rstd[row] = equal ? 1.0f / sqrtf(p.eps) : s.rstd * down;
       }
     } else if (p.mean && lane == 0) {
       p.mean[row] = s.mean + s.off;
@@ -425,8 +435,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
         s.y += d * d;
       });
       off = s.x / n;
-      float var = s.y / n - off * off;
-      var = var < 0.0f ? 0.0f : var;
+      const float var = variance(s.y / n, off);
       rstd = 1.0f / sqrtf(var + p.eps * down * down);
       if (rstd > 0.0f || again) break;
       float most = 0.0f;
@@ -440,9 +449,11 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
       const int e = (int)(__float_as_uint(most) >> 23) - 127;
       down = pow2f(-(e < 126 ? e : 126));
     }
+    const bool equal = down != 1.0f && equal_values(rstd, p.eps);
+    if (equal) rstd = 0.0f;
     if (p.mean && threadIdx.x == 0) {
       p.mean[row] = (mean + off) / down;
-      p.rstd[row] = rstd * down;
+      p.rstd[row] = equal ? 1.0f / sqrtf(p.eps) : rstd * down;
     }
     for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
       float v[8], w[8], b[8];

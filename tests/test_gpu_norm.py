@@ -197,6 +197,23 @@ def test_constant_rows():
     assert (dx == 0).all() and (dw == 0).all() and (db == 2).all()
 
 
+@pytest.mark.parametrize("cols", [5, 48, 1000, 3000, 9000, 20000])
+@pytest.mark.parametrize("value", [1000.1, -1e10, 1e15, 1.1e19, -7e25, 2.0 ** 127, 3e38])
+def test_equal_values_far_from_zero(cols, value):
+    """Nothing is left of them but rounding: a mean is _chain() roundings off, the difference's own mean as many of
+    it, and rstd is at most 2^22 over that mean."""
+    hf = need_gpu()
+    say("norm equal", cols, value)
+    x = torch.full((3, cols), value, device="cuda")
+    x[1] = torch.arange(cols, device="cuda") % 7
+    y, saved = hf.layer_norm(x, save=True)
+    assert (y[0].abs() <= _chain(cols) / 2).all() and torch.equal(y[0], y[2])
+    assert torch.equal(y[1], hf.layer_norm(x[1:2])[0])
+    assert abs(saved.mean[0].item() / x[0, 0].item() - 1) <= 2 * D and saved.rstd.isfinite().all()
+    dx, dw, db = hf.layer_norm_backward(torch.ones_like(x), x, saved)
+    assert dx.isfinite().all() and dw.isfinite().all() and (db == 3).all()
+
+
 def test_no_rows_and_in_place():
     hf = need_gpu()
     w = torch.ones(64, device="cuda")
