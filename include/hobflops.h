@@ -408,7 +408,7 @@ int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, 
  * x and y (rows ldy apart) of `type`, weight and bias [cols] of `wtype`: `type` or float32; NULL: 1 and 0.
  * Sums in float32, one rounding at the end. Any finite row has its result, also where its squares pass
  * float32's range; NaN and infinities make their own row NaN. With eps 0 a row of one value has rstd
- * infinity and is NaN. y may be x. mean and rstd, float32 [rows], are for the backward pass
+ * infinity and is NaN. y may be x (the same rows) and otherwise overlaps no input (HOBFLOPS_EINVAL). mean and rstd, float32 [rows], are for the backward pass
  * (both or neither NULL). */
 typedef struct {
   int64_t rows, cols;
@@ -436,7 +436,7 @@ int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, co
  * x [T][K] (rows ldx apart), w [N][K] (ldw), bias [N], residual [T][N] (ldr) and y [T][N] (ldy) of type
  * bfloat16 or float16; bias and residual may be NULL. act: HOBFLOPS_GATE_*, or HOBFLOPS_GATE_NONE: z itself.
  * Sums, z and the activation in float32, one rounding at the end. y may be the residual (same rows), and
- * otherwise overlaps no input. z, if not NULL, receives z [T][N], dense, rounded to the type: what the backward pass
+ * otherwise overlaps no input (HOBFLOPS_EINVAL). z, if not NULL, receives z [T][N], dense, rounded to the type: what the backward pass
  * needs of an activation.
  * With align 16 and K, ldx and ldw multiples of 8 the kernels read x and w in place; else a call of more than a few
  * tokens copies what it must into the workspace first. */

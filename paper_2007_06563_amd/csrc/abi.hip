@@ -255,6 +255,26 @@ int linear_check(const hobflops_linear_desc* d) {
   return d->type == HOBFLOPS_TYPE_F32 ? HOBFLOPS_EUNSUPPORTED : HOBFLOPS_OK;
 }
 
+// Rows of values, a vector among them.
+struct Rows {
+  const void* p;
+  int64_t rows, cols, ld;
+  int bytes;  // of a value
+};
+int same_rows(const Rows& a, const Rows& b) { return a.p == b.p && (a.ld == b.ld || a.rows == 1); }
+// Whether two of them have memory in common. (Columns beside each other in one wider matrix have none.)
+int overlap(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p) return 0;
+  const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  const uintptr_t na = (uintptr_t)a.cols * a.bytes, nb = (uintptr_t)b.cols * b.bytes;
+  if (pa + (uintptr_t)((a.rows - 1) * a.ld * a.bytes) + na <= pb || pb + (uintptr_t)((b.rows - 1) * b.ld * b.bytes) + nb <= pa)
+    return 0;
+  const uintptr_t step = (uintptr_t)(a.rows > 1 ? a.ld * a.bytes : b.ld * b.bytes);
+  if (b.rows > 1 && (uintptr_t)(b.ld * b.bytes) != step) return 1;
+  const uintptr_t apart = pb >= pa ? (pb - pa) % step : (step - (pa - pb) % step) % step;  // from a row of a to the next of b
+  return !(apart >= na && apart + nb <= step);
+}
+
 // Memory that a call writes or only reads.
 struct Range {
   uintptr_t begin, end;
@@ -784,6 +804,10 @@ int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* 
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(weight, wb) || !aligned_to(bias, wb) ||
       !aligned_to(mean, 4) || !aligned_to(rstd, 4))
     return HOBFLOPS_EALIGN;
+  const Rows in{x, d->rows, d->cols, d->ldx, b}, out{y, d->rows, d->cols, d->ldy, b};
+  if ((overlap(in, out) && !same_rows(in, out)) || overlap(out, Rows{weight, 1, d->cols, d->cols, wb}) ||
+      overlap(out, Rows{bias, 1, d->cols, d->cols, wb}))
+    return HOBFLOPS_EINVAL;
   LayerNorm p{d->rows, d->cols, d->ldx, d->ldy, 0, d->type, d->wtype, d->eps};
   p.x = x;
   p.w = weight;
@@ -858,6 +882,13 @@ int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w,
       !aligned_to(residual, 2) || !aligned_to(y, 2) || !aligned_to(z, 2) ||
       (need > 0 && !aligned_to(workspace, 16)))
     return HOBFLOPS_EALIGN;
+  const Rows more{residual, d->T, d->N, d->ldr, 2};
+  for (const Rows& out : {Rows{y, d->T, d->N, d->ldy, 2}, Rows{z, d->T, d->N, d->N, 2}}) {
+    if (overlap(out, Rows{x, d->T, d->K, d->ldx, 2}) || overlap(out, Rows{w, d->N, d->K, d->ldw, 2}) ||
+        overlap(out, Rows{bias, 1, d->N, d->N, 2}) || (overlap(out, more) && !(out.p == y && same_rows(out, more))))
+      return HOBFLOPS_EINVAL;
+  }
+  if (overlap(Rows{y, d->T, d->N, d->ldy, 2}, Rows{z, d->T, d->N, d->N, 2})) return HOBFLOPS_EINVAL;
   const LinearForward p{x, w, bias, residual, y, z, workspace};
   return hip_status(launch_linear_forward(*d, p, (hipStream_t)stream));
 }

@@ -228,3 +228,22 @@ def test_8_bit_states_train_as_float32_ones_do():
     # square a value, over 8192 of them 0.4 % of the mean
     assert abs(left[3] / left[1] - 1) < 0.05
     assert left[2] < 2 * left[0]
+
+
+def test_columns_of_one_matrix():
+    """Inputs and results beside each other in wider rows; what would overlap is refused."""
+    hf = need_gpu()
+    g = torch.Generator().manual_seed(3)
+    for T in (1, 5, 300):
+        both = torch.randn(T, 264, generator=g).bfloat16().cuda()
+        w = torch.randn(132, 132, generator=g).bfloat16().cuda()
+        x, y = both[:, :132], both[:, 132:]
+        want = hf.layer_norm(x.clone()), hf.linear(x.clone(), w)
+        assert torch.equal(hf.layer_norm(x, out=y), want[0])
+        assert torch.equal(hf.linear(x, w, out=y), want[1])
+        assert torch.equal(hf.linear(y, w, out=x), hf.linear(want[1], w))
+        for out in (x, both[:, 1:133]):
+            with pytest.raises(hf.HobflopsError):
+                hf.linear(x, w, out=out)
+        with pytest.raises(hf.HobflopsError):
+            hf.layer_norm(x, out=both[:, 131:263])

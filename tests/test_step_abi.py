@@ -60,6 +60,27 @@ def test_norm_pointers(hf):
     assert L.hobflops_layer_norm_backward(_norm_desc(hf, ld_add=63), *[FAKE] * 10, BIG, None) == -1
 
 
+@pytest.mark.parametrize("y,kw", [
+    (0x10002, {}), (0x10000 - 2 * 255, {}), (0x10000 + 2 * 255, {}),    # one value of the first or the last row
+    (0x10000, dict(ldx=128)), (0x10000 + 2 * 65, dict(ldx=128, ldy=128)), (0x10000 + 2 * 64, dict(ldx=128, ldy=129)),
+    (0x10000 + 2 * 64, dict(rows=1, cols=65, ldx=65, ldy=65)), (0x20000 - 2, {}), (0x30000 + 4 * 63, {})])
+def test_norm_overlaps(hf, y, kw):
+    """x at 0x10000, weight and bias (float32) at 0x20000 and 0x30000."""
+    args = [ctypes.c_void_p(p) for p in (0x10000, 0x20000, 0x30000, y)]
+    assert hf.lib().hobflops_layer_norm(_norm_desc(hf, **kw), *args, None, None, None) == -1
+
+
+@pytest.mark.parametrize("kw", [
+    dict(y=0x100000), dict(y=0x200000 + 2 * 64 * 95), dict(y=0x300000 - 2), dict(y=0x400002),
+    dict(y=0x400000, ldr=97), dict(z=0x400000), dict(z=0x100000 - 2), dict(y=0x600000 + 2 * 96 * 19),
+    dict(y=0x100000 + 2 * 63, ldx=192, ldy=192)])
+def test_linear_overlaps(hf, kw):
+    a = dict(x=0x100000, w=0x200000, bias=0x300000, residual=0x400000, y=0x500000, z=0x600000)
+    d = _linear_desc(hf, **{k: v for k, v in kw.items() if k not in a})
+    a.update({k: v for k, v in kw.items() if k in a})
+    assert hf.lib().hobflops_linear(d, *[ctypes.c_void_p(p) for p in a.values()], FAKE, BIG, None) == -1
+
+
 def _linear_desc(hf, **kw):
     d = dict(T=20, K=64, N=96, ldx=64, ldw=64, ldy=96, ldr=96, type=1, act=0, align=16)
     d.update(kw)
