@@ -55,24 +55,43 @@ __device__ __forceinline__ Sigmoid silu_gate(float z) {
   const float e = far_exp(z) * 0x1p-64f, r = __builtin_amdgcn_rcpf(1.0f + e), far = e * r;
   return z < 0.0f ? Sigmoid{far, r} : Sigmoid{r, far};
 }
-__device__ __forceinline__ float act_of(float z, int act) {
+// The activation of N values, or dy times its derivative. The choice of the activation stands around the values, so that they
+// run through its chain of instructions beside each other. (A choice for each value: an epilogue of gelu, z and residual
+// 20 us a round of tiles of 256 x 256, this 14.)
+template <int N>
+__device__ __forceinline__ void act_on(float (&v)[N], int act) {
   if (act == HOBFLOPS_GATE_SILU) {
-    const float e = far_exp(z), v = z * __builtin_amdgcn_rcpf(__builtin_fmaf(e, 0x1p-64f, 1.0f));
-    return z < 0.0f ? v * e * 0x1p-64f : v;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float z = v[k], e = far_exp(z), y = z * __builtin_amdgcn_rcpf(__builtin_fmaf(e, 0x1p-64f, 1.0f));
+      v[k] = z < 0.0f ? y * e * 0x1p-64f : y;
+    }
+  } else if (act == HOBFLOPS_GATE_GELU) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] *= gelu_gate(v[k]).p;
+  } else if (act == HOBFLOPS_GATE_RELU) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = v[k] > 0.0f || v[k] != v[k] ? v[k] : 0.0f;
   }
-  if (act == HOBFLOPS_GATE_GELU) return z * gelu_gate(z).p;
-  return act == kNoAct || z > 0.0f || z != z ? z : 0.0f;
 }
-__device__ __forceinline__ float act_grad_of(float z, int act) {
+template <int N>
+__device__ __forceinline__ void times_act_grad(float (&d)[N], const float (&z)[N], int act) {
   if (act == HOBFLOPS_GATE_SILU) {
-    const Sigmoid v = silu_gate(z);
-    return v.s * __builtin_fmaf(z, v.c, 1.0f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const Sigmoid v = silu_gate(z[k]);
+      d[k] *= v.s * __builtin_fmaf(z[k], v.c, 1.0f);
+    }
+  } else if (act == HOBFLOPS_GATE_GELU) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const Gate v = gelu_gate(z[k]);
+      d[k] *= __builtin_fmaf(z[k], v.e * 0.398942280f, v.p);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) d[k] *= z[k] > 0.0f ? 1.0f : z[k] != z[k] ? z[k] : 0.0f;
   }
-  if (act == HOBFLOPS_GATE_GELU) {
-    const Gate v = gelu_gate(z);
-    return __builtin_fmaf(z, v.e * 0.398942280f, v.p);
-  }
-  return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
 }
 
 struct LinearArgs {
@@ -188,18 +207,19 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
 #pragma unroll 1
       for (int n = 0; n < kPasses; ++n) {
         f32x4* at = (f32x4*)(mine + n * kAtOnce * kRow);
-        f32x4 v[2] = {at[0], at[1]};
+        const f32x4 sum[2] = {at[0], at[1]};
         const int64_t t = t0 + 16 * j + n * kAtOnce + first;
+        float v[8];
         Vec z;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float e = v[k >> 2][k & 3] + bias[k];
-          z[k] = (E)e;
-          v[k >> 2][k & 3] = act_of(e, p.act);
+          v[k] = sum[k >> 2][k & 3] + bias[k];
+          z[k] = (E)v[k];
         }
         if (p.z && t < p.T_) store8((E*)p.z + t * p.N, z);
-        at[0] = v[0];
-        at[1] = v[1];
+        act_on(v, p.act);
+        at[0] = f32x4{v[0], v[1], v[2], v[3]};
+        at[1] = f32x4{v[4], v[5], v[6], v[7]};
       }
     }
 #pragma unroll
@@ -300,9 +320,10 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int spli
     }
     f32x4 r = {};
     if (p.residual) r = load4<T>((const E*)p.residual + row * p.ldr, col, p.N);
-    float e[4];
+    float e[4] = {v[0], v[1], v[2], v[3]};
+    act_on(e, p.act);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = act_of(v[k], p.act) + r[k];
+    for (int k = 0; k < 4; ++k) e[k] += r[k];
     store4<T>((E*)p.y + row * p.ldy, col, p.N, e);
   }
 }
@@ -452,9 +473,10 @@ __global__ __launch_bounds__(kDirectWaves * 64) void direct_kernel(LinearArgs p)
     }
     f32x4 more = {};
     if (p.residual) more = load4<T>((const E*)p.residual + t * p.ldr, at, p.N);
-    float e[4];
+    float e[4] = {v[0], v[1], v[2], v[3]};
+    act_on(e, p.act);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = act_of(v[k], p.act) + more[k];
+    for (int k = 0; k < 4; ++k) e[k] += more[k];
     store4<T>((E*)p.y + t * p.ldy, at, p.N, e);
   }
 #endif
@@ -500,15 +522,18 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs
             if (p.z) z[j] = ((const E*)p.z)[t * p.N + col + j];
           }
       }
+      float v[8], w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = (float)d[j];
+        w[j] = (float)z[j];
+      }
+      if (p.z) times_act_grad(v, w, p.act);
       typename T::vec8 o;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float v = (float)d[j];
-        if (p.z) {
-          v = col + j < p.N ? v * act_grad_of((float)z[j], p.act) : 0.0f;
-        }
-        db[j] += v;
-        o[j] = (E)v;
+        db[j] += v[j];
+        o[j] = (E)v[j];
       }
       if (p.out) *(typename T::vec8*)((E*)p.out + t * p.ldo + col) = o;
     }
