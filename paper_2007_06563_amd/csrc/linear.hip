@@ -303,6 +303,19 @@ __global__ __launch_bounds__(256, 2) void linear_small_kernel(LinearArgs p) {
   HOBFLOPS_STAGES2(128, 128);
   linear_tile<T, 128, 128, 2, 2, 2>(p, sa, sb);
 }
+// Launches of about a workgroup a CU, which nothing else hides the latency of: four stages of 128 x 128 sums, or six of 64 x
+// 128, under way, and two waves on a SIMD. (1024 x 4096 -> 4096: 34 us, of linear_small_kernel's 44; 512 x 4096 -> 4096:
+// 24 in 64 x 128, 28 in 128 x 128, 41; four waves with four stages, a wave on a SIMD: 37 and 31.)
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_deep_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES4(128, 128);
+  linear_tile<T, 128, 128, 2, 4, 4>(p, sa, sb);
+}
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_deepest_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES6(64, 128);
+  linear_tile<T, 64, 128, 2, 4, 6>(p, sa, sb);
+}
 
 // The parts of a sum in their order, then the epilogue: 4 values a thread.
 template <class T>
@@ -614,27 +627,31 @@ __global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t
 // ---- plans -------------------------------------------------------------------
 
 // The tiles of a product through LDS and the parts of its sum, by an estimate of their time in microseconds: rounds of
-// workgroups, each its steps of 64 k and about five more to start and end; the parts of a sum are written and read
-// once more in float32, 4 TB/s, and joined in a launch.
+// workgroups, each its steps of 64 k and some more to start and end; the parts of a sum are written and read
+// once more in float32, 4 TB/s, and joined in a launch. The kinds' times are those of the sizes that each is for, measured: of
+// 4096 x 4096 -> 4096 (98 us), 2048 x 4096 -> 4096 (60, the others 84, 65 and 88), 1024 x 4096 -> 4096 (34; 78, 44, 46) and
+// 512 x 4096 -> 4096 (24; 76, 41, 28).
 struct Kind {
-  int side, per_cu;
-  double step;
+  int rows, cols, per_cu;
+  double step, lead;
 };
-constexpr Kind kKinds[] = {{256, 1, 1.42}, {128, 2, 0.8}};
+constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}};
+constexpr int kForwardKinds = 4, kGradKinds = 2;
 struct Tiling {
   int kind, splits;
   double us;
 };
 constexpr int kMostSplits = 32;
-Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K) {
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int kinds) {
   const int64_t steps = (K + kStepK - 1) / kStepK;
   Tiling best{0, 1, -1.0};
-  for (int k = 0; k < 2; ++k) {
-    const int64_t side = kKinds[k].side, slots = kKinds[k].per_cu * kCUs;
-    const int64_t tiles = ((rows + side - 1) / side) * ((cols + side - 1) / side);
+  for (int k = 0; k < kinds; ++k) {
+    const Kind& kind = kKinds[k];
+    const int64_t slots = kind.per_cu * kCUs;
+    const int64_t tiles = ((rows + kind.rows - 1) / kind.rows) * ((cols + kind.cols - 1) / kind.cols);
     for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); ++n) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
-      double us = rounds * ((double)((steps + n - 1) / n) + 5.0) * kKinds[k].step;
+      double us = rounds * ((double)((steps + n - 1) / n) + kind.lead) * kind.step;
       if (n > 1) us += 4.0 + (double)(2 * n) * rows * cols * 4.0 / 4e6;
       if (best.us < 0.0 || us < best.us) best = Tiling{k, n, us};
     }
@@ -683,7 +700,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
   const int64_t Kp = round_up(d.K, 8);
-  p.tiles = plan_tiles(d.N, d.T, d.K);
+  p.tiles = plan_tiles(d.N, d.T, d.K, kForwardKinds);
   double us = p.tiles.us + (p.tiles.splits > 1 ? 4.0 : 0.0), direct = 0.0;  // (the second launch's start)
   // (rows that are not in place are copied in a launch of their own first)
   if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
@@ -716,11 +733,11 @@ BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need
   if (need.dw && !in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * p.Kp * 2);
   if (need.dx && !in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * p.Kp * 2);
   if (need.dx) {
-    p.dx = plan_tiles(d.T, d.K, p.Np);
+    p.dx = plan_tiles(d.T, d.K, p.Np, kGradKinds);
     if (p.dx.splits > 1) p.part_x = take(&p.bytes, p.dx.splits * d.T * round_up(d.K, 4) * 4);
   }
   if (need.dw) {
-    p.dw = plan_tiles(d.N, d.K, d.T);
+    p.dw = plan_tiles(d.N, d.K, d.T, kGradKinds);
     if (p.dw.splits > 1) p.part_w = take(&p.bytes, p.dw.splits * d.N * round_up(d.K, 4) * 4);
   }
   const int64_t strips = (d.N + 255) / 256, most = (d.T + 7) / 8, wanted = (2048 + strips - 1) / strips;
@@ -784,23 +801,25 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   if (plan.x >= 0 && plan.w >= 0) p.K = align.ldd;
   const int64_t splits = splits_of(p.K, plan.tiles.splits, &p.per);
   if (splits > 1) p.part = (float*)(ws + plan.part);
-  const int side = kKinds[plan.tiles.kind].side;
-  p.ni = (uint32_t)((d.N + side - 1) / side);
-  p.nj = (uint32_t)((d.T + side - 1) / side);
+  const Kind& kind = kKinds[plan.tiles.kind];
+  p.ni = (uint32_t)((d.N + kind.rows - 1) / kind.rows);
+  p.nj = (uint32_t)((d.T + kind.cols - 1) / kind.cols);
   const unsigned grid = (unsigned)(p.ni * p.nj * splits);
-  if (plan.tiles.kind == 0)
-    linear_kernel<T><<<grid, 512, 0, s>>>(p);
-  else
-    linear_small_kernel<T><<<grid, 256, 0, s>>>(p);
+  switch (plan.tiles.kind) {
+    case 0: linear_kernel<T><<<grid, 512, 0, s>>>(p); break;
+    case 1: linear_small_kernel<T><<<grid, 256, 0, s>>>(p); break;
+    case 2: linear_deep_kernel<T><<<grid, 512, 0, s>>>(p); break;
+    default: linear_deepest_kernel<T><<<grid, 512, 0, s>>>(p);
+  }
   if (p.part)
     linear_join_kernel<T><<<grid_of(d.T * round_up(d.N, 4) / 4, 4096), 256, 0, s>>>(p, (int)splits);
   return hipGetLastError();
 }
 
 uint32_t count_tiles(GradArgs& p, const Tiling& t) {
-  const int64_t b = kKinds[t.kind].side;
-  p.ni = (uint32_t)((p.ni_ + b - 1) / b);
-  p.nj = (uint32_t)((p.nj_ + b - 1) / b);
+  const Kind& kind = kKinds[t.kind];
+  p.ni = (uint32_t)((p.ni_ + kind.rows - 1) / kind.rows);
+  p.nj = (uint32_t)((p.nj_ + kind.cols - 1) / kind.cols);
   return p.ni * p.nj;
 }
 template <class T>

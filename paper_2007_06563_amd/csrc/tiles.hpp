@@ -117,6 +117,20 @@ __device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, boo
   __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128], b2[rows_b * 128];  \
   uint8_t* const sa[3] = {a0, a1, a2};                                                      \
   uint8_t* const sb[3] = {b0, b1, b2}
+#define HOBFLOPS_STAGES4(rows_a, rows_b)                                                        \
+  __shared__ __align__(1024) uint8_t a0[rows_a * 128], a1[rows_a * 128], a2[rows_a * 128],      \
+      a3[rows_a * 128];                                                                         \
+  __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128], b2[rows_b * 128],      \
+      b3[rows_b * 128];                                                                         \
+  uint8_t* const sa[4] = {a0, a1, a2, a3};                                                      \
+  uint8_t* const sb[4] = {b0, b1, b2, b3}
+#define HOBFLOPS_STAGES6(rows_a, rows_b)                                                        \
+  __shared__ __align__(1024) uint8_t a0[rows_a * 128], a1[rows_a * 128], a2[rows_a * 128],      \
+      a3[rows_a * 128], a4[rows_a * 128], a5[rows_a * 128];                                     \
+  __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128], b2[rows_b * 128],      \
+      b3[rows_b * 128], b4[rows_b * 128], b5[rows_b * 128];                                     \
+  uint8_t* const sa[6] = {a0, a1, a2, a3, a4, a5};                                              \
+  uint8_t* const sb[6] = {b0, b1, b2, b3, b4, b5}
 
 // The gradients' products, D[i][j] with i along a row of the output; kParts weights side by side (the gated
 // block's two, a linear layer's one):

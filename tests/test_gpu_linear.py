@@ -129,6 +129,19 @@ def test_many_tiles(T, K, N, dtype, act):
     _backward(hf, xs, ws, z, T, K, N, dtype, act, lds, 0)
 
 
+@pytest.mark.parametrize("T,K,N", [(500, 2040, 4100), (260, 4104, 4000), (700, 16400, 264), (500, 1000, 1100),
+                                   (2048, 512, 1400), (1000, 1027, 4000), (257, 72, 8200), (128, 4096, 11264)])
+@pytest.mark.parametrize("dtype,act,bias,res", [("bf16", 1, True, True), ("f16", None, False, True),
+                                                ("bf16", 2, True, False)])
+def test_a_workgroup_a_cu(T, K, N, dtype, act, bias, res):
+    """Sizes whose tiles have four or six stages, with steps that are no multiple of them, and in parts."""
+    hf = need_gpu()
+    say("linear deep", T, K, N, dtype, act, bias, res)
+    lds = (K, K, N, N)
+    xs, ws, z = _forward(hf, T, K, N, dtype, act, bias, res, lds, 0)
+    _backward(hf, xs, ws, z, T, K, N, dtype, act, lds, 0)
+
+
 @pytest.mark.parametrize("T,K,N", [(1, 64, 40), (9, 1000, 300), (40, 264, 100), (300, 520, 520), (20, 8192, 64)])
 @pytest.mark.parametrize("act", [None, 0])
 def test_the_residual_may_be_the_output(T, K, N, act):
@@ -141,7 +154,8 @@ def test_the_residual_may_be_the_output(T, K, N, act):
     assert torch.equal(r, want)
 
 
-@pytest.mark.parametrize("T,K,N", [(1, 64, 40), (40, 264, 100), (300, 520, 4096), (20, 8192, 64), (2100, 136, 2600)])
+@pytest.mark.parametrize("T,K,N", [(1, 64, 40), (40, 264, 100), (300, 520, 4096), (20, 8192, 64), (2100, 136, 2600),
+                                   (500, 2040, 4104), (260, 4104, 4000)])
 def test_z_without_an_activation(T, K, N):
     """The C call takes a z then, too: y before the residual."""
     import ctypes
