@@ -563,15 +563,15 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs
 }
 
 // Workgroups of dx, as many as `parts`, then those of dW.
-template <class T, int B, int WJ>
+template <class T, int B, int WJ, int S>
 __device__ __forceinline__ void linear_grad_tiles(const GradArgs& dx, const GradArgs& dw, uint32_t parts,
-                                                  uint8_t* const (&sa)[2], uint8_t* const (&sb)[2]) {
+                                                  uint8_t* const (&sa)[S], uint8_t* const (&sb)[S]) {
   const bool first = blockIdx.x < parts;
   const uint32_t b = first ? blockIdx.x : blockIdx.x - parts;
   if (first)
-    grad_tile<T, false, 1, B, B, WJ, 2>(dx, sa, sb, b % (dx.ni * dx.nj), b / (dx.ni * dx.nj));
+    grad_tile<T, false, 1, B, B, WJ, S>(dx, sa, sb, b % (dx.ni * dx.nj), b / (dx.ni * dx.nj));
   else
-    grad_tile<T, true, 1, B, B, WJ, 2>(dw, sa, sb, b % (dw.ni * dw.nj), b / (dw.ni * dw.nj));
+    grad_tile<T, true, 1, B, B, WJ, S>(dw, sa, sb, b % (dw.ni * dw.nj), b / (dw.ni * dw.nj));
 }
 template <class T>
 __global__ __launch_bounds__(512, 2) void linear_grad_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
@@ -582,6 +582,11 @@ template <class T>
 __global__ __launch_bounds__(256, 2) void linear_grad_small_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
   HOBFLOPS_STAGES2(128, 128);
   linear_grad_tiles<T, 128, 2>(dx, dw, parts, sa, sb);
+}
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_grad_deep_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
+  HOBFLOPS_STAGES4(128, 128);
+  linear_grad_tiles<T, 128, 4>(dx, dw, parts, sa, sb);
 }
 
 // What is left after the products, in one launch: the parts of dx and of dW joined in their order, 4 values a thread, and
@@ -636,27 +641,39 @@ struct Kind {
   double step, lead;
 };
 constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}};
-constexpr int kForwardKinds = 4, kGradKinds = 2;
+constexpr int kForwardKinds = 4, kGradKinds = 3;
 struct Tiling {
   int kind, splits;
-  double us;
+  int64_t groups;           // workgroups
+  double each, join, us;    // the time of a workgroup, of the parts, of all
 };
 constexpr int kMostSplits = 32;
-Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int kinds) {
+// The best of kinds first, .. last - 1.
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last) {
   const int64_t steps = (K + kStepK - 1) / kStepK;
-  Tiling best{0, 1, -1.0};
-  for (int k = 0; k < kinds; ++k) {
+  Tiling best{first, 1, 0, 0.0, 0.0, -1.0};
+  for (int k = first; k < last; ++k) {
     const Kind& kind = kKinds[k];
     const int64_t slots = kind.per_cu * kCUs;
     const int64_t tiles = ((rows + kind.rows - 1) / kind.rows) * ((cols + kind.cols - 1) / kind.cols);
     for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); ++n) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
-      double us = rounds * ((double)((steps + n - 1) / n) + kind.lead) * kind.step;
-      if (n > 1) us += 4.0 + (double)(2 * n) * rows * cols * 4.0 / 4e6;
-      if (best.us < 0.0 || us < best.us) best = Tiling{k, n, us};
+      const double each = ((double)((steps + n - 1) / n) + kind.lead) * kind.step;
+      const double join = n > 1 ? 4.0 + (double)(2 * n) * rows * cols * 4.0 / 4e6 : 0.0;
+      const double us = rounds * each + join;
+      if (best.us < 0.0 || us < best.us) best = Tiling{k, n, tiles * n, each, join, us};
     }
   }
   return best;
+}
+// Of one launch with a's workgroups and then b's, of one kind: b's begin where a's leave CUs idle.
+double pair_us(const Tiling& a, const Tiling& b) {
+  const int64_t slots = kKinds[a.kind].per_cu * kCUs, rounds = (a.groups + slots - 1) / slots;
+  const int64_t beside = (rounds * slots - a.groups) * (a.each > b.each ? (int64_t)(a.each / b.each) : 1);
+  const int64_t left = b.groups > beside ? b.groups - beside : 0;
+  const double t = (double)rounds * a.each + (double)((left + slots - 1) / slots) * b.each;
+  const double alone = (double)(rounds - 1) * a.each + b.each;
+  return (t > alone ? t : alone) + a.join + b.join;
 }
 // The tile of direct_kernel in 16 rows of W and 16 tokens, by an estimate: rounds of workgroups, one on each CU, which
 // read their rows at 100 bytes a nanosecond, and start and end, the longer the larger the tile. Measured, us, in the order
@@ -694,13 +711,13 @@ int64_t splits_of(int64_t K, int splits, int64_t* per) {
 
 struct ForwardPlan {
   int64_t x = -1, w = -1, part = -1, bytes = 0;
-  Tiling tiles{0, 1, 0.0};
+  Tiling tiles{0, 1};
   int direct = -1;  // of kDirect
 };
 ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
   const int64_t Kp = round_up(d.K, 8);
-  p.tiles = plan_tiles(d.N, d.T, d.K, kForwardKinds);
+  p.tiles = plan_tiles(d.N, d.T, d.K, 0, kForwardKinds);
   double us = p.tiles.us + (p.tiles.splits > 1 ? 4.0 : 0.0), direct = 0.0;  // (the second launch's start)
   // (rows that are not in place are copied in a launch of their own first)
   if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
@@ -720,7 +737,7 @@ struct BackwardPlan {
   int64_t x = -1, w = -1, dz = -1, db = -1, part_x = -1, part_w = -1, bytes = 0;
   int64_t Kp, Np;
   uint32_t parts = 1;  // of db
-  Tiling dx{0, 1, 0.0}, dw{0, 1, 0.0};
+  Tiling dx{0, 1}, dw{0, 1};
 };
 // need: the gradients asked for
 BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need) {
@@ -732,14 +749,23 @@ BackwardPlan plan_backward(const hobflops_linear_desc& d, const LinearNeed& need
   if (products && (d.act != kNoAct || !in_place(d.N, d.ldy, d.align))) p.dz = take(&p.bytes, d.T * p.Np * 2);
   if (need.dw && !in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * p.Kp * 2);
   if (need.dx && !in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * p.Kp * 2);
-  if (need.dx) {
-    p.dx = plan_tiles(d.T, d.K, p.Np, kGradKinds);
-    if (p.dx.splits > 1) p.part_x = take(&p.bytes, p.dx.splits * d.T * round_up(d.K, 4) * 4);
+  if (need.dx) p.dx = plan_tiles(d.T, d.K, p.Np, 0, kGradKinds);
+  if (need.dw) p.dw = plan_tiles(d.N, d.K, d.T, 0, kGradKinds);
+  if (need.dx && need.dw) {
+    // the kinds that are best alone, a launch each, or one kind and launch for both (77 x 1022 -> 2731: 3 us less)
+    double us = p.dx.us + p.dw.us + 3.0;
+    if (p.dx.kind == p.dw.kind) us = pair_us(p.dx, p.dw);
+    for (int k = 0; k < kGradKinds; ++k) {
+      const Tiling a = plan_tiles(d.T, d.K, p.Np, k, k + 1), b = plan_tiles(d.N, d.K, d.T, k, k + 1);
+      const double t = pair_us(a, b);
+      if (t >= us) continue;
+      us = t;
+      p.dx = a;
+      p.dw = b;
+    }
   }
-  if (need.dw) {
-    p.dw = plan_tiles(d.N, d.K, d.T, kGradKinds);
-    if (p.dw.splits > 1) p.part_w = take(&p.bytes, p.dw.splits * d.N * round_up(d.K, 4) * 4);
-  }
+  if (need.dx && p.dx.splits > 1) p.part_x = take(&p.bytes, p.dx.splits * d.T * round_up(d.K, 4) * 4);
+  if (need.dw && p.dw.splits > 1) p.part_w = take(&p.bytes, p.dw.splits * d.N * round_up(d.K, 4) * 4);
   const int64_t strips = (d.N + 255) / 256, most = (d.T + 7) / 8, wanted = (2048 + strips - 1) / strips;
   p.parts = (uint32_t)(most < wanted ? most : wanted);
   if (need.db) p.db = take(&p.bytes, (int64_t)p.parts * p.Np * 4);
@@ -825,10 +851,11 @@ uint32_t count_tiles(GradArgs& p, const Tiling& t) {
 template <class T>
 void grad_products(const GradArgs& dx, uint32_t parts, const GradArgs& dw, uint32_t tiles, int kind, hipStream_t s) {
   if (parts + tiles == 0) return;
-  if (kind)
-    linear_grad_small_kernel<T><<<parts + tiles, 256, 0, s>>>(dx, dw, parts);
-  else
-    linear_grad_kernel<T><<<parts + tiles, 512, 0, s>>>(dx, dw, parts);
+  switch (kind) {
+    case 0: linear_grad_kernel<T><<<parts + tiles, 512, 0, s>>>(dx, dw, parts); break;
+    case 1: linear_grad_small_kernel<T><<<parts + tiles, 256, 0, s>>>(dx, dw, parts); break;
+    default: linear_grad_deep_kernel<T><<<parts + tiles, 512, 0, s>>>(dx, dw, parts);
+  }
 }
 
 template <class T>
