@@ -680,11 +680,14 @@ double pair_us(const Tiling& a, const Tiling& b) {
 // of kDirect, and in tiles through LDS: 16 x 4096 -> 4096 8.5, 9.3, 10.7, 9.6, 12.0, 18.1, LDS 15.3; 64 x 4096 -> 4096
 // 19.0, 15.5, 12.1, 10.7, 13.5, 18.4, LDS 17.3; 333 x 2730 -> 1000 24.5, 20.6, 19.2, 16.8, 13.0, 18.6, LDS 24.2;
 // 1024 x 1024 -> 1024 33, 29, 19, 16, 13, 9.4, LDS 14.0; 2048 x 512 -> 1408 77, 66, 25, 38, 22, 18, LDS 10.0.
+// Rows that do not begin on lines of 128 bytes take a third more, rows at odd values twice as long (333 x 8192 -> 1000: 21,
+// of 8200 values 26, of 8193 37).
+double row_factor(int64_t ld, int align) { return ld % 2 != 0 || align == 2 ? 2.0 : ld % 64 != 0 ? 1.33 : 1.0; }
 struct Direct {
   int ni, nj;
 };
 constexpr Direct kDirect[] = {{1, 1}, {1, 2}, {1, 4}, {2, 2}, {2, 4}, {4, 4}};
-int plan_direct(int64_t N, int64_t T, int64_t K, double* us) {
+int plan_direct(int64_t N, int64_t T, int64_t K, double factor, double* us) {
   int best = 0;
   *us = -1.0;
   for (int i = 0; i < 6; ++i) {
@@ -692,7 +695,7 @@ int plan_direct(int64_t N, int64_t T, int64_t K, double* us) {
     if (d.nj > 1 && T <= 8 * d.nj) continue;  // more than half of the tokens would be nobody's
     const int64_t groups = ((N + 16 * d.ni - 1) / (16 * d.ni)) * ((T + 16 * d.nj - 1) / (16 * d.nj));
     const double rounds = (double)((groups + kCUs - 1) / kCUs);
-    const double t = rounds * ((double)(16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0 + 0.18 * d.ni * d.nj) + 3.0;
+    const double t = rounds * (factor * (16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0 + 0.18 * d.ni * d.nj) + 3.0;
     if (*us < 0.0 || t < *us) {
       *us = t;
       best = i;
@@ -722,7 +725,8 @@ ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   // (rows that are not in place are copied in a launch of their own first)
   if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
     us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
-  const int i = plan_direct(d.N, d.T, d.K, &direct);
+  const double x = row_factor(d.ldx, d.align), w = row_factor(d.ldw, d.align);
+  const int i = plan_direct(d.N, d.T, d.K, x > w ? x : w, &direct);
   if (direct < us) {
     p.direct = i;
     return p;
