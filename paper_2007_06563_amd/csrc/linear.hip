@@ -99,7 +99,8 @@ struct LinearArgs {
   void *y, *z;
   float* part;  // with splits: [splits][T][N rounded up to 4]
   int64_t ldw, ldx, ldr, ldy, T_, N, K, per;  // z: rows N apart; per: k of a split, a multiple of 64
-  int act;
+  // (tiles through LDS: K without its last K % 8, which `tail` is)
+  int act, tail;
   uint32_t ni, nj;
 };
 
@@ -240,6 +241,26 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
 }
 #endif
 
+// A fragment of the last K % 8 values of 16 rows, and zeros: the lanes of the first 8 k have them.
+template <class T>
+__device__ __forceinline__ typename T::vec8 tail_of(const void* p, int64_t ld, int64_t rows, int64_t row0, int64_t K, int tail,
+                                                    int lane) {
+  u32x4v v = {0, 0, 0, 0};
+  if (lane < 16) {
+    const int64_t r = row0 + lane < rows ? row0 + lane : rows - 1;  // (sums of rows beyond the end: nobody stores them)
+    const uint16_t* end = (const uint16_t*)p + r * ld + K + tail;
+    if (K > 0) {
+      __builtin_memcpy(&v, end - 8, 16);
+      v = shifted_down(v, (uint32_t)(8 - tail) * 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 7; ++j)
+        if (j < tail) v[j >> 1] |= (uint32_t)(end - tail)[j] << (16 * (j & 1));
+    }
+  }
+  return __builtin_bit_cast(typename T::vec8, v);
+}
+
 template <class T, int BI, int BJ, int WI, int WJ, int S>
 __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const (&sa)[S],
                                             uint8_t* const (&sb)[S]) {
@@ -266,6 +287,17 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const 
   typename T::vec8 more[kPassesOf<NI>] = {};
   load_residual<T, NI>(p, f0, t0, lane, more);
   f32x4 acc[NI][NJ] = {};
+  if (p.tail && split == 0) {
+    typename T::vec8 b[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) b[j] = tail_of<T>(p.x, p.ldx, p.T_, t0 + 16 * j, p.K, p.tail, lane);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const typename T::vec8 a = tail_of<T>(p.w, p.ldw, p.N, f0 + 16 * i, p.K, p.tail, lane);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(a, b[j], acc[i][j]);
+    }
+  }
   const auto load = [&](int s) {
     la.load(sa[s], wave);
     lb.load(sb[s], wave);
@@ -717,13 +749,15 @@ struct ForwardPlan {
   Tiling tiles{0, 1};
   int direct = -1;  // of kDirect
 };
+// Rows that the forward product reads in place: loads of 16 bytes into LDS need addresses of whole words.
+bool words(int64_t ld, int align) { return align >= 4 && ld % 2 == 0 && ld < (int64_t)1 << 21; }
 ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
   const int64_t Kp = round_up(d.K, 8);
   p.tiles = plan_tiles(d.N, d.T, d.K, 0, kForwardKinds);
   double us = p.tiles.us + (p.tiles.splits > 1 ? 4.0 : 0.0), direct = 0.0;  // (the second launch's start)
   // (rows that are not in place are copied in a launch of their own first)
-  if (!in_place(d.K, d.ldx, d.align) || !in_place(d.K, d.ldw, d.align))
+  if (!words(d.ldx, d.align) || !words(d.ldw, d.align))
     us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
   const double x = row_factor(d.ldx, d.align), w = row_factor(d.ldw, d.align);
   const int i = plan_direct(d.N, d.T, d.K, x > w ? x : w, &direct);
@@ -731,8 +765,8 @@ ForwardPlan plan_forward(const hobflops_linear_desc& d) {
     p.direct = i;
     return p;
   }
-  if (!in_place(d.K, d.ldx, d.align)) p.x = take(&p.bytes, d.T * Kp * 2);
-  if (!in_place(d.K, d.ldw, d.align)) p.w = take(&p.bytes, d.N * Kp * 2);
+  if (!words(d.ldx, d.align)) p.x = take(&p.bytes, d.T * Kp * 2);
+  if (!words(d.ldw, d.align)) p.w = take(&p.bytes, d.N * Kp * 2);
   if (p.tiles.splits > 1) p.part = take(&p.bytes, p.tiles.splits * d.T * round_up(d.N, 4) * 4);
   return p;
 }
@@ -829,7 +863,9 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   align_rows<T>(align, s);
   // (rows that were copied have zeros up to the multiple of 8)
   if (plan.x >= 0 && plan.w >= 0) p.K = align.ldd;
-  const int64_t splits = splits_of(p.K, plan.tiles.splits, &p.per);
+  p.tail = (int)(p.K % 8);
+  p.K -= p.tail;
+  const int64_t splits = splits_of(p.K > 0 ? p.K : 1, plan.tiles.splits, &p.per);
   if (splits > 1) p.part = (float*)(ws + plan.part);
   const Kind& kind = kKinds[plan.tiles.kind];
   p.ni = (uint32_t)((d.N + kind.rows - 1) / kind.rows);

@@ -142,6 +142,21 @@ def test_a_workgroup_a_cu(T, K, N, dtype, act, bias, res):
     _backward(hf, xs, ws, z, T, K, N, dtype, act, lds, 0)
 
 
+@pytest.mark.parametrize("T,K,N,lds,off", [(1000, 1026, 4000, None, 0), (2100, 4, 5000, None, 0), (4100, 70, 4100, None, 0),
+                                           (300, 1998, 1030, None, 0), (520, 16414, 264, None, 0),
+                                           (600, 2046, 1100, (2050, 2060, 1100, 1101), 2), (600, 2046, 1100, (2051, 2046, 1100, 1100), 0),
+                                           (600, 2046, 1100, (2046, 2047, 1100, 1100), 0), (3000, 7, 3000, (8, 12, 3000, 3000), 0),
+                                           (600, 2040, 1100, (2042, 2046, 1100, 1100), 6)])
+@pytest.mark.parametrize("dtype,act", [("bf16", 1), ("f16", None)])
+def test_rows_of_words_in_tiles(T, K, N, lds, off, dtype, act):
+    """K that is no multiple of 8, rows and tensors at whole words but not at 16 bytes, one operand copied and one not."""
+    hf = need_gpu()
+    say("linear words", T, K, N, lds, off, dtype, act)
+    lds = lds or (K, K, N, N)
+    xs, ws, z = _forward(hf, T, K, N, dtype, act, True, True, lds, off)
+    _backward(hf, xs, ws, z, T, K, N, dtype, act, lds, off)
+
+
 @pytest.mark.parametrize("T,K,N", [(1, 64, 40), (9, 1000, 300), (40, 264, 100), (300, 520, 520), (20, 8192, 64)])
 @pytest.mark.parametrize("act", [None, 0])
 def test_the_residual_may_be_the_output(T, K, N, act):
