@@ -10,10 +10,10 @@
 // the end of its last group, hold zeros. A thread's 16 bytes make whole lines a wave
 // and leave enough waves to keep HBM busy without a loop.
 //
-// Measured: 16384 x 4096 bfloat16 in 8 bits: pack 42 us, unpack 39 us, 4.9 and 5.2 TB/s of
+// Measured: 16384 x 4096 bfloat16 in 8 bits: pack 42 us, unpack 33 us, 4.9 and 6.1 TB/s of
 // what they read and write (a large copy: 5.1); 4097 x 2731 float32, rows 5 values
-// apart and no row aligned: 11 us and 16 us; one row of 4096: 2.5 us, a launch. In 4 bits, groups of 32:
-// pack 71 to 75 us (33 at a copy's rate), bound by a division a value, unpack 40 to 42 to 16 bits, 50 under
+// apart and no row aligned: 11 us and 15 us; one row of 4096: 2.5 us, a launch. In 4 bits, groups of 32:
+// pack 70 to 75 us (33 at a copy's rate), bound by a division a value, unpack 35 to 16 bits, 46 under
 // float32 scales (round_wide_product), 83 to 94 to float32 (60 at a copy's rate).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -193,10 +193,15 @@ __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
       typename T::elem e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = round(v[j]);
-      u32x4v w[sizeof e / 16];
-      __builtin_memcpy(w, e, sizeof e);
-#pragma unroll
-      for (int i = 0; i < (int)(sizeof e / 16); ++i) stream16((u32x4v*)dst + i, w[i]);
+      // (whole lines a wave go past the caches, 16384 x 4096: 33 us instead of 50; of float32 a lane's 32 bytes are two
+      // stores of half lines, which took 4 to 7 % longer in that way)
+      if constexpr (sizeof e == 16) {
+        u32x4v w;
+        __builtin_memcpy(&w, e, 16);
+        stream16(dst, w);
+      } else {
+        __builtin_memcpy(dst, e, sizeof e);
+      }
     } else {
       for (int j = 0; j < 8 && col + j < p.cols; ++j) dst[j] = round(v[j]);
     }
