@@ -34,6 +34,7 @@ struct BlockParams {
   int64_t rows, cols, ld, row_bytes;  // row_bytes: codes of a row
   int64_t chunks;                     // threads a row: whole groups
   int group_log, scale;
+  bool past;  // unpacked values go past the caches
 };
 
 template <class T>
@@ -193,12 +194,12 @@ __global__ __launch_bounds__(kThreads) void block_unpack_kernel(BlockParams p) {
       typename T::elem e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = round(v[j]);
-      // (whole lines a wave go past the caches, 16384 x 4096: 33 us instead of 50; of float32 a lane's 32 bytes are two
-      // stores of half lines, which took 4 to 7 % longer in that way)
+      // (16384 x 4096 past the caches: 33 us instead of 50; of float32 a lane's 32 bytes are two stores of half lines, which
+      // took 4 to 7 % longer in that way)
       if constexpr (sizeof e == 16) {
         u32x4v w;
         __builtin_memcpy(&w, e, 16);
-        stream16(dst, w);
+        store16(dst, w, p.past);
       } else {
         __builtin_memcpy(dst, e, sizeof e);
       }
@@ -256,6 +257,7 @@ hipError_t run(const BlockTensor& t, int fmt, bool pack, hipStream_t stream) {
   p.group_log = t.group == 32 ? 5 : t.group == 64 ? 6 : 7;
   p.chunks = (t.cols + t.group - 1) / t.group * (t.group / kPer);
   p.scale = t.scale;
+  p.past = past_caches(t.rows * t.cols * 2);
   if (t.type == HOBFLOPS_TYPE_F32) launch_fmt<TypeF32>(p, fmt, pack, stream);
   if (t.type == HOBFLOPS_TYPE_BF16) launch_fmt<TypeBF16>(p, fmt, pack, stream);
   if (t.type == HOBFLOPS_TYPE_F16) launch_fmt<TypeF16>(p, fmt, pack, stream);

@@ -101,6 +101,7 @@ struct LinearArgs {
   int64_t ldw, ldx, ldr, ldy, T_, N, K, per;  // z: rows N apart; per: k of a split, a multiple of 64
   // (tiles through LDS: K without its last K % 8, which `tail` is)
   int act, tail;
+  bool past;  // y and z go past the caches
   uint32_t ni, nj;
 };
 
@@ -180,7 +181,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs& p, const f32x4 (&ac
   };
   const auto store8 = [&](E* row, const Vec& v) {
     if (whole) {
-      stream16(row + f, __builtin_bit_cast(u32x4v, v));
+      store16(row + f, __builtin_bit_cast(u32x4v, v), p.past);
     } else {
 #pragma unroll
       for (int k = 0; k < 7; ++k)
@@ -834,6 +835,7 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   p.N = d.N;
   p.K = d.K;
   p.act = d.act;
+  p.past = past_caches(d.T * d.N * 2);
   const ForwardPlan plan = plan_forward(d);
   if (plan.direct >= 0) {
     switch (plan.direct) {

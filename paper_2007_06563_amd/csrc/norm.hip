@@ -28,6 +28,7 @@ struct NormArgs {
   float *mean, *rstd, *part;  // part: [parts][2][cols]
   int64_t rows, cols, ldx, ldy, ld_add;  // ldy: of y or of dy
   float eps;
+  bool past;  // y or dx goes past the caches
 };
 
 // A thread's values at a time: 16 bytes.
@@ -84,13 +85,13 @@ struct Chunk {
     __builtin_memcpy(&w, (const typename T::elem*)row + at, 16);
     return w;
   }
-  __device__ __forceinline__ void store(void* row, const float (&v)[kVec<T>]) const {
+  __device__ __forceinline__ void store(void* row, const float (&v)[kVec<T>], bool past) const {
     typename T::elem e[kVec<T>];
 #pragma unroll
     for (int j = 0; j < kVec<T>; ++j) e[j] = (typename T::elem)v[j];
     u32x4v w;
     __builtin_memcpy(&w, e, 16);
-    if (there) stream16((typename T::elem*)row + at, w);
+    if (there) store16((typename T::elem*)row + at, w, past);
   }
 };
 // Values of a chunk as they count for sums.
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
       for (int j = 0; j < V; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c][j] + b[c][j];
-      chunk[c].store((E*)p.y + row * p.ldy, x[c]);
+      chunk[c].store((E*)p.y + row * p.ldy, x[c], p.past);
     }
   }
 }
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
         v[j] = r * (g * wc[j] - s.x - xh * s.y);
         if (p.add) v[j] += value_of<T>(ae[c], j);
       }
-      chunk[c].store((E*)p.dx + row * p.cols, v);
+      chunk[c].store((E*)p.dx + row * p.cols, v, p.past);
     }
   }
   if (!p.part) return;
@@ -651,6 +652,7 @@ hipError_t run(const LayerNorm& c, bool grad, hipStream_t s) {
   p.ldy = c.ldy;
   p.ld_add = c.ld_add;
   p.eps = (float)c.eps;
+  p.past = past_caches(c.rows * c.cols * (c.type == HOBFLOPS_TYPE_F32 ? 4 : 2));
   if (c.type == HOBFLOPS_TYPE_F32) run_type<TypeF32>(c, p, grad, s);
   if (c.type == HOBFLOPS_TYPE_BF16) run_type<TypeBF16>(c, p, grad, s);
   if (c.type == HOBFLOPS_TYPE_F16) run_type<TypeF16>(c, p, grad, s);
