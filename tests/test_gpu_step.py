@@ -247,3 +247,25 @@ def test_columns_of_one_matrix():
                 hf.linear(x, w, out=out)
         with pytest.raises(hf.HobflopsError):
             hf.layer_norm(x, out=both[:, 131:263])
+
+
+def test_results_of_more_than_the_caches():
+    """Results from 64 MiB on are stored in another way: the same values as of parts of the rows."""
+    hf = need_gpu()
+    say("results past the caches")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rows, cols = 8200, 4103
+    x = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
+    w = torch.randn(cols, 72, generator=g, device="cuda").bfloat16()
+    codes = hf.block_pack(x, (4, 3))
+    parts = [slice(0, 4100), slice(4100, rows)]
+    y, saved = hf.layer_norm(x, save=True)
+    dx = hf.layer_norm_backward(x, y, saved, add=x)[0]
+    up = hf.block_unpack(*codes, cols, (4, 3), dtype=torch.bfloat16)
+    out, z = hf.linear(y[:, :72].contiguous(), w, None, hf.GATE_RELU, residual=x, save=True)
+    for p in parts:
+        assert torch.equal(y[p], hf.layer_norm(x[p]))
+        assert torch.equal(dx[p], hf.layer_norm_backward(x[p], y[p], hf.NormSaved(saved.mean[p], saved.rstd[p]), add=x[p])[0])
+        assert torch.equal(up[p], hf.block_unpack(codes[0][p], codes[1][p], cols, (4, 3), dtype=torch.bfloat16))
+        some = hf.linear(y[p, :72].contiguous(), w, None, hf.GATE_RELU, residual=x[p], save=True)
+        assert torch.equal(out[p], some[0]) and torch.equal(z[p], some[1])
