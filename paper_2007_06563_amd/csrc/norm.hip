@@ -9,6 +9,10 @@
 //
 // The sums over rows: a workgroup takes many rows and keeps its part of dw and db in registers; a second
 // launch adds the parts in their order (no atomics: the same inputs give the same bits).
+//
+// Measured: 16384 x 4096 bfloat16 forward 46 to 51 us (5.3 to 5.9 TB/s of what it must read and write), backward with a
+// gradient to add 94 (5.7) and 5.4 for the parts (25 MB of them); 4097 x 2731 float32 in rows that begin anywhere 22 (4.1), 24.3
+// (5.5) and 4.0; one row of 4096 3.1, of which the work is one load's latency and two sums'. A large copy: 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -276,7 +280,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
 }
 
 // As norm_kernel; a lane also keeps its columns' parts of dw and db. Sixteen waves with four times 16 bytes a lane have
-// registers for neither the next row nor the weights, which come from L2 for each row.
+// registers for neither the next row nor the weights, which come from L2 for each row (2048 x 16384 float32: 137 us, 2.9 TB/s).
 template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
@@ -404,7 +408,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
   }
 }
 
-// Rows of more than 32 KB (float32: 64), or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the first).
+// Rows of more than 32 KB (float32: 64), or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the
+// first), at less than a third of the others' rate: 4096 x 16392 bfloat16 forward 155 us, backward 303.
 constexpr int kWide = 16;  // waves
 
 template <class T, class Each>

@@ -895,7 +895,8 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
     copies: bfloat16 or float16 tensors that receive the new weights too (None entries: none). grad_scale: a factor of
     the gradients. seed: of the rounding of 8-bit states (the random numbers depend on it, the step and a
     value's place). lr, step (int64) and grad_scale (else float32) may be GPU tensors of one value; skip, a
-    float32 one: where it is not 0 nothing changes."""
+    float32 one: where it is not 0 nothing changes. In a captured graph numbers are those of the capture: a step or rate
+    that moves on is such a tensor there, as is the step of 8-bit states, whose rounding it sets."""
     if len(params) != len(grads) or (copies is not None and len(copies) != len(params)):
         raise ValueError("adamw: params, grads and copies must be as many")
     if not params:
