@@ -210,7 +210,8 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
 }
 
 // A wave, or the NW waves of a workgroup, has a row, a lane NC times 16 bytes of it; the next row is under way
-// while a row's sums meet.
+// while a row's sums meet. 32 values a lane leave no registers for w and b, which come from L2 for each
+// row (4096 x 16392 bfloat16: 110 us, walked 155).
 template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs p) {
   typedef typename T::elem E;
@@ -229,9 +230,12 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
     for (int c = 0; c < NC; ++c) next[c] = chunk[c].load((const E*)p.x + row * p.ldx);
   };
   load(row);
-  float w[NC][V], b[NC][V];
-  load_columns<T, W>(p.w, chunk, 1.0f, w);
-  load_columns<T, W>(p.b, chunk, 0.0f, b);
+  constexpr bool kHeld = NC * V < 32;  // w and b
+  float w[kHeld ? NC : 1][V], b[kHeld ? NC : 1][V];
+  if constexpr (kHeld) {
+    load_columns<T, W>(p.w, chunk, 1.0f, w);
+    load_columns<T, W>(p.b, chunk, 0.0f, b);
+  }
   for (; row < p.rows; row += stride) {
     float x[NC][V];
 #pragma unroll
@@ -272,20 +276,27 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      constexpr int kStep = kHeld ? 1 : 0;
+      if constexpr (!kHeld) {
+        const Chunk<T> one[1] = {chunk[c]};
+        load_columns<T, W>(p.w, one, 1.0f, w);
+        load_columns<T, W>(p.b, one, 0.0f, b);
+      }
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c][j] + b[c][j];
+      for (int j = 0; j < V; ++j) x[c][j] = (x[c][j] - s.off) * s.rstd * w[c * kStep][j] + b[c * kStep][j];
       chunk[c].store((E*)p.y + row * p.ldy, x[c], p.past);
     }
   }
 }
 
-// As norm_kernel; a lane also keeps its columns' parts of dw and db. Sixteen waves with four times 16 bytes a lane have
+// As norm_kernel; a lane also keeps its columns' parts of dw and db, but where it has 32 values (norm_columns_kernel reads x and
+// dy again there: 4096 x 16392 bfloat16: 161 us, walked 303). Sixteen waves with four times 16 bytes a lane have
 // registers for neither the next row nor the weights, which come from L2 for each row (2048 x 16384 float32: 137 us, 2.9 TB/s).
 template <class T, class W, int NW, int NC>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
   constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;
-  constexpr bool kAhead = NW * NC < 64;
+  constexpr bool kAhead = NW * NC < 64, kSums = NC * V < 32;
   __shared__ float2 lds[2 * NW];
   const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t stride = (int64_t)gridDim.x * kRows;
@@ -310,7 +321,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     }
   };
   if (kAhead && first < p.rows) load(first);
-  float w[kAhead ? NC : 1][V], dw[NC][V] = {}, db[NC][V] = {};
+  float w[kAhead ? NC : 1][V], dw[kSums ? NC : 1][V] = {}, db[kSums ? NC : 1][V] = {};
   if constexpr (kAhead) load_columns<T, W>(p.w, chunk, 1.0f, w);
   const auto weights = [&](int c) -> const float(&)[V] {
     if constexpr (kAhead) {
@@ -362,15 +373,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
       for (int j = 0; j < V; ++j) {
         const float g = value_of<T>(ge[c], j);
         const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
-        dw[c][j] += g * xh;
-        db[c][j] += g;
+        if constexpr (kSums) {
+          dw[c][j] += g * xh;
+          db[c][j] += g;
+        }
         v[j] = r * (g * wc[j] - s.x - xh * s.y);
         if (p.add) v[j] += value_of<T>(ae[c], j);
       }
       chunk[c].store((E*)p.dx + row * p.cols, v, p.past);
     }
   }
-  if (!p.part) return;
+  if (!kSums || !p.part) return;
   if constexpr (NW == 1) {
     // the four waves' parts as one, wave after wave
     __shared__ float sums[2][NC][V][64];
@@ -397,19 +410,20 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
       __syncthreads();
     }
   }
+  if constexpr (!kSums) return;
   if (NW > 1 || threadIdx.x < 64) {
     float* to = p.part + (int64_t)blockIdx.x * 2 * p.cols;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
       if (chunk[c].there) {
-        __builtin_memcpy(to + chunk[c].at, dw[c], 4 * V);
-        __builtin_memcpy(to + p.cols + chunk[c].at, db[c], 4 * V);
+        __builtin_memcpy(to + chunk[c].at, dw[kSums ? c : 0], 4 * V);
+        __builtin_memcpy(to + p.cols + chunk[c].at, db[kSums ? c : 0], 4 * V);
       }
   }
 }
 
-// Rows of more than 32 KB (float32: 64), or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the
-// first), at less than a third of the others' rate: 4096 x 16392 bfloat16 forward 155 us, backward 303.
+// Rows of more than 64 KB, or less than 16 bytes: a workgroup walks the row, three times over (from L2 after the
+// first), at a third of the others' rate.
 constexpr int kWide = 16;  // waves
 
 template <class T, class Each>
@@ -516,23 +530,49 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
   }
 }
 
-// The parts of dw and db of wide rows: 2048 columns and every gridDim.y-th row a workgroup.
+// The parts of dw and db of rows that nobody has in registers: 2048 columns and every gridDim.y-th row a workgroup.
 template <class T>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
   typedef typename T::elem E;
   const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (col >= p.cols) return;
   float dw[8] = {}, db[8] = {};
-  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
-    float x[8], g[8];
-    load_values<T, 8>((const E*)p.x + row * p.ldx, col, p.cols, x);
-    load_values<T, 8>((const E*)p.dy + row * p.ldy, col, p.cols, g);
+  const auto add = [&](const float (&x)[8], const float (&g)[8], int64_t row) {
     const float half = 0.5f * p.mean[row], twice = 2.0f * p.rstd[row];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       dw[j] += g[j] * (__builtin_fmaf(0.5f, x[j], -half) * twice);
       db[j] += g[j];
     }
+  };
+  int64_t row = blockIdx.y;
+  if (col + 8 <= p.cols) {
+    // four rows under way
+    for (; row + 3 * (int64_t)gridDim.y < p.rows; row += 4 * (int64_t)gridDim.y) {
+      E x[4][8], g[4][8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = row + i * (int64_t)gridDim.y;
+        __builtin_memcpy(x[i], (const E*)p.x + r * p.ldx + col, sizeof x[i]);
+        __builtin_memcpy(g[i], (const E*)p.dy + r * p.ldy + col, sizeof g[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8], d[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[j] = (float)x[i][j];
+          d[j] = (float)g[i][j];
+        }
+        add(v, d, row + i * (int64_t)gridDim.y);
+      }
+    }
+  }
+  for (; row < p.rows; row += gridDim.y) {
+    float x[8], g[8];
+    load_values<T, 8>((const E*)p.x + row * p.ldx, col, p.cols, x);
+    load_values<T, 8>((const E*)p.dy + row * p.ldy, col, p.cols, g);
+    add(x, g, row);
   }
   float* to = p.part + (int64_t)blockIdx.y * 2 * p.cols + col;
 #pragma unroll
@@ -543,7 +583,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
     }
 }
 
-// The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane (of float32 rows beyond 8192 four), the
+// The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane (beyond 32 KB four), the
 // more waves the longer it is. (Four a lane, 4097 x 2731 float32: backward 40 us, two waves on a SIMD; two a lane 28.)
 struct Shape {
   int waves;
@@ -556,8 +596,10 @@ int shape_of(int64_t cols, int type) {
   if (cols < (type == HOBFLOPS_TYPE_F32 ? 4 : 8)) return kWalk;  // (no whole 16 bytes)
   int i = 0;
   while (i < kWalk && chunks > kShapes[i].chunks) ++i;
-  return i == 6 && type != HOBFLOPS_TYPE_F32 ? kWalk : i;  // (32 values of 16 bits a lane: too many registers)
+  return i;
 }
+// Whether the sums over rows have a launch of their own.
+bool columns_apart(int shape, int type) { return shape == kWalk || (shape == 6 && type != HOBFLOPS_TYPE_F32); }
 // Backward, eight waves of 16-bit values, which are twice as many a lane, would be one workgroup on a CU, or two whose
 // registers spill (8192 x 8192 bfloat16: 226 us); sixteen waves with half of a lane's values take 96.
 bool wide_grad(int shape, int type) { return shape == 4 && type != HOBFLOPS_TYPE_F32; }
@@ -576,7 +618,7 @@ int64_t groups_of(int64_t rows, int64_t cols, int type, bool grad) {
 // The parts of the sums over rows: one a workgroup.
 constexpr int64_t kWideParts = 128;
 int64_t parts_of(int64_t rows, int64_t cols, int type) {
-  if (shape_of(cols, type) == kWalk) return rows < kWideParts ? rows : kWideParts;
+  if (columns_apart(shape_of(cols, type), type)) return rows < kWideParts ? rows : kWideParts;
   return groups_of(rows, cols, type, true);
 }
 
@@ -611,18 +653,19 @@ void launch_rows(const NormArgs& p, bool grad, hipStream_t s) {
       return launch<T, W, 8, 2>(p, grad, s);
     case 5: return launch<T, W, 16, 2>(p, grad, s);
     case 6:
-      if constexpr (kVec<T> == 4) return launch<T, W, 16, 4>(p, grad, s);
+      launch<T, W, 16, 4>(p, grad, s);
       break;
+    default: {
+      const unsigned grid = (unsigned)groups_of(p.rows, p.cols, kType<T>, grad);
+      if (grad)
+        norm_grad_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
+      else
+        norm_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
+    }
   }
-  const unsigned grid = (unsigned)groups_of(p.rows, p.cols, kType<T>, grad);
-  if (grad) {
-    norm_grad_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
-    if (p.part)
-      norm_columns_kernel<T><<<dim3((unsigned)((p.cols + 2047) / 2048), (unsigned)parts_of(p.rows, p.cols, kType<T>)), 256,
-                               0, s>>>(p);
-  } else {
-    norm_wide_kernel<T, W><<<grid, kWide * 64, 0, s>>>(p);
-  }
+  if (grad && p.part && columns_apart(shape_of(p.cols, kType<T>), kType<T>))
+    norm_columns_kernel<T><<<dim3((unsigned)((p.cols + 2047) / 2048), (unsigned)parts_of(p.rows, p.cols, kType<T>)), 256, 0,
+                             s>>>(p);
 }
 
 template <class T, class W>

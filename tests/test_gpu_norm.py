@@ -122,6 +122,30 @@ def test_more_rows_than_workgroups(rows, cols):
     _case(hf, rows, cols, "bf16", "f32")
 
 
+@pytest.mark.parametrize("rows,cols", [(5, 16385), (300, 17000), (3, 32768), (7, 32777), (4, 40001)])
+@pytest.mark.parametrize("dtype,wdtype", [("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+def test_wide_rows(rows, cols, dtype, wdtype):
+    """Four times 16 bytes a lane, and rows that are walked."""
+    hf = need_gpu()
+    say("norm wide", rows, cols, dtype, wdtype)
+    _case(hf, rows, cols, dtype, wdtype)
+    x, _ = _rows(rows, cols, dtype, 14, cols + 1, 1)
+    want = hf.layer_norm(x)
+    assert hf.layer_norm(x, out=x) is x and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("cols", [40, 20000, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_equal_wide_values(cols, dtype):
+    hf = need_gpu()
+    x = torch.full((3, cols), 2.0 ** 120, device="cuda").to(TYPES[dtype])
+    x[1] = 0.0
+    y, saved = hf.layer_norm(x, save=True)
+    assert (y == 0).all() and saved.rstd.isfinite().all()
+    dx, dw, db = hf.layer_norm_backward(torch.ones_like(x), x, saved)
+    assert (dx == 0).all() and (dw == 0).all() and (db == 3).all()
+
+
 @pytest.mark.parametrize("cols", [96, 1536, 4096, 20000])
 def test_rows_far_from_zero(cols):
     """A mean a thousand times the deviation: what float32 holds of the differences is there."""
