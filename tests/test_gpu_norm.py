@@ -134,6 +134,36 @@ def test_wide_rows(rows, cols, dtype, wdtype):
     assert hf.layer_norm(x, out=x) is x and torch.equal(x, want)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 2), (700, 3), (300000, 3), (262145, 5), (1000, 7), (64, 6)])
+@pytest.mark.parametrize("dtype,wdtype", [("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+def test_rows_of_a_few_values(rows, cols, dtype, wdtype):
+    hf = need_gpu()
+    say("norm few", rows, cols, dtype, wdtype)
+    _case(hf, rows, cols, dtype, wdtype, cols + 2, 1)
+    x, _ = _rows(rows, cols, dtype, 15)
+    want = hf.layer_norm(x)
+    assert hf.layer_norm(x, out=x) is x and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("cols", [1, 2, 3, 7])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_few_large_and_odd_values(cols, dtype):
+    hf = need_gpu()
+    x, _ = _rows(6, cols, dtype, 16)
+    x[1] *= 2.0 ** 100
+    x[3, 0] = float("inf")
+    x[4, cols - 1] = float("nan")
+    base = x.clone()
+    base[1] *= 2.0 ** -100
+    y, saved = hf.layer_norm(x, eps=0.0 if cols > 1 else 1e-5, save=True)
+    z = hf.layer_norm(base, eps=0.0 if cols > 1 else 1e-5)
+    assert y[3].isnan().all() and y[4].isnan().all()
+    for row in (0, 1, 2, 5):
+        # (the quotient of two roundings' neighbours: a few steps)
+        assert torch.allclose(y[row].double(), z[row].double(), rtol=0, atol=8 * ref.HALF[dtype])
+    assert saved.rstd[1].isfinite() and saved.mean[1].isfinite()
+
+
 @pytest.mark.parametrize("cols", [40, 20000, 40000])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_equal_wide_values(cols, dtype):
