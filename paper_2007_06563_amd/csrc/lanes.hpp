@@ -69,20 +69,29 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   return max(a, b);
 }
 
-// The sum of the wave's x, the same in every lane.
-__device__ __forceinline__ float wave_sum(float x) {
+// The sum of x over each L lanes, 4 to 64, the same in all of them.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
 #define HOBFLOPS_ADD(S) x += __uint_as_float(row_xor<S>(__float_as_uint(x)))
-  HOBFLOPS_ADD(0);
-  HOBFLOPS_ADD(1);
+  if constexpr (L >= 16) HOBFLOPS_ADD(0);
+  if constexpr (L >= 8) HOBFLOPS_ADD(1);
   HOBFLOPS_ADD(2);
   HOBFLOPS_ADD(3);
 #undef HOBFLOPS_ADD
-  const uint32_t a = __float_as_uint(x);
-  const auto s = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  const uint32_t b = __float_as_uint(__uint_as_float(s[0]) + __uint_as_float(s[1]));
-  const auto t = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+  if constexpr (L >= 32) {
+    const uint32_t a = __float_as_uint(x);
+    const auto s = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    x = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  if constexpr (L >= 64) {
+    const uint32_t b = __float_as_uint(x);
+    const auto t = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    x = __uint_as_float(t[0]) + __uint_as_float(t[1]);
+  }
+  return x;
 }
+// The sum of the wave's x, the same in every lane.
+__device__ __forceinline__ float wave_sum(float x) { return lanes_sum<64>(x); }
 
 // The stages d = 8, 4, 2, 1 on N words.
 template <int N>

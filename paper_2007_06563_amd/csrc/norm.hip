@@ -131,10 +131,10 @@ __device__ __forceinline__ void load_columns(const void* p, const Chunk<T> (&chu
 // Sums (or largest values) of a row over its NW waves, the same in every thread; the waves' shares meet in LDS, in one of
 // two places, so that one barrier a sum is enough: who writes a place again has passed the barrier of
 // the other one, which stands behind all reads of the first.
-template <int NW>
+template <int NW, int L = 64>
 __device__ __forceinline__ float2 row_sums(float2 v, float2* lds, int place) {
-  v.x = wave_sum(v.x);
-  v.y = wave_sum(v.y);
+  v.x = lanes_sum<L>(v.x);
+  v.y = lanes_sum<L>(v.y);
   if constexpr (NW > 1) {
     float2* s = lds + place * NW;
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
@@ -148,10 +148,10 @@ __device__ __forceinline__ float2 row_sums(float2 v, float2* lds, int place) {
   }
   return v;
 }
-template <int NW>
+template <int NW, int L = 64>
 __device__ __forceinline__ float row_max(float v, float2* lds) {
 #pragma unroll
-  for (int m = 32; m > 0; m >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, m));
+  for (int m = L / 2; m > 0; m >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, m));
   if constexpr (NW > 1) {
     __syncthreads();  // (a rare path: nothing of the sums' places is relied on)
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6].x = v;
@@ -179,7 +179,7 @@ __device__ __forceinline__ float variance(float squares, float off) {
 __device__ __forceinline__ bool equal_values(float rstd, float eps) { return rstd == INFINITY && eps > 0.0f; }
 
 // A row's values become their differences from the mean.
-template <class T, int NW, int NC>
+template <class T, int NW, int NC, int L>
 __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T> (&chunk)[NC], int64_t cols,
                                           float eps, float2* lds) {
   constexpr int V = kVec<T>;
@@ -190,7 +190,7 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
 #pragma unroll
     for (int j = 0; j < V; ++j) s.x += counted<NC>(x[c][j], c, j, chunk[c].lead);
   Stats r;
-  r.mean = row_sums<NW>(s, lds, 0).x / n;
+  r.mean = row_sums<NW, L>(s, lds, 0).x / n;
   s.x = 0.0f;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
@@ -201,7 +201,7 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
       s.x += d;
       s.y += d * d;
     }
-  s = row_sums<NW>(s, lds, 1);
+  s = row_sums<NW, L>(s, lds, 1);
   r.off = s.x / n;
   const float var = variance(s.y / n, r.off);
   r.rstd = 1.0f / sqrtf(var + eps);
@@ -209,21 +209,22 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
   return r;
 }
 
-// A wave, or the NW waves of a workgroup, has a row, a lane NC times 16 bytes of it; the next row is under way
+// L lanes of a wave (64 of them but for rows of less than 1 KB), or the NW waves of a workgroup, have a row, a lane NC times 16 bytes of it; the next row is under way
 // while a row's sums meet. 32 values a lane leave no registers for w and b, which come from L2 for each
 // row (4096 x 16392 bfloat16: 110 us, walked 155).
-template <class T, class W, int NW, int NC>
+template <class T, class W, int NW, int NC, int L>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs p) {
   typedef typename T::elem E;
-  constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;  // kRows: of a workgroup at a time
+  static_assert(NW == 1 || L == 64);
+  constexpr int kRows = NW == 1 ? 256 / L : 1, V = kVec<T>;  // kRows: of a workgroup at a time
   __shared__ float2 lds[2 * NW];
-  const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int lane = NW == 1 ? threadIdx.x & (L - 1) : threadIdx.x;
   const int64_t stride = (int64_t)gridDim.x * kRows;
-  int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
+  int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x / L : 0);
   if (row >= p.rows) return;
   Chunk<T> chunk[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * 64 + lane) * V, (int)p.cols);
+  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * L + lane) * V, (int)p.cols);
   u32x4v next[NC];
   const auto load = [&](int64_t row) {
 #pragma unroll
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
 #pragma unroll
       for (int j = 0; j < V; ++j) x[c][j] = value_of<T>(next[c], j);
     load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
-    Stats s = stats_of<T, NW>(x, chunk, p.cols, p.eps, lds);
+    Stats s = stats_of<T, NW, NC, L>(x, chunk, p.cols, p.eps, lds);
     if (!(s.rstd > 0.0f)) {
       // squares beyond float32: the row scaled by a power of two (what is not finite stays NaN)
       float most = 0.0f;
@@ -256,14 +257,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
           most = __builtin_fmaxf(most, __builtin_fabsf(x[c][j]));
         }
       }
-      most = row_max<NW>(most, lds);
+      most = row_max<NW, L>(most, lds);
       const int e = (int)(__float_as_uint(most) >> 23) - 127;
       const float down = pow2f(-(e < 126 ? e : 126));
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int j = 0; j < V; ++j) x[c][j] *= down;
-      s = stats_of<T, NW>(x, chunk, p.cols, p.eps * down * down, lds);
+      s = stats_of<T, NW, NC, L>(x, chunk, p.cols, p.eps * down * down, lds);
       const bool equal = equal_values(s.rstd, p.eps);
       if (equal) s.rstd = 0.0f;
       if (p.mean && lane == 0) {
@@ -292,18 +293,19 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
 // As norm_kernel; a lane also keeps its columns' parts of dw and db, but where it has 32 values (norm_columns_kernel reads x and
 // dy again there: 4096 x 16392 bfloat16: 161 us, walked 303). Sixteen waves with four times 16 bytes a lane have
 // registers for neither the next row nor the weights, which come from L2 for each row (2048 x 16384 float32: 137 us, 2.9 TB/s).
-template <class T, class W, int NW, int NC>
+template <class T, class W, int NW, int NC, int L>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(NormArgs p) {
   typedef typename T::elem E;
-  constexpr int kRows = NW == 1 ? 4 : 1, V = kVec<T>;
+  static_assert(NW == 1 || L == 64);
+  constexpr int kRows = NW == 1 ? 256 / L : 1, V = kVec<T>;
   constexpr bool kAhead = NW * NC < 64, kSums = NC * V < 32;
   __shared__ float2 lds[2 * NW];
-  const int lane = NW == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int lane = NW == 1 ? threadIdx.x & (L - 1) : threadIdx.x;
   const int64_t stride = (int64_t)gridDim.x * kRows;
-  const int64_t first = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x >> 6 : 0);
+  const int64_t first = (int64_t)blockIdx.x * kRows + (NW == 1 ? threadIdx.x / L : 0);
   Chunk<T> chunk[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * 64 + lane) * V, (int)p.cols);
+  for (int c = 0; c < NC; ++c) chunk[c].start((c * NW * L + lane) * V, (int)p.cols);
   const float n = (float)p.cols;
   u32x4v xn[NC], gn[NC], an[NC] = {};  // the next row
   float mean = 0.0f, rstd = 0.0f;
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
         s.y += a * counted<NC>(xh, c, j, chunk[c].lead);
       }
     }
-    s = row_sums<NW>(s, lds, place);
+    s = row_sums<NW, L>(s, lds, place);
     place ^= 1;
     s.x /= n;
     s.y /= n;
@@ -385,10 +387,19 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
   }
   if (!kSums || !p.part) return;
   if constexpr (NW == 1) {
-    // the four waves' parts as one, wave after wave
-    __shared__ float sums[2][NC][V][64];
-    for (int i = 1; i < kRows; ++i) {
-      if ((int)threadIdx.x >> 6 == i) {
+    // a wave's rows' parts as one, then the four waves', wave after wave
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int m = L; m < 64; m *= 2) {
+          dw[c][j] += __shfl_xor(dw[c][j], m);
+          db[c][j] += __shfl_xor(db[c][j], m);
+        }
+    __shared__ float sums[2][NC][V][L];
+    for (int i = 1; i < 4; ++i) {
+      if ((int)threadIdx.x / L == i * (64 / L)) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -398,7 +409,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
           }
       }
       __syncthreads();
-      if (threadIdx.x < 64) {
+      if (threadIdx.x < L) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -411,7 +422,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
     }
   }
   if constexpr (!kSums) return;
-  if (NW > 1 || threadIdx.x < 64) {
+  if (NW > 1 || threadIdx.x < L) {
     float* to = p.part + (int64_t)blockIdx.x * 2 * p.cols;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -709,6 +720,13 @@ int shape_of(int64_t cols, int type) {
   while (i < kWalk && chunks > kShapes[i].chunks) ++i;
   return i;
 }
+// Lanes of a row of up to 64 times 16 bytes.
+int lanes_of(int64_t cols, int type) {
+  const int64_t chunks = (cols + (type == HOBFLOPS_TYPE_F32 ? 3 : 7)) / (type == HOBFLOPS_TYPE_F32 ? 4 : 8);
+  int lanes = 4;
+  while (lanes < 64 && lanes < chunks) lanes *= 2;
+  return lanes;
+}
 // Whether the sums over rows have a launch of their own.
 bool columns_apart(int shape, int type) { return shape == kWalk || (shape == 6 && type != HOBFLOPS_TYPE_F32); }
 // Backward, eight waves of 16-bit values, which are twice as many a lane, would be one workgroup on a CU, or two whose
@@ -720,7 +738,7 @@ int64_t groups_of(int64_t rows, int64_t cols, int type, bool grad) {
   const int i = shape_of(cols, type);
   if (i == kWalk) return rows < 512 ? rows : 512;
   if (i == kThread) return rows < 256 * 1024 ? (rows + 255) / 256 : 1024;
-  const int64_t groups = kShapes[i].waves == 1 ? (rows + 3) / 4 : rows;
+  const int64_t each = i == 0 ? 256 / lanes_of(cols, type) : kShapes[i].waves == 1 ? 4 : 1, groups = (rows + each - 1) / each;
   const int64_t most = !grad                                ? (kShapes[i].waves == 16 ? 512 : 2048)
                        : kShapes[i].waves <= 4              ? 768
                        : kShapes[i].waves == 8 && !wide_grad(i, type) ? 512
@@ -737,24 +755,31 @@ int64_t parts_of(int64_t rows, int64_t cols, int type) {
 template <class T>
 constexpr int kType = kVec<T> == 4 ? HOBFLOPS_TYPE_F32 : HOBFLOPS_TYPE_BF16;  // (either 16-bit type)
 
-template <class T, class W, int NW, int NC>
+template <class T, class W, int NW, int NC, int L = 64>
 void launch_grad(const NormArgs& p, hipStream_t s) {
-  norm_grad_kernel<T, W, NW, NC>
+  norm_grad_kernel<T, W, NW, NC, L>
       <<<(unsigned)groups_of(p.rows, p.cols, kType<T>, true), NW == 1 ? 256 : NW * 64, 0, s>>>(p);
 }
-template <class T, class W, int NW, int NC>
+template <class T, class W, int NW, int NC, int L = 64>
 void launch(const NormArgs& p, bool grad, hipStream_t s) {
   if constexpr (NW != 8 || kVec<T> == 4) {
-    if (grad) return launch_grad<T, W, NW, NC>(p, s);
+    if (grad) return launch_grad<T, W, NW, NC, L>(p, s);
   }
-  norm_kernel<T, W, NW, NC>
+  norm_kernel<T, W, NW, NC, L>
       <<<(unsigned)groups_of(p.rows, p.cols, kType<T>, false), NW == 1 ? 256 : NW * 64, 0, s>>>(p);
 }
 template <class T, class W>
 void launch_rows(const NormArgs& p, bool grad, hipStream_t s) {
   if (p.rows == 0) return;
   switch (shape_of(p.cols, kType<T>)) {
-    case 0: return launch<T, W, 1, 1>(p, grad, s);
+    case 0:
+      switch (lanes_of(p.cols, kType<T>)) {
+        case 4: return launch<T, W, 1, 1, 4>(p, grad, s);
+        case 8: return launch<T, W, 1, 1, 8>(p, grad, s);
+        case 16: return launch<T, W, 1, 1, 16>(p, grad, s);
+        case 32: return launch<T, W, 1, 1, 32>(p, grad, s);
+        default: return launch<T, W, 1, 1>(p, grad, s);
+      }
     case 1: return launch<T, W, 1, 2>(p, grad, s);
     case 2: return launch<T, W, 4, 1>(p, grad, s);
     case 3: return launch<T, W, 4, 2>(p, grad, s);
