@@ -706,12 +706,14 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
 }
 
 // The kernels' shapes: a row in up to `chunks` times 16 bytes, two a lane (beyond 32 KB four), the
-// more waves the longer it is. (Four a lane, 4097 x 2731 float32: backward 40 us, two waves on a SIMD; two a lane 28.)
+// more waves the longer it is. (Four a lane, 4097 x 2731 float32: backward 40 us, two waves on a SIMD; two a lane 28.
+// Two waves with two each rather than four with one: 2^25 bfloat16 values in rows of 2048 23 us instead of 31, of 1536 28 instead
+// of 37. Short rows share a wave: in rows of 64 27 us, with a wave each 166.)
 struct Shape {
   int waves;
   int64_t chunks;  // at most
 };
-constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {4, 256}, {4, 512}, {8, 1024}, {16, 2048}, {16, 4096}};
+constexpr Shape kShapes[] = {{1, 64}, {1, 128}, {2, 256}, {4, 512}, {8, 1024}, {16, 2048}, {16, 4096}};
 constexpr int kWalk = 7, kThread = 8;  // none of them: rows are walked, or a thread's
 int shape_of(int64_t cols, int type) {
   const int64_t chunks = (cols + (type == HOBFLOPS_TYPE_F32 ? 3 : 7)) / (type == HOBFLOPS_TYPE_F32 ? 4 : 8);
@@ -740,6 +742,7 @@ int64_t groups_of(int64_t rows, int64_t cols, int type, bool grad) {
   if (i == kThread) return rows < 256 * 1024 ? (rows + 255) / 256 : 1024;
   const int64_t each = i == 0 ? 256 / lanes_of(cols, type) : kShapes[i].waves == 1 ? 4 : 1, groups = (rows + each - 1) / each;
   const int64_t most = !grad                                ? (kShapes[i].waves == 16 ? 512 : 2048)
+                       : kShapes[i].waves == 2              ? 1536
                        : kShapes[i].waves <= 4              ? 768
                        : kShapes[i].waves == 8 && !wide_grad(i, type) ? 512
                                                             : 256;
@@ -781,7 +784,7 @@ void launch_rows(const NormArgs& p, bool grad, hipStream_t s) {
         default: return launch<T, W, 1, 1>(p, grad, s);
       }
     case 1: return launch<T, W, 1, 2>(p, grad, s);
-    case 2: return launch<T, W, 4, 1>(p, grad, s);
+    case 2: return launch<T, W, 2, 2>(p, grad, s);
     case 3: return launch<T, W, 4, 2>(p, grad, s);
     case 4:
       if constexpr (kVec<T> == 8) {
