@@ -353,14 +353,28 @@ __global__ __launch_bounds__(512, 2) void linear_deepest_kernel(LinearArgs p) {
   linear_tile<T, 64, 128, 2, 4, 6>(p, sa, sb);
 }
 
+// Four values of parts that are `stride` apart, added in their order; eight parts' loads under way.
+__device__ __forceinline__ f32x4 sum_parts(const float* part, int64_t stride, int parts) {
+  f32x4 v = *(const f32x4*)part;
+  int s = 1;
+  for (; s + 8 <= parts; s += 8) {
+    f32x4 e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = *(const f32x4*)(part + (s + j) * stride);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v += e[j];
+  }
+  for (; s < parts; ++s) v += *(const f32x4*)(part + s * stride);
+  return v;
+}
+
 // The parts of a sum in their order, then the epilogue: 4 values a thread.
 template <class T>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int splits) {
   typedef typename T::elem E;
   const int64_t ldp = (p.N + 3) & ~(int64_t)3, n = p.T_ * ldp;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
-    f32x4 v = *(const f32x4*)(p.part + i);
-    for (int s = 1; s < splits; ++s) v += *(const f32x4*)(p.part + s * n + i);
+    f32x4 v = sum_parts(p.part + i, n, splits);
     const int64_t row = i / ldp, col = i - row * ldp;
     if (p.bias) v += load4<T>((const E*)p.bias, col, p.N);
     if (p.z) {
@@ -642,8 +656,7 @@ template <class T>
 __device__ __forceinline__ void join_of(const JoinArgs& p, int64_t i, int64_t stride) {
   const int64_t ldp = (p.cols + 3) & ~(int64_t)3, n = p.rows * ldp;
   for (i *= 4; i < n; i += stride * 4) {
-    f32x4 v = *(const f32x4*)(p.part + i);
-    for (int s = 1; s < p.splits; ++s) v += *(const f32x4*)(p.part + s * n + i);
+    const f32x4 v = sum_parts(p.part + i, n, p.splits);
     const int64_t row = i / ldp, col = i - row * ldp;
     const float e[4] = {v[0], v[1], v[2], v[3]};
     store4<T>((typename T::elem*)p.out + row * p.cols, col, p.cols, e);
@@ -673,7 +686,7 @@ __global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t
 
 // The tiles of a product through LDS and the parts of its sum, by an estimate of their time in microseconds: rounds of
 // workgroups, each its steps of 64 k and some more to start and end; the parts of a sum are written and read
-// once more in float32, 4 TB/s, and joined in a launch. The kinds' times are those of the sizes that each is for, measured: of
+// once more in float32, 4 TB/s, and joined in a launch, eight at a time. The kinds' times are those of the sizes that each is for, measured: of
 // 4096 x 4096 -> 4096 (98 us), 2048 x 4096 -> 4096 (60, the others 84, 65 and 88), 1024 x 4096 -> 4096 (34; 78, 44, 46) and
 // 512 x 4096 -> 4096 (24; 76, 41, 28).
 struct Kind {
@@ -687,7 +700,7 @@ struct Tiling {
   int64_t groups;           // workgroups
   double each, join, us;    // the time of a workgroup, of the parts, of all
 };
-constexpr int kMostSplits = 32;
+constexpr int kMostSplits = 128;
 // The best of kinds first, .. last - 1.
 Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last) {
   const int64_t steps = (K + kStepK - 1) / kStepK;
@@ -696,10 +709,10 @@ Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last) {
     const Kind& kind = kKinds[k];
     const int64_t slots = kind.per_cu * kCUs;
     const int64_t tiles = ((rows + kind.rows - 1) / kind.rows) * ((cols + kind.cols - 1) / kind.cols);
-    for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); ++n) {
+    for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); n += 1 + n / 16) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
       const double each = ((double)((steps + n - 1) / n) + kind.lead) * kind.step;
-      const double join = n > 1 ? 4.0 + (double)(2 * n) * rows * cols * 4.0 / 4e6 : 0.0;
+      const double join = n > 1 ? 4.0 + 0.1 * n + (double)(2 * n) * rows * cols * 4.0 / 4e6 : 0.0;
       const double us = rounds * each + join;
       if (best.us < 0.0 || us < best.us) best = Tiling{k, n, tiles * n, each, join, us};
     }
