@@ -11,7 +11,7 @@
 // launch adds the parts in their order (no atomics: the same inputs give the same bits).
 //
 // Measured: 16384 x 4096 bfloat16 forward 46 to 51 us (5.3 to 5.9 TB/s of what it must read and write), backward with a
-// gradient to add 94 (5.7) and 5.4 for the parts (25 MB of them); 4097 x 2731 float32 in rows that begin anywhere 22 (4.1), 24.3
+// gradient to add 94 (5.7) and 5.4 for the parts (25 MB of them); 4097 x 2731 float32 in rows that begin anywhere 20.5 (4.4), 24.3
 // (5.5) and 4.0; one row of 4096 3.1, of which the work is one load's latency and two sums'. A large copy: 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
