@@ -715,8 +715,8 @@ def _bytes_of(query, device, *args):
 def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
     """y = (x - mean) rstd weight + bias over the rows of x [rows, cols] (float32, bfloat16 or
     float16, dense rows any distance apart); weight and bias [cols] of x's type or float32 (one type).
-    With save: (y, saved), what layer_norm_backward needs beside x. out may be x. Autograd
-    records nothing of it."""
+    With save: (y, saved), what layer_norm_backward needs beside x. out may be x (another overlap is an
+    error). Autograd records nothing of it."""
     px, rows, cols, ldx = _rows(x, "layer_norm x")
     kind, dev = _type(x, "layer_norm x"), x.device
     pw = _vector(weight, cols, (x.dtype, torch.float32), dev, "layer_norm weight")
@@ -765,8 +765,8 @@ def layer_norm_backward(dy, x, saved, weight=None, add=None, dw=True, db=True):
 def linear(x, w, bias=None, act=None, residual=None, save=False, out=None):
     """y = act(x w^T + bias) + residual: x [T, K], w [N, K], bias [N], residual [T, N], bfloat16 or
     float16 -> y [T, N]. act: GATE_SILU, GATE_GELU, GATE_RELU or None. With save: (y, z), z [T, N] what act
-    was applied to, for linear_backward (None without act). out may be the residual. Autograd records
-    nothing of it."""
+    was applied to, for linear_backward (None without act). out may be the residual (another overlap is an
+    error). Autograd records nothing of it."""
     px, T, K, ldx = _rows(x, "linear x")
     pw, N, Kw, ldw = _rows(w, "linear w")
     kind, dev = _type(x, "linear x"), x.device
