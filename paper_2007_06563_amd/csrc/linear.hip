@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p, int spli
   const int64_t ldp = (p.N + 3) & ~(int64_t)3, n = p.T_ * ldp;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
     f32x4 v = sum_parts(p.part + i, n, splits);
-    const int64_t row = i / ldp, col = i - row * ldp;
+    const int64_t row = quotient(i, ldp), col = i - row * ldp;
     if (p.bias) v += load4<T>((const E*)p.bias, col, p.N);
     if (p.z) {
       const float e[4] = {v[0], v[1], v[2], v[3]};
@@ -657,7 +657,7 @@ __device__ __forceinline__ void join_of(const JoinArgs& p, int64_t i, int64_t st
   const int64_t ldp = (p.cols + 3) & ~(int64_t)3, n = p.rows * ldp;
   for (i *= 4; i < n; i += stride * 4) {
     const f32x4 v = sum_parts(p.part + i, n, p.splits);
-    const int64_t row = i / ldp, col = i - row * ldp;
+    const int64_t row = quotient(i, ldp), col = i - row * ldp;
     const float e[4] = {v[0], v[1], v[2], v[3]};
     store4<T>((typename T::elem*)p.out + row * p.cols, col, p.cols, e);
   }

@@ -13,6 +13,12 @@ namespace hobflops {
 
 constexpr int64_t kCUs = 256;
 
+// a / b of numbers that are not negative, mostly below 2^32, where it takes a quarter of the instructions.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
+
 // Rows of operands as the products need them: 16-byte aligned, zeros from cols up to ldd. Up to three
 // tensors of one width in a launch. (Whole chunks are read 16 bytes at a time whatever their alignment.)
 struct AlignArgs {
@@ -27,7 +33,7 @@ __device__ __forceinline__ void align_rows_of(const AlignArgs& p, int64_t i, int
   typedef typename T::elem E;
   const int64_t per = p.ldd / 8, n = p.rows[2] * per;
   for (; i < n; i += stride) {
-    const int64_t all = i / per, col = (i - all * per) * 8;
+    const int64_t all = quotient(i, per), col = (i - all * per) * 8;
     const int which = all < p.rows[0] ? 0 : all < p.rows[1] ? 1 : 2;
     const int64_t row = all - (which == 0 ? 0 : which == 1 ? p.rows[0] : p.rows[1]);
     const E* s = (const E*)p.src[which] + row * p.ld[which] + col;
