@@ -423,7 +423,7 @@ int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* 
  *   dx = rstd (a - mean(a) - xh mean(a xh)) + add, dweight = sum over rows of dy xh,
  *   dbias = sum over rows of dy
  * add (rows ld_add apart; NULL: none): a gradient that reaches x past the norm, joined before the one rounding. dx is
- * dense and overlaps none of the call's inputs. dweight and dbias of wtype, either may be NULL. Sums run in a
+ * dense. dweight and dbias of wtype, either may be NULL. None of the three overlaps another or an input (HOBFLOPS_EINVAL). Sums run in a
  * fixed order. The workspace is needed where one of these two is asked for. */
 int hobflops_layer_norm_workspace(const hobflops_norm_desc* d, int64_t* bytes);
 int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, const void* x,
@@ -458,7 +458,7 @@ int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w,
 
 /* Gradients from dy [T][N] (rows ldy apart) and z:
  *   dz = dy act'(z) (act' of max(z, 0) is 0 at 0), dx = dz w [T][K], dw = dz^T x [N][K], dbias = sum over tokens of dz
- * all dense and of d->type; those that are NULL are not computed. The residual's gradient is dy. dz is rounded
+ * all dense and of d->type; those that are NULL are not computed, none overlaps another or an input (HOBFLOPS_EINVAL). The residual's gradient is dy. dz is rounded
  * to d->type before the products (dbias is summed before that), whose sums are float32. z is needed with an
  * activation, x for dw, w for dx. With T = 0 dw and dbias are zero. Sums run in a fixed order. */
 int hobflops_linear_backward(const hobflops_linear_desc* d, const void* dy, const void* x,

@@ -275,6 +275,17 @@ int overlap(const Rows& a, const Rows& b) {
   return !(apart >= na && apart + nb <= step);
 }
 
+// Whether any of n results overlaps another one or one of m inputs.
+int any_overlap(const Rows* out, int n, const Rows* in, int m) {
+  for (int i = 0; i < n; ++i) {
+    for (int j = 0; j < m; ++j)
+      if (overlap(out[i], in[j])) return 1;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return 1;
+  }
+  return 0;
+}
+
 // Memory that a call writes or only reads.
 struct Range {
   uintptr_t begin, end;
@@ -844,6 +855,12 @@ int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, co
       !aligned_to(weight, wb) || !aligned_to(dweight, wb) || !aligned_to(dbias, wb) ||
       !aligned_to(mean, 4) || !aligned_to(rstd, 4) || (d->rows > 0 && !aligned_to(workspace, 16)))
     return HOBFLOPS_EALIGN;
+  if (d->rows > 0) {
+    const Rows out[] = {{dx, d->rows, d->cols, d->cols, b}, {dweight, 1, d->cols, d->cols, wb}, {dbias, 1, d->cols, d->cols, wb}};
+    const Rows in[] = {{x, d->rows, d->cols, d->ldx, b}, {dy, d->rows, d->cols, d->ldy, b}, {add, d->rows, d->cols, d->ld_add, b},
+                       {weight, 1, d->cols, d->cols, wb}, {mean, 1, d->rows, d->rows, 4}, {rstd, 1, d->rows, d->rows, 4}};
+    if (any_overlap(out, 3, in, 6)) return HOBFLOPS_EINVAL;
+  }
   LayerNorm p{d->rows, d->cols, d->ldx, d->ldy, d->ld_add, d->type, d->wtype, d->eps};
   p.x = x;
   p.w = weight;
@@ -909,6 +926,12 @@ int hobflops_linear_backward(const hobflops_linear_desc* d, const void* dy, cons
   if (!aligned_to(dy, d->align) || !aligned_to(x, d->align) || !aligned_to(w, d->align) ||
       !aligned_to(z, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(dbias, 2))
     return HOBFLOPS_EALIGN;
+  if (d->T > 0) {
+    const Rows out[] = {{dx, d->T, d->K, d->K, 2}, {dw, d->N, d->K, d->K, 2}, {dbias, 1, d->N, d->N, 2}};
+    const Rows in[] = {{dy, d->T, d->N, d->ldy, 2}, {x, d->T, d->K, d->ldx, 2}, {w, d->N, d->K, d->ldw, 2},
+                       {d->act == HOBFLOPS_GATE_NONE ? nullptr : z, d->T, d->N, d->N, 2}};
+    if (any_overlap(out, 3, in, 4)) return HOBFLOPS_EINVAL;
+  }
   const LinearBackward p{dy, x, w, z, dx, dw, dbias, workspace};
   return hip_status(launch_linear_backward(*d, p, (hipStream_t)stream));
 }

@@ -81,6 +81,24 @@ def test_linear_overlaps(hf, kw):
     assert hf.lib().hobflops_linear(d, *[ctypes.c_void_p(p) for p in a.values()], FAKE, BIG, None) == -1
 
 
+@pytest.mark.parametrize("kw", [dict(dx=0x100000), dict(dx=0x200000 + 2 * 255), dict(dx=0x600000 - 2), dict(dw=0x700000 + 4),
+                                dict(dw=0x300000), dict(db=0x400000 - 4), dict(db=0x800000 + 4 * 63), dict(dw=0x500000)])
+def test_norm_backward_overlaps(hf, kw):
+    """dy, x (bfloat16), weight, mean, rstd (float32), add; dx, dw, db."""
+    a = dict(dy=0x100000, x=0x200000, w=0x300000, mean=0x400000, rstd=0x500000, add=0x600000, dx=0x700000, dw=0x800000,
+             db=0x900000, ws=0xa00000)
+    a.update(kw)
+    assert hf.lib().hobflops_layer_norm_backward(_norm_desc(hf), *[ctypes.c_void_p(p) for p in a.values()], BIG, None) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(dx=0x100000), dict(dx=0x200000), dict(dw=0x300000), dict(db=0x400000), dict(dw=0x500000 + 2),
+                                dict(db=0x600000 + 2 * 64 * 95)])
+def test_linear_backward_overlaps(hf, kw):
+    a = dict(dy=0x100000, x=0x200000, w=0x300000, z=0x400000, dx=0x500000, dw=0x600000, db=0x700000, ws=0x800000)
+    a.update(kw)
+    assert hf.lib().hobflops_linear_backward(_linear_desc(hf), *[ctypes.c_void_p(p) for p in a.values()], BIG, None) == -1
+
+
 def _linear_desc(hf, **kw):
     d = dict(T=20, K=64, N=96, ldx=64, ldw=64, ldy=96, ldr=96, type=1, act=0, align=16)
     d.update(kw)
