@@ -339,9 +339,10 @@ __global__ __launch_bounds__(256, 2) void linear_small_kernel(LinearArgs p) {
   HOBFLOPS_STAGES2(128, 128);
   linear_tile<T, 128, 128, 2, 2, 2>(p, sa, sb);
 }
-// Launches of about a workgroup a CU, which nothing else hides the latency of: four stages of 128 x 128 sums, or six of 64 x
-// 128, under way, and two waves on a SIMD. (1024 x 4096 -> 4096: 34 us, of linear_small_kernel's 44; 512 x 4096 -> 4096:
-// 24 in 64 x 128, 28 in 128 x 128, 41; four waves with four stages, a wave on a SIMD: 37 and 31.)
+// Launches of about a workgroup a CU, which nothing else hides the latency of: four stages of 128 x 128 sums, six of 64 x
+// 128 or eight of 64 x 64 under way, and two waves on a SIMD. (1024 x 4096 -> 4096: 34 us, of linear_small_kernel's 44; 512 x
+// 4096 -> 4096: 24 in 64 x 128, 28 in 128 x 128, 41; 256 x 4096 -> 4096: 16 in 64 x 64, 20, 27, 40; 32 x 4096 -> 11264: 19 in 64 x
+// 64, 23 in 64 x 128; four waves with four stages, a wave on a SIMD: 37 and 31.)
 template <class T>
 __global__ __launch_bounds__(512, 2) void linear_deep_kernel(LinearArgs p) {
   HOBFLOPS_STAGES4(128, 128);
@@ -351,6 +352,11 @@ template <class T>
 __global__ __launch_bounds__(512, 2) void linear_deepest_kernel(LinearArgs p) {
   HOBFLOPS_STAGES6(64, 128);
   linear_tile<T, 64, 128, 2, 4, 6>(p, sa, sb);
+}
+template <class T>
+__global__ __launch_bounds__(512, 2) void linear_least_kernel(LinearArgs p) {
+  HOBFLOPS_STAGES8(64, 64);
+  linear_tile<T, 64, 64, 2, 4, 8>(p, sa, sb);
 }
 
 // Four values of parts that are `stride` apart, added in their order; eight parts' loads under way.
@@ -685,25 +691,28 @@ __global__ __launch_bounds__(256) void zeros_kernel(typename T::elem* p, int64_t
 
 // ---- plans -------------------------------------------------------------------
 
+// Reading rows that do not begin on lines of 128 bytes takes a third more, rows at odd values twice as long (direct_kernel, 333 x
+// 8192 -> 1000: 21 us, of 8200 values 26, of 8193 37; in tiles 512 x 4104 -> 4096 32, of 4096 values 23).
+double row_factor(int64_t ld, int align) { return ld % 2 != 0 || align == 2 ? 2.0 : ld % 64 != 0 ? 1.33 : 1.0; }
 // The tiles of a product through LDS and the parts of its sum, by an estimate of their time in microseconds: rounds of
 // workgroups, each its steps of 64 k and some more to start and end; the parts of a sum are written and read
 // once more in float32, 4 TB/s, and joined in a launch, eight at a time. The kinds' times are those of the sizes that each is for, measured: of
-// 4096 x 4096 -> 4096 (98 us), 2048 x 4096 -> 4096 (60, the others 84, 65 and 88), 1024 x 4096 -> 4096 (34; 78, 44, 46) and
-// 512 x 4096 -> 4096 (24; 76, 41, 28).
+// 4096 x 4096 -> 4096 (98 us), 2048 x 4096 -> 4096 (60, the others 84, 65 and 88), 1024 x 4096 -> 4096 (34; 78, 44, 46),
+// 512 x 4096 -> 4096 (24; 76, 41, 28, 31) and 256 x 4096 -> 4096 (16). Steps of rows off the lines of memory take longer, as above.
 struct Kind {
   int rows, cols, per_cu;
   double step, lead;
 };
-constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}};
-constexpr int kForwardKinds = 4, kGradKinds = 3;
+constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}, {64, 64, 1, 0.17, 25}};
+constexpr int kForwardKinds = 5, kGradKinds = 3;
 struct Tiling {
   int kind, splits;
   int64_t groups;           // workgroups
   double each, join, us;    // the time of a workgroup, of the parts, of all
 };
 constexpr int kMostSplits = 128;
-// The best of kinds first, .. last - 1.
-Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last) {
+// The best of kinds first, .. last - 1. off: whether rows begin off the lines of memory.
+Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last, bool off = false) {
   const int64_t steps = (K + kStepK - 1) / kStepK;
   Tiling best{first, 1, 0, 0.0, 0.0, -1.0};
   for (int k = first; k < last; ++k) {
@@ -712,7 +721,7 @@ Tiling plan_tiles(int64_t rows, int64_t cols, int64_t K, int first, int last) {
     const int64_t tiles = ((rows + kind.rows - 1) / kind.rows) * ((cols + kind.cols - 1) / kind.cols);
     for (int n = 1; n <= kMostSplits && (n == 1 || steps / n >= 3); n += 1 + n / 16) {
       const double rounds = (double)((tiles * n + slots - 1) / slots);
-      const double each = ((double)((steps + n - 1) / n) + kind.lead) * kind.step;
+      const double each = ((double)((steps + n - 1) / n) * (off ? (k == 0 ? 1.17 : 1.33) : 1.0) + kind.lead) * kind.step;
       const double join = n > 1 ? 4.0 + 0.1 * n + (double)(2 * n) * rows * cols * 4.0 / 4e6 : 0.0;
       const double us = rounds * each + join;
       if (best.us < 0.0 || us < best.us) best = Tiling{k, n, tiles * n, each, join, us};
@@ -730,13 +739,11 @@ double pair_us(const Tiling& a, const Tiling& b) {
   return (t > alone ? t : alone) + a.join + b.join;
 }
 // The tile of direct_kernel in 16 rows of W and 16 tokens, by an estimate: rounds of workgroups, one on each CU, which
-// read their rows at 100 bytes a nanosecond, and start and end, the longer the larger the tile. Measured, us, in the order
+// read their rows at 100 bytes a nanosecond, and start and end, the longer the larger the tile; or the weights from HBM, at
+// the rate that the CUs in use leave of it (32 x 4096 -> 11264: 352 workgroups, 24 us; in tiles of 64 x 64 19). Measured, us, in the order
 // of kDirect, and in tiles through LDS: 16 x 4096 -> 4096 8.5, 9.3, 10.7, 9.6, 12.0, 18.1, LDS 15.3; 64 x 4096 -> 4096
 // 19.0, 15.5, 12.1, 10.7, 13.5, 18.4, LDS 17.3; 333 x 2730 -> 1000 24.5, 20.6, 19.2, 16.8, 13.0, 18.6, LDS 24.2;
 // 1024 x 1024 -> 1024 33, 29, 19, 16, 13, 9.4, LDS 14.0; 2048 x 512 -> 1408 77, 66, 25, 38, 22, 18, LDS 10.0.
-// Rows that do not begin on lines of 128 bytes take a third more, rows at odd values twice as long (333 x 8192 -> 1000: 21,
-// of 8200 values 26, of 8193 37).
-double row_factor(int64_t ld, int align) { return ld % 2 != 0 || align == 2 ? 2.0 : ld % 64 != 0 ? 1.33 : 1.0; }
 struct Direct {
   int ni, nj;
 };
@@ -749,7 +756,11 @@ int plan_direct(int64_t N, int64_t T, int64_t K, double factor, double* us) {
     if (d.nj > 1 && T <= 8 * d.nj) continue;  // more than half of the tokens would be nobody's
     const int64_t groups = ((N + 16 * d.ni - 1) / (16 * d.ni)) * ((T + 16 * d.nj - 1) / (16 * d.nj));
     const double rounds = (double)((groups + kCUs - 1) / kCUs);
-    const double t = rounds * (factor * (16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0 + 0.18 * d.ni * d.nj) + 3.0;
+    double t = rounds * (factor * (16 * (d.ni + d.nj)) * K * 2.0 / 100e3 + 1.0 + 0.18 * d.ni * d.nj);
+    // the weights from HBM, 4.9 TB/s of full rounds; what is shorter of the two is not all hidden
+    const double read = (double)N * K * 2.0 / 4.9e6 * rounds * kCUs / groups;
+    t = t > read ? t + 0.1 * read : read + 0.1 * t;
+    t += 3.0;
     if (*us < 0.0 || t < *us) {
       *us = t;
       best = i;
@@ -773,22 +784,26 @@ struct ForwardPlan {
 };
 // Rows that the forward product reads in place: loads of 16 bytes into LDS need addresses of whole words.
 bool words(int64_t ld, int align) { return align >= 4 && ld % 2 == 0 && ld < (int64_t)1 << 21; }
+// Values between the rows of a copy, whose last ones are zeros: rows that are not short begin on lines of memory.
+int64_t copied_ld(int64_t K) { return round_up(K, K < 512 ? 8 : 64); }
 ForwardPlan plan_forward(const hobflops_linear_desc& d) {
   ForwardPlan p;
-  const int64_t Kp = round_up(d.K, 8);
-  p.tiles = plan_tiles(d.N, d.T, d.K, 0, kForwardKinds);
-  double us = p.tiles.us + (p.tiles.splits > 1 ? 4.0 : 0.0), direct = 0.0;  // (the second launch's start)
+  const double fx = row_factor(d.ldx, d.align), fw = row_factor(d.ldw, d.align);
+  double direct = 0.0;
+  const int i = plan_direct(d.N, d.T, d.K, fx > fw ? fx : fw, &direct);
+  const bool x = words(d.ldx, d.align), w = words(d.ldw, d.align);  // in place
+  p.tiles = plan_tiles(d.N, d.T, d.K, 0, kForwardKinds, (x && fx > 1.0) || (w && fw > 1.0));
+  const double read = (double)d.N * d.K * 2.0 / 4.4e6 + 3.0;  // the weights from HBM
+  double us = (p.tiles.us > read ? p.tiles.us : read) + (p.tiles.splits > 1 ? 4.0 : 0.0);  // (the second launch's start)
   // (rows that are not in place are copied in a launch of their own first)
-  if (!words(d.ldx, d.align) || !words(d.ldw, d.align))
-    us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
-  const double x = row_factor(d.ldx, d.align), w = row_factor(d.ldw, d.align);
-  const int i = plan_direct(d.N, d.T, d.K, x > w ? x : w, &direct);
-  if (direct < us) {
+  if (!x || !w) us += 4.0 + (double)(d.T + d.N) * d.K * 4.0 / 4e6;
+  // (a tile through LDS would be three quarters nobody's tokens, and direct_kernel reads the weights at HBM's rate)
+  if (direct < us || d.T <= 16) {
     p.direct = i;
     return p;
   }
-  if (!words(d.ldx, d.align)) p.x = take(&p.bytes, d.T * Kp * 2);
-  if (!words(d.ldw, d.align)) p.w = take(&p.bytes, d.N * Kp * 2);
+  if (!x) p.x = take(&p.bytes, d.T * copied_ld(d.K) * 2);
+  if (!w) p.w = take(&p.bytes, d.N * copied_ld(d.K) * 2);
   if (p.tiles.splits > 1) p.part = take(&p.bytes, p.tiles.splits * d.T * round_up(d.N, 4) * 4);
   return p;
 }
@@ -872,7 +887,7 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   uint8_t* ws = (uint8_t*)c.workspace;
   AlignArgs align{};
   align.cols = d.K;
-  align.ldd = round_up(d.K, 8);
+  align.ldd = copied_ld(d.K);
   if (plan.x >= 0) {
     add_rows(align, 0, c.x, d.ldx, d.T, ws + plan.x);
     p.x = ws + plan.x;
@@ -885,7 +900,7 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
   }
   align_rows<T>(align, s);
   // (rows that were copied have zeros up to the multiple of 8)
-  if (plan.x >= 0 && plan.w >= 0) p.K = align.ldd;
+  if (plan.x >= 0 && plan.w >= 0) p.K = round_up(d.K, 8);
   p.tail = (int)(p.K % 8);
   p.K -= p.tail;
   const int64_t splits = splits_of(p.K > 0 ? p.K : 1, plan.tiles.splits, &p.per);
@@ -898,7 +913,8 @@ hipError_t forward(const hobflops_linear_desc& d, const LinearForward& c, hipStr
     case 0: linear_kernel<T><<<grid, 512, 0, s>>>(p); break;
     case 1: linear_small_kernel<T><<<grid, 256, 0, s>>>(p); break;
     case 2: linear_deep_kernel<T><<<grid, 512, 0, s>>>(p); break;
-    default: linear_deepest_kernel<T><<<grid, 512, 0, s>>>(p);
+    case 3: linear_deepest_kernel<T><<<grid, 512, 0, s>>>(p); break;
+    default: linear_least_kernel<T><<<grid, 512, 0, s>>>(p);
   }
   if (p.part)
     linear_join_kernel<T><<<grid_of(d.T * round_up(d.N, 4) / 4, 4096), 256, 0, s>>>(p, (int)splits);

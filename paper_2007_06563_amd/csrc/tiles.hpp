@@ -137,6 +137,13 @@ __device__ __forceinline__ void store_rows(typename T::elem* p, int64_t end, boo
       b3[rows_b * 128], b4[rows_b * 128], b5[rows_b * 128];                                     \
   uint8_t* const sa[6] = {a0, a1, a2, a3, a4, a5};                                              \
   uint8_t* const sb[6] = {b0, b1, b2, b3, b4, b5}
+#define HOBFLOPS_STAGES8(rows_a, rows_b)                                                        \
+  __shared__ __align__(1024) uint8_t a0[rows_a * 128], a1[rows_a * 128], a2[rows_a * 128],      \
+      a3[rows_a * 128], a4[rows_a * 128], a5[rows_a * 128], a6[rows_a * 128], a7[rows_a * 128]; \
+  __shared__ __align__(1024) uint8_t b0[rows_b * 128], b1[rows_b * 128], b2[rows_b * 128],      \
+      b3[rows_b * 128], b4[rows_b * 128], b5[rows_b * 128], b6[rows_b * 128], b7[rows_b * 128]; \
+  uint8_t* const sa[8] = {a0, a1, a2, a3, a4, a5, a6, a7};                                      \
+  uint8_t* const sb[8] = {b0, b1, b2, b3, b4, b5, b6, b7}
 
 // The gradients' products, D[i][j] with i along a row of the output; kParts weights side by side (the gated
 // block's two, a linear layer's one):

@@ -131,11 +131,12 @@ def test_many_tiles(T, K, N, dtype, act):
 
 @pytest.mark.parametrize("T,K,N", [(500, 2040, 4100), (260, 4104, 4000), (700, 16400, 264), (500, 1000, 1100),
                                    (2048, 512, 1400), (1000, 1027, 4000), (257, 72, 8200), (128, 4096, 11264),
-                                   (30000, 100, 130)])
+                                   (30000, 100, 130), (250, 2050, 4000), (33, 4096, 11270), (100, 9000, 1100),
+                                   (300, 2055, 2000), (48, 5000, 5001)])
 @pytest.mark.parametrize("dtype,act,bias,res", [("bf16", 1, True, True), ("f16", None, False, True),
                                                 ("bf16", 2, True, False)])
 def test_a_workgroup_a_cu(T, K, N, dtype, act, bias, res):
-    """Sizes whose tiles have four or six stages, with steps that are no multiple of them, and in parts."""
+    """Sizes whose tiles have four to eight stages, with steps that are no multiple of them, and in parts."""
     hf = need_gpu()
     say("linear deep", T, K, N, dtype, act, bias, res)
     lds = (K, K, N, N)
