@@ -703,7 +703,7 @@ struct Kind {
   int rows, cols, per_cu;
   double step, lead;
 };
-constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}, {64, 64, 1, 0.17, 25}};
+constexpr Kind kKinds[] = {{256, 256, 1, 1.42, 5}, {128, 128, 2, 0.8, 5}, {128, 128, 1, 0.45, 11}, {64, 128, 1, 0.31, 14}, {64, 64, 1, 0.17, 30}};
 constexpr int kForwardKinds = 5, kGradKinds = 3;
 struct Tiling {
   int kind, splits;
