@@ -457,7 +457,7 @@ int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w,
                     int64_t workspace_bytes, void* stream);
 
 /* Gradients from dy [T][N] (rows ldy apart) and z:
- *   dz = dy act'(z) (act' of max(z, 0) is 0 at 0), dx = dz w [T][K], dw = dz^T x [N][K], dbias = sum over tokens of dz
+ *   dz = dy act'(z) (act' of max(z, 0) is 0 at 0; of an infinite z, as one beyond float16 is kept, 0 or 1), dx = dz w [T][K], dw = dz^T x [N][K], dbias = sum over tokens of dz
  * all dense and of d->type; those that are NULL are not computed, none overlaps another or an input (HOBFLOPS_EINVAL). The residual's gradient is dy. dz is rounded
  * to d->type before the products (dbias is summed before that), whose sums are float32. z is needed with an
  * activation, x for dw, w for dx. With T = 0 dw and dbias are zero. Sums run in a fixed order. */

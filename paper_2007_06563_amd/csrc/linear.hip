@@ -74,23 +74,30 @@ __device__ __forceinline__ void act_on(float (&v)[N], int act) {
     for (int k = 0; k < N; ++k) v[k] = v[k] > 0.0f || v[k] != v[k] ? v[k] : 0.0f;
   }
 }
+// A z that was kept as an infinity (float16 ends at 65504, the float32 z that y is of does not) has the slope of the
+// largest float32, 0 or 1: infinity times the 0 of the gate's other half would be NaN.
+__device__ __forceinline__ float finite_z(float z) {
+  return __builtin_isinf(z) ? __builtin_copysignf(0x1.FFFFFEp127f, z) : z;
+}
 template <int N>
-__device__ __forceinline__ void times_act_grad(float (&d)[N], const float (&z)[N], int act) {
+__device__ __forceinline__ void times_act_grad(float (&d)[N], const float (&kept)[N], int act) {
   if (act == HOBFLOPS_GATE_SILU) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const Sigmoid v = silu_gate(z[k]);
-      d[k] *= v.s * __builtin_fmaf(z[k], v.c, 1.0f);
+      const float z = finite_z(kept[k]);
+      const Sigmoid v = silu_gate(z);
+      d[k] *= v.s * __builtin_fmaf(z, v.c, 1.0f);
     }
   } else if (act == HOBFLOPS_GATE_GELU) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const Gate v = gelu_gate(z[k]);
-      d[k] *= __builtin_fmaf(z[k], v.e * 0.398942280f, v.p);
+      const float z = finite_z(kept[k]);
+      const Gate v = gelu_gate(z);
+      d[k] *= __builtin_fmaf(z, v.e * 0.398942280f, v.p);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < N; ++k) d[k] *= z[k] > 0.0f ? 1.0f : z[k] != z[k] ? z[k] : 0.0f;
+    for (int k = 0; k < N; ++k) d[k] *= kept[k] > 0.0f ? 1.0f : kept[k] != kept[k] ? kept[k] : 0.0f;
   }
 }
 
