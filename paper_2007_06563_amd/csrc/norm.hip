@@ -4,8 +4,8 @@
 //   dw = sum over rows of dy xh,  db = sum over rows of dy.
 // HBM-bound: x, and dy, are read once and stay in registers, a row in one wave or the waves of a
 // workgroup. Sums are float32. The variance is of differences from the mean, whose own mean, what the first
-// one's rounding left, is taken off again: rows far from 0 keep their digits. Rows whose squares pass float32's
-// range are scaled by a power of two.
+// one's rounding left, is taken off again: rows far from 0 keep their digits. Rows whose squares leave float32's
+// range, above or below, are scaled by a power of two.
 //
 // The sums over rows: a workgroup takes many rows and keeps its part of dw and db in registers; a second
 // launch adds the parts in their order (no atomics: the same inputs give the same bits).
@@ -14,6 +14,7 @@
 // gradient to add 94 (5.7) and 5.4 for the parts (25 MB of them); 4097 x 2731 float32 in rows that begin anywhere 20.5 (4.4), 24.3
 // (5.5) and 4.0; one row of 4096 3.1, of which the work is one load's latency and two sums'. A large copy: 5.2 TB/s.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -32,6 +33,7 @@ struct NormArgs {
   float *mean, *rstd, *part;  // part: [parts][2][cols]
   int64_t rows, cols, ldx, ldy, ld_add;  // ldy: of y or of dy
   float eps;
+  float root;  // the power of two below eps's root, or 0
   bool past;  // y or dx goes past the caches
 };
 
@@ -168,6 +170,15 @@ __device__ __forceinline__ float row_max(float v, float2* lds) {
 struct Stats {
   float mean, off, rstd;  // the mean is mean + off
 };
+// Whether they were. A variance (with eps) of more than 2^-120 holds squares to 2^-30 of it, each at most 2^-150 off.
+__device__ __forceinline__ bool in_range(float rstd) { return rstd > 0.0f && rstd < 0x1p60f; }
+// What a row is scaled by otherwise, from its largest magnitude: that becomes 1 or 2, or less where eps, which is
+// scaled twice, would pass the range. (The exponent clamped between both limits would hold one of them in a register, which
+// 16-bit rows of 32 to 64 KB do not have: 4096 x 16392 122 us instead of 107.)
+__device__ __forceinline__ float scale_down(float most, float root) {
+  const int e = (int)(__float_as_uint(__builtin_fmaxf(most, root)) >> 23) - 127;
+  return pow2f(-(e < 126 ? e : 126));
+}
 
 // From the mean of the differences' squares. What is left of equal values far from 0 is rounding, 2^-24 of the
 // differences' mean; a variance of no less than 2^-44 of its square keeps that from growing.
@@ -205,7 +216,7 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
   r.off = s.x / n;
   const float var = variance(s.y / n, r.off);
   r.rstd = 1.0f / sqrtf(var + eps);
-  // (NaN, or 0 for an infinite variance: for the caller)
+  // (NaN, 0 for an infinite variance, large for a lost one: for the caller)
   return r;
 }
 
@@ -245,8 +256,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
       for (int j = 0; j < V; ++j) x[c][j] = value_of<T>(next[c], j);
     load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
     Stats s = stats_of<T, NW, NC, L>(x, chunk, p.cols, p.eps, lds);
-    if (!(s.rstd > 0.0f)) {
-      // squares beyond float32: the row scaled by a power of two (what is not finite stays NaN)
+    if (!in_range(s.rstd)) {
+      // the row scaled by a power of two (what is not finite stays NaN)
       float most = 0.0f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
@@ -258,8 +269,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_kernel(NormArgs 
         }
       }
       most = row_max<NW, L>(most, lds);
-      const int e = (int)(__float_as_uint(most) >> 23) - 127;
-      const float down = pow2f(-(e < 126 ? e : 126));
+      const float down = scale_down(most, p.root);
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -473,12 +483,11 @@ __global__ __launch_bounds__(256) void norm_few_kernel(NormArgs p) {
       }
       r.off = off / (float)n;
       r.rstd = 1.0f / sqrtf(variance(squares / (float)n, r.off) + p.eps * down * down);
-      if (r.rstd > 0.0f || again) break;
+      if (in_range(r.rstd) || again) break;
       float most = 0.0f;
 #pragma unroll
       for (int j = 0; j < M; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(x[j]));
-      const int e = (int)(__float_as_uint(most) >> 23) - 127;
-      down = pow2f(-(e < 126 ? e : 126));
+      down = scale_down(most, p.root);
 #pragma unroll
       for (int j = 0; j < M; ++j) x[j] *= down;
     }
@@ -579,7 +588,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
       off = s.x / n;
       const float var = variance(s.y / n, off);
       rstd = 1.0f / sqrtf(var + p.eps * down * down);
-      if (rstd > 0.0f || again) break;
+      if (in_range(rstd) || again) break;
       float most = 0.0f;
       for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
         float v[8];
@@ -588,8 +597,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_wide_kernel(NormArgs p) {
         for (int j = 0; j < 8; ++j) most = __builtin_fmaxf(most, __builtin_fabsf(v[j]));
       }
       most = row_max<kWide>(most, lds);
-      const int e = (int)(__float_as_uint(most) >> 23) - 127;
-      down = pow2f(-(e < 126 ? e : 126));
+      down = scale_down(most, p.root);
     }
     const bool equal = down != 1.0f && equal_values(rstd, p.eps);
     if (equal) rstd = 0.0f;
@@ -862,6 +870,7 @@ hipError_t run(const LayerNorm& c, bool grad, hipStream_t s) {
   p.ldy = c.ldy;
   p.ld_add = c.ld_add;
   p.eps = (float)c.eps;
+  p.root = p.eps > 0.0f ? ldexpf(1.0f, ilogbf(p.eps) >> 1) : 0.0f;
   p.past = past_caches(c.rows * c.cols * (c.type == HOBFLOPS_TYPE_F32 ? 4 : 2));
   if (c.type == HOBFLOPS_TYPE_F32) run_type<TypeF32>(c, p, grad, s);
   if (c.type == HOBFLOPS_TYPE_BF16) run_type<TypeBF16>(c, p, grad, s);
