@@ -220,6 +220,19 @@ __device__ __forceinline__ Stats stats_of(float (&x)[NC][kVec<T>], const Chunk<T
   return r;
 }
 
+// xh from the saved statistics: the difference passes float32's range where rstd is small enough, its half does not, nor
+// twice rstd; where rstd is over 1 neither is halved or doubled, as twice the largest ones would pass it. kRow: the whole wave's
+// row is one, and the half takes no vector register.
+template <bool kRow>
+struct Normed {
+  float part, mean, rstd;  // 1/2 or 1; that of the mean; rstd over it
+  __device__ __forceinline__ Normed(float m, float r)
+      : part(r > 1.0f ? 1.0f : 0.5f), mean(part * m), rstd(r > 1.0f ? r : 2.0f * r) {
+    if constexpr (kRow) part = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(part)));
+  }
+  __device__ __forceinline__ float of(float x) const { return __builtin_fmaf(part, x, -mean) * rstd; }
+};
+
 // L lanes of a wave (64 of them but for rows of less than 1 KB), or the NW waves of a workgroup, have a row, a lane NC times 16 bytes of it; the next row is under way
 // while a row's sums meet. 32 values a lane leave no registers for w and b, which come from L2 for each
 // row (4096 x 16392 bfloat16: 110 us, walked 155).
@@ -354,8 +367,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
       ge[c] = gn[c];
       ae[c] = an[c];
     }
-    // half of the difference, which stays within range, and twice rstd
-    const float half = 0.5f * mean, twice = 2.0f * rstd, r = rstd;
+    const Normed<L == 64> normed(mean, rstd);
+    const float r = rstd;
     if (kAhead) load(row + stride < p.rows ? row + stride : row);  // (of the last row again, rather than a branch)
     float2 s{0.0f, 0.0f};
 #pragma unroll
@@ -364,7 +377,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float g = value_of<T>(ge[c], j);
-        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
+        const float xh = normed.of(value_of<T>(xe[c], j));
         const float a = counted<NC>(g * wc[j], c, j, chunk[c].lead);
         s.x += a;
         s.y += a * counted<NC>(xh, c, j, chunk[c].lead);
@@ -384,7 +397,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void norm_grad_kernel(Norm
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float g = value_of<T>(ge[c], j);
-        const float xh = __builtin_fmaf(0.5f, value_of<T>(xe[c], j), -half) * twice;
+        const float xh = normed.of(value_of<T>(xe[c], j));
         if constexpr (kSums) {
           dw[c][j] += g * xh;
           db[c][j] += g;
@@ -517,11 +530,12 @@ __global__ __launch_bounds__(256) void norm_grad_few_kernel(NormArgs p) {
     load_few<T>((const E*)p.x + row * p.ldx, n, x);
     load_few<T>((const E*)p.dy + row * p.ldy, n, g);
     if (p.add) load_few<T>((const E*)p.add + row * p.ld_add, n, more);
-    const float half = 0.5f * p.mean[row], r = p.rstd[row], twice = 2.0f * r;
+    const float r = p.rstd[row];
+    const Normed<false> normed(p.mean[row], r);
     float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
     for (int j = 0; j < M; ++j) {
-      x[j] = j < n ? __builtin_fmaf(0.5f, x[j], -half) * twice : 0.0f;
+      x[j] = j < n ? normed.of(x[j]) : 0.0f;
       dw[j] += g[j] * x[j];
       db[j] += g[j];
       s0 += g[j] * w[j];
@@ -626,7 +640,8 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
   int place = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const E *src = (const E*)p.x + row * p.ldx, *dy = (const E*)p.dy + row * p.ldy;
-    const float half = 0.5f * p.mean[row], r = p.rstd[row], twice = 2.0f * r;
+    const float r = p.rstd[row];
+    const Normed<true> normed(p.mean[row], r);
     float2 s{0.0f, 0.0f};
     for (int64_t col = (int64_t)threadIdx.x * 8; col < p.cols; col += kWide * 64 * 8) {
       float x[8], g[8], w[8];
@@ -637,7 +652,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
       for (int j = 0; j < 8; ++j) {
         const float a = p.w ? g[j] * w[j] : g[j];
         s.x += a;
-        s.y += a * (__builtin_fmaf(0.5f, x[j], -half) * twice);
+        s.y += a * normed.of(x[j]);
       }
     }
     s = row_sums<kWide>(s, lds, place);
@@ -653,7 +668,7 @@ __global__ __launch_bounds__(kWide * 64) void norm_grad_wide_kernel(NormArgs p) 
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float a = p.w ? g[j] * w[j] : g[j];
-        x[j] = r * (a - s.x - (__builtin_fmaf(0.5f, x[j], -half) * twice) * s.y) + (p.add ? more[j] : 0.0f);
+        x[j] = r * (a - s.x - normed.of(x[j]) * s.y) + (p.add ? more[j] : 0.0f);
       }
       store_values<T, 8>((E*)p.dx + row * p.cols, col, p.cols, x);
     }
@@ -668,10 +683,10 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs p) {
   if (col >= p.cols) return;
   float dw[8] = {}, db[8] = {};
   const auto add = [&](const float (&x)[8], const float (&g)[8], int64_t row) {
-    const float half = 0.5f * p.mean[row], twice = 2.0f * p.rstd[row];
+    const Normed<true> normed(p.mean[row], p.rstd[row]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      dw[j] += g[j] * (__builtin_fmaf(0.5f, x[j], -half) * twice);
+      dw[j] += g[j] * normed.of(x[j]);
       db[j] += g[j];
     }
   };

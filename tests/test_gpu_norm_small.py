@@ -63,3 +63,71 @@ def test_equal_small_values(cols, eps):
     assert torch.equal(saved.mean, x[:, 0])
     assert torch.allclose(saved.rstd.double(), torch.full((6,), eps ** -0.5, dtype=torch.float64, device="cuda"),
                           rtol=4 * D, atol=0)
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_small_rows(cols, dtype):
+    """Up to the largest rstd that a float32 holds (dy small enough for dx to be one too). xh is formed from the saved mean, which
+    is D of it, and 2^-150 as a subnormal, off."""
+    hf = need_gpu()
+    say("norm small gradients", cols, dtype)
+    g = torch.Generator().manual_seed(2)
+    powers = (0, -60, -100, -120, -124, -126)
+    x = torch.randn(3 * len(powers), cols, generator=g, dtype=torch.float64)
+    x[:, 0] += 0.5
+    # deviations of 1, 3/4 and 9/16: the last row's rstd is 2^126.8
+    x = (x - x.mean(1, keepdim=True)) / x.std(1, keepdim=True, unbiased=False)
+    x = x * torch.tensor([s * 2.0 ** k for k in powers for s in (1, 0.75, 0.5625)], dtype=torch.float64)[:, None]
+    x[0] += 20
+    xt = x.float().to(TYPES[dtype]).cuda()
+    x = xt.double().cpu().numpy()
+    gt = (torch.randn(len(x), cols, generator=g) * 2.0 ** -30).to(TYPES[dtype]).cuda()
+    dy = gt.double().cpu().numpy()
+    wt, w = _vector(cols, "f32", 4, 1.0)
+    _, saved = hf.layer_norm(xt, wt, None, 0.0, save=True)
+    _, mu, rstd, xh = ref.layer_norm(x, w, 0.0, 0.0)
+    assert saved.rstd.isfinite().all() and rstd.max() > 2.0 ** 126.5
+    dx, dw, db = hf.layer_norm_backward(gt, xt, saved, wt)
+    n = _chain(cols)
+    ex = _ex(xh, cols) + D * np.abs(mu) * rstd + 2 * D * np.abs(xh) + 2.0 ** -150 * rstd
+    want, ww, wb = ref.layer_norm_grad(dy, xh, rstd, w)
+    a = dy * w
+    ma, mh = np.abs(a).mean(1, keepdims=True), np.abs(a * xh).mean(1, keepdims=True)
+    pair = np.abs((a * xh).mean(1, keepdims=True))
+    err = rstd * (D * (4 * np.abs(a) + (n + 4) * ma + np.abs(xh) * (n + 4) * mh)
+                  + np.abs(xh) * (np.abs(a) * ex).mean(1, keepdims=True) + ex * pair)
+    err = err + (n / 2 + 8) * D * np.abs(want) + 3 * D * np.abs(want)
+    _check(dx, want, err, dtype)
+    _check(dw, ww, (np.abs(dy) * ex).sum(0) + (len(x) + 2) * D * np.abs(dy * xh).sum(0), "f32")
+    _check(db, wb, len(x) * D * np.abs(dy).sum(0), "f32")
+
+
+@pytest.mark.parametrize("cols", [3, 64, 3000, 20000, 40000])
+def test_gradients_of_the_largest_rstd(cols):
+    """Rows of two values whose deviation is 2^-127.5: rstd is float32's last power of two and a half, xh is -1 and 1."""
+    hf = need_gpu()
+    say("norm small largest rstd", cols)
+    d = round(2.0 ** 21.5) * 2.0 ** -149
+    sign = torch.ones(cols, dtype=torch.float64)
+    sign[:cols // 2] = -1.0
+    if cols % 2:
+        sign[-1] = 0.0
+    xt = (sign * d).float()[None, :].repeat(5, 1).cuda()
+    x = xt.double().cpu().numpy()
+    g = torch.Generator().manual_seed(3)
+    gt = (torch.randn(5, cols, generator=g) * 2.0 ** -30).cuda()
+    dy = gt.double().cpu().numpy()
+    _, saved = hf.layer_norm(xt, None, None, 0.0, save=True)
+    _, mu, rstd, xh = ref.layer_norm(x, 1.0, 0.0, 0.0)
+    assert (rstd > 2.0 ** 127.4).all() and saved.rstd.isfinite().all()
+    dx, dw, db = hf.layer_norm_backward(gt, xt, saved)
+    n = _chain(cols)
+    ex = _ex(xh, cols) + 2 * D * np.abs(xh) + 2.0 ** -150 * rstd
+    want, ww, _ = ref.layer_norm_grad(dy, xh, rstd, 1.0)
+    ma, mh = np.abs(dy).mean(1, keepdims=True), np.abs(dy * xh).mean(1, keepdims=True)
+    pair = np.abs((dy * xh).mean(1, keepdims=True))
+    err = rstd * (D * (4 * np.abs(dy) + (n + 4) * ma + np.abs(xh) * (n + 4) * mh)
+                  + np.abs(xh) * (np.abs(dy) * ex).mean(1, keepdims=True) + ex * pair)
+    _check(dx, want, err + (n / 2 + 11) * D * np.abs(want), "f32")
+    _check(dw, ww, (np.abs(dy) * ex).sum(0) + 7 * D * np.abs(dy * xh).sum(0), "f32")
