@@ -409,7 +409,7 @@ int hobflops_w4_gated(const void* x, int type, int64_t T, int64_t K, int64_t N, 
  * eps as a float32. Sums in float32, one rounding at the end. Any finite row has its result, also where its squares leave
  * float32's range, above or below; NaN and infinities make their own row NaN. With eps 0 a row of one value has rstd
  * infinity and is NaN. y may be x (the same rows) and otherwise overlaps no input (HOBFLOPS_EINVAL). mean and rstd, float32 [rows], are for the backward pass
- * (both or neither NULL); an rstd beyond float32's range is infinity. */
+ * (both or neither NULL) and overlap nothing else (HOBFLOPS_EINVAL); an rstd beyond float32's range is infinity. */
 typedef struct {
   int64_t rows, cols;
   int64_t ldx, ldy, ld_add; /* ldy: rows of y, or of its gradient dy */

@@ -815,9 +815,10 @@ int hobflops_layer_norm(const hobflops_norm_desc* d, const void* x, const void* 
   if (!aligned_to(x, b) || !aligned_to(y, b) || !aligned_to(weight, wb) || !aligned_to(bias, wb) ||
       !aligned_to(mean, 4) || !aligned_to(rstd, 4))
     return HOBFLOPS_EALIGN;
-  const Rows in{x, d->rows, d->cols, d->ldx, b}, out{y, d->rows, d->cols, d->ldy, b};
-  if ((overlap(in, out) && !same_rows(in, out)) || overlap(out, Rows{weight, 1, d->cols, d->cols, wb}) ||
-      overlap(out, Rows{bias, 1, d->cols, d->cols, wb}))
+  const Rows out[] = {{y, d->rows, d->cols, d->ldy, b}, {mean, 1, d->rows, d->rows, 4}, {rstd, 1, d->rows, d->rows, 4}};
+  const Rows in[] = {{weight, 1, d->cols, d->cols, wb}, {bias, 1, d->cols, d->cols, wb}, {x, d->rows, d->cols, d->ldx, b}};
+  // (y may be x)
+  if (any_overlap(out, 3, in, same_rows(in[2], out[0]) ? 2 : 3) || overlap(out[1], in[2]) || overlap(out[2], in[2]))
     return HOBFLOPS_EINVAL;
   LayerNorm p{d->rows, d->cols, d->ldx, d->ldy, 0, d->type, d->wtype, d->eps};
   p.x = x;
