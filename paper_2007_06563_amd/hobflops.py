@@ -935,7 +935,11 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
                   grad_scale, step, seed, lr_at, step_at, scale_at, skip_at)
     table = array.array("q", words)
     _call(dev, lib().hobflops_adamw, ctypes.byref(d), table.buffer_info()[0], n, pm, ps, pv, pt, total)
-    # what autograd has kept of these tensors is not theirs any more
+    # what autograd has kept of these tensors is not theirs any more (those without a gradient are as they were)
+    given = words[1::4]
+    if 0 in given:
+        params = [p for p, g in zip(params, given) if g]
+        copies = copies and [c for c, g in zip(copies, given) if g]
     torch.autograd.graph.increment_version(params)
     if ctype is not None:
         torch.autograd.graph.increment_version([c for c in copies if c is not None])
