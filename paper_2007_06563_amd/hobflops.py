@@ -494,6 +494,12 @@ def _out_rows(t, shape, dtype, device, name):
     return t, ptr, ld
 
 
+def _written(out):
+    """Says that a call has written a caller's output: what autograd has kept of it is not there any more."""
+    if out is not None:
+        torch.autograd.graph.increment_version(out)
+
+
 def block_shapes(rows, cols, f, group=32):
     """The shapes of the codes and of the scales of a [rows, cols] matrix in blocks."""
     bits = 1 + sum(f) if isinstance(f, tuple) else 1 + f.wE + f.wF
@@ -510,6 +516,7 @@ def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
     of the narrow format f ((4, 3), (5, 2): 8 bits, (2, 1): 4 bits), uint8, and the scales of
     their groups: (codes, scales). 8-bit codes take groups of 32 and SCALE_POW2."""
     f = fmt(f)
+    given = codes, scales
     ptr, rows, cols, ld = _rows(src, "block_pack src")
     kind = _type(src, "block_pack src")
     cshape, sshape = _block_shapes(rows, cols, f, group)
@@ -525,6 +532,8 @@ def block_pack(src, f, group=32, scale=SCALE_POW2, codes=None, scales=None):
     else:
         ps = _dense(scales, sshape, stype, dev, "block_pack scales")
     _call(dev, lib().hobflops_block_pack, ptr, kind, rows, cols, ld, f, group, scale, pc, ps)
+    for t in given:
+        _written(t)
     return codes, scales
 
 
@@ -541,10 +550,11 @@ def block_unpack(codes, scales, cols, f, group=32, dtype=torch.float32, out=None
     ps = _dense(scales, sshape, scales.dtype, dev, "block_unpack scales")
     if out is not None:
         dtype = out.dtype
-    out, ptr, ld = _out_rows(out, (rows, cols), dtype, dev, "block_unpack out")
+    y, ptr, ld = _out_rows(out, (rows, cols), dtype, dev, "block_unpack out")
     _call(dev, lib().hobflops_block_unpack, pc, ps, rows, cols, f, group, _SCALES[scales.dtype], ptr,
-          _type(out, "block_unpack out"), ld)
-    return out
+          _type(y, "block_unpack out"), ld)
+    _written(out)
+    return y
 
 
 def _gated_weights(x, w_gate, w_up):
@@ -609,11 +619,13 @@ def gated_forward(x, w_gate, w_up, act=GATE_SILU, ckpt=None, out=None):
     forward = lib().hobflops_gated_forward
     if ckpt is None:
         _call(x.device, forward, ctypes.byref(d), px, pg, pu, ph, None, None, None, None, pw, nw)
+        _written(out)
         return h
     cshape, sshape = block_shapes(T, F, f)
     blocks = [torch.empty(s, dtype=torch.uint8, device=x.device)
               for s in (cshape, sshape, cshape, sshape)]
     _call(x.device, forward, ctypes.byref(d), px, pg, pu, ph, *[b.data_ptr() for b in blocks], pw, nw)
+    _written(out)
     return h, GatedSaved(block_pack(x, f), tuple(blocks[:2]), tuple(blocks[2:]), f)
 
 
@@ -665,6 +677,7 @@ def w4_linear(x, codes, scales, group=32, out=None):
     y, head, tail = _w4(x, (codes, scales), group, out, "w4_linear")
     _no_gradient("w4_linear", x)
     _call(x.device, lib().hobflops_w4_linear, *head, *tail)
+    _written(out)
     return y
 
 
@@ -673,6 +686,7 @@ def w4_gated(x, g_codes, g_scales, u_codes, u_scales, act=GATE_SILU, group=32, o
     y, head, tail = _w4(x, (g_codes, g_scales, u_codes, u_scales), group, out, "w4_gated")
     _no_gradient("w4_gated", x)
     _call(x.device, lib().hobflops_w4_gated, *head, act, *tail)
+    _written(out)
     return y
 
 
@@ -737,6 +751,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, out=None):
                           torch.empty(rows, dtype=torch.float32, device=dev))
         pm, pr = saved.mean.data_ptr(), saved.rstd.data_ptr()
     _call(dev, lib().hobflops_layer_norm, d, px, pw, pb, py, pm, pr)
+    _written(out)
     return (y, saved) if save else y
 
 
@@ -788,6 +803,7 @@ def linear(x, w, bias=None, act=None, residual=None, save=False, out=None):
     ws, pws, n = _bytes_of(lib().hobflops_linear_workspace, dev, d, 0)
     _call(dev, lib().hobflops_linear, d, px, pw, pb, pr, py,
           None if z is None else z.data_ptr(), pws, n)
+    _written(out)
     return (y, z) if save else y
 
 
@@ -940,6 +956,7 @@ def adamw(params, grads, state, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
     if 0 in given:
         params = [p for p, g in zip(params, given) if g]
         copies = copies and [c for c, g in zip(copies, given) if g]
-    torch.autograd.graph.increment_version(params)
+    written = [*params, state.m, state.v] if state.fmt is None else [*params, *state.m, *state.v]
     if ctype is not None:
-        torch.autograd.graph.increment_version([c for c in copies if c is not None])
+        written += [c for c in copies if c is not None]
+    torch.autograd.graph.increment_version(written)
