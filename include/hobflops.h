@@ -438,8 +438,9 @@ int hobflops_layer_norm_backward(const hobflops_norm_desc* d, const void* dy, co
  * Sums, z and the activation in float32, one rounding at the end. y may be the residual (same rows), and
  * otherwise overlaps no input (HOBFLOPS_EINVAL). z, if not NULL, receives z [T][N], dense, rounded to the type: what the backward pass
  * needs of an activation.
- * With align 16 and K, ldx and ldw multiples of 8 the kernels read x and w in place; else a call of more than a few
- * tokens copies what it must into the workspace first. */
+ * Forward, x and w are each read in place where align is 4 or more and their rows are an even number of values apart, below
+ * 2^21; few tokens and small layers are whatever the alignment. Backward, x and w are with align 16 and K and ldx, or ldw, multiples
+ * of 8, the latter below 2^21, and dy without an activation with N and ldy so. What is not is copied into the workspace first. */
 enum { HOBFLOPS_GATE_NONE = -1 };
 enum { HOBFLOPS_NEED_DX = 1, HOBFLOPS_NEED_DW = 2, HOBFLOPS_NEED_DBIAS = 4 };
 typedef struct {

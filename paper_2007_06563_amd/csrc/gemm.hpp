@@ -1,8 +1,8 @@
-// The matrix products of the gated block: 16-bit operands, float32 sums.
+// The matrix products of the gated block and of the linear layer: 16-bit operands, float32 sums.
 //
 // A workgroup computes a tile of BI x BJ sums, D[i][j] = sum_k A[i][k] B[j][k], 64 of
 // k at a time. The tiles of A and B go from global memory straight into LDS (buffer
-// loads with the LDS as their target, 16 bytes a lane), into one of two or three stages while the
+// loads with the LDS as their target, 16 bytes a lane), into one of two to eight stages while the
 // matrix instructions work on another. Two layouts of an operand in memory:
 //  - K-contiguous ([row][k], the weights and x of the forward product): an LDS row is 64
 //    k (128 bytes), and a fragment (8 k of a row a lane) is one 16-byte LDS read.
@@ -15,8 +15,9 @@
 //
 // Rows and k beyond an operand's end come back as zero from the buffer descriptor's
 // range check (K-contiguous rows: lanes whose k is beyond the end are given an offset out
-// of range), so that no element of a neighbouring row takes part in a sum. Operands have 16-byte
-// aligned rows; the K of a K-contiguous one is a multiple of 8.
+// of range), so that no element of a neighbouring row takes part in a sum. Rows begin at 16 bytes, or
+// in the linear layer's forward products, K-contiguous both, at whole words, which is what the loads need; the
+// K of a K-contiguous operand is a multiple of 8.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
