@@ -460,7 +460,7 @@ int hobflops_linear(const hobflops_linear_desc* d, const void* x, const void* w,
 /* Gradients from dy [T][N] (rows ldy apart) and z:
  *   dz = dy act'(z) (act' of max(z, 0) is 0 at 0; of an infinite z, as one beyond float16 is kept, 0 or 1), dx = dz w [T][K], dw = dz^T x [N][K], dbias = sum over tokens of dz
  * all dense and of d->type; those that are NULL are not computed, none overlaps another or an input (HOBFLOPS_EINVAL). The residual's gradient is dy. dz is rounded
- * to d->type before the products (dbias is summed before that), whose sums are float32. z is needed with an
+ * to d->type before the products (a float16 dz beyond 65504 is an infinity; dbias is summed before that), whose sums are float32. z is needed with an
  * activation, x for dw, w for dx. With T = 0 dw and dbias are zero. Sums run in a fixed order. */
 int hobflops_linear_backward(const hobflops_linear_desc* d, const void* dy, const void* x,
                              const void* w, const void* z, void* dx, void* dw, void* dbias,

@@ -3,7 +3,7 @@
 //   p = p (1 - lr decay) - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // HBM-bound: every tensor is read and written once, in one launch for up to 64 of them (their
 // addresses are kernel arguments). A thread takes 4 values at a time: 138 M values with bfloat16 gradients and copies
-// 715 us (5.4 TB/s of 28 bytes a value), with 8-bit states 436 (5.1, of 16.1 bytes); 2.16 M with float32 gradients 11.8, from
+// 715 us (5.4 TB/s of 28 bytes a value), with 8-bit states 418 (5.3, of 16.1 bytes); 2.16 M with float32 gradients 11.8, from
 // the last cache; forty tensors of 0.8 M values 8.1, a launch and one round's latency.
 //
 // All operations are float32 ones, each rounded (no multiply-add takes two of them together), so

@@ -628,7 +628,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs
 }
 
 // Workgroups of dx, as many as `parts`, then those of dW: both products in one launch, so that dW's first tiles fill the
-// CUs that dx's last ones leave. 4096 x 4096 -> 11264: 548 to 560 us (1.35 to 1.38 PFLOP/s), matrix instructions busy 79 %.
+// CUs that dx's last ones leave. 4096 x 4096 -> 11264: 534 to 560 us (1.35 to 1.42 PFLOP/s), matrix instructions busy 79 %.
 template <class T, int B, int WJ, int S>
 __device__ __forceinline__ void linear_grad_tiles(const GradArgs& dx, const GradArgs& dw, uint32_t parts,
                                                   uint8_t* const (&sa)[S], uint8_t* const (&sb)[S]) {
