@@ -331,7 +331,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& p, uint8_t* const 
 }
 
 // 256 x 256 sums a workgroup, eight waves, one workgroup on a CU. Bound by the matrix instructions and the clock under them:
-// 8192 x 11264 -> 4096 536 to 569 us from card to card (1.33 to 1.41 PFLOP/s; a library product 473 to 482), the
+// 8192 x 11264 -> 4096 536 to 595 us from card to card (1.27 to 1.41 PFLOP/s; a library product 473 to 482), the
 // instructions busy 75 % of the time; 4096 x 4096 -> 11264 with gelu, z and residual 327 to 345, 59 %: 704 tiles are 2.75 rounds
 // that take 3, and a round's epilogue, 14 us, has nothing beside it.
 template <class T>
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DzArgs p, AlignArgs
 }
 
 // Workgroups of dx, as many as `parts`, then those of dW: both products in one launch, so that dW's first tiles fill the
-// CUs that dx's last ones leave. 4096 x 4096 -> 11264: 534 to 560 us (1.35 to 1.42 PFLOP/s), matrix instructions busy 79 %.
+// CUs that dx's last ones leave. 4096 x 4096 -> 11264: 534 to 581 us from card to card (1.30 to 1.42 PFLOP/s), matrix instructions busy 79 %.
 template <class T, int B, int WJ, int S>
 __device__ __forceinline__ void linear_grad_tiles(const GradArgs& dx, const GradArgs& dw, uint32_t parts,
                                                   uint8_t* const (&sa)[S], uint8_t* const (&sb)[S]) {
